@@ -329,6 +329,105 @@ coral_status coral_lmhead_dense(const void *hidden, const void *lm_W, int M, int
                                 size_t workspace_bytes, void *hip_stream);
 
 /*
+ * Products with 4-bit weights and a scale per group of columns: an LM head, the router's pre-mix
+ * (act = CORAL_ACT_SILU, residual = x) or a drafter's projections at a quarter of the bytes.
+ *   y[m,n] = act(sum_j x[m,j] * w[n,j] + bias[n]) + residual[m,n]
+ *   w[n,j] = scales[n, j / group] * (code[n,j] - zeros[n, j / group])      CORAL_W4_INT
+ *   w[n,j] = scales[n, j / group] * e2m1(code[n,j])                        CORAL_W4_E2M1
+ * e2m1: sign, two exponent bits, one mantissa bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives.
+ * Products are exact and summed in fp32 for every storage type; bias, activation and residual are
+ * applied in fp32 and y is rounded once.  Weights need no preparation: codes, scales and zeros are
+ * row-major as a checkpoint holds them.
+ *   x        [device] [M,K] storage type dt, 16-byte aligned
+ *   codes    [device] [N,K/2] bytes, column 2j in the low half of byte j, 16-byte aligned
+ *   scales   [device] [N, ceil(K / group)] storage type dt
+ *   zeros    [device] [N, ceil(K / group)] uint8, or NULL for 8; NULL with CORAL_W4_E2M1
+ *   bias     [device] [N] fp32, or NULL
+ *   residual [device] [M,N] storage type dt, or NULL
+ *   out_dt   CORAL_F32, or dt
+ *   y        [device] out [M,N] of out_dt; overlaps no input, but may be the residual itself where
+ *            out_dt is dt
+ * Limits: 1 <= M <= 64; K a multiple of 8, at most CORAL_W4_MAX_K; group 32, 64 or a multiple of 128
+ * (the last one may be cut short by K).  Values of x must be finite: the results of a token with
+ * another value are unspecified, the other tokens' are not.  Needs no workspace.
+ */
+typedef enum {
+    CORAL_W4_INT = 0,
+    CORAL_W4_E2M1 = 1
+} coral_w4_code;
+
+#define CORAL_W4_MAX_K (1 << 20)
+
+coral_status coral_matvec_w4(const void *x, const void *codes, const void *scales,
+                             const void *zeros, const float *bias, const void *residual, int M,
+                             int N, int K, int group, coral_w4_code code, coral_dtype dt,
+                             coral_activation act, coral_dtype out_dt, void *y,
+                             void *hip_stream);
+
+/*
+ * Rules on a step's logits z[m,v], in this order, each operation rounded to fp32:
+ *   repetition  z > 0 ? z / r : z * r   where v is in the row's prompt or output   (r > 0)
+ *   frequency   z - count * f           count: how often v is in the row's output
+ *   presence    z - p                   where count > 0
+ *   bias        z + b                   the last entry for v in the row's list of biases
+ *   mask        -inf                    where v's bit is 0
+ * The struct is host memory; a part that is not wanted is NULL with its companions.
+ *   history        [device] [n_history] token ids, all rows' together
+ *   history_ranges [device] [M,4]: begin and end of the row's prompt, begin and end of its output,
+ *                  as places of history; rows may share ranges (the nodes of a draft tree their
+ *                  prompt)
+ *   penalties      [device] [M,3] fp32: r, f, p.  history may be NULL where n_history is 0
+ *   bias_ids, bias_values [device] [n_biases]; bias_ranges [device] [M,2]: begin and end; rows may
+ *                  share ranges
+ *   mask           [device] [M, ceil(V / 32)] words, bit v % 32 of word v / 32
+ * Ranges are cut to the arrays, and ids outside 0..V-1 are passed over.
+ */
+typedef struct {
+    const int32_t *history;
+    const int32_t *history_ranges;
+    const float *penalties;
+    const int32_t *bias_ids;
+    const float *bias_values;
+    const int32_t *bias_ranges;
+    const uint32_t *mask;
+    int32_t n_history;                  /* at most 2^30, as n_biases */
+    int32_t n_biases;
+} coral_logit_rules;
+
+#define CORAL_LOGITS_MAX_V 1000000
+
+/*
+ * The logits under their rules, rounded once to the storage type.
+ *   logits [device] [M,V] storage type dt, 16-byte aligned
+ *   rules  [host]   or NULL for none
+ *   out    [device] out [M,V] of dt, 16-byte aligned: logits itself, or memory that overlaps neither
+ *          them nor the rules
+ * Masked places hold -inf whatever the logits hold there, NaN too; a row whose mask leaves nothing
+ * holds -inf throughout.  Limits: 1 <= M <= 64, V <= CORAL_LOGITS_MAX_V.  Needs no workspace.
+ */
+coral_status coral_logits_adjust(const void *logits, const coral_logit_rules *rules, int M, int V,
+                                 coral_dtype dt, void *out, void *hip_stream);
+
+/*
+ * The k best tokens of every row under the rules, and their log-probabilities: what
+ * coral_tree_expand takes and sampling needs, with the logits read once and nothing written back.
+ *   topk_ids     [device] out [M,k] int32, best first; equal values: lower id first
+ *   topk_logprob [device] out [M,k] fp32: z' - log sum_v exp(z'[m,v]), z' the logits under the rules
+ *                (not rounded to the storage type)
+ * A value of -inf or NaN is no candidate and adds nothing to the sum; slots beyond the row's last
+ * candidate hold (-1, -inf).  With a value of +inf the row's log-probabilities are unspecified.
+ *   workspace [device] at least coral_logits_topk_workspace_bytes(M, V, k) bytes, 256-byte aligned,
+ *             prepared once by coral_lmhead_workspace_init (or filled with zeros); one that the heads
+ *             use serves too, for calls that do not overlap.  Outputs overlap neither it nor an input.
+ * Limits: 1 <= M <= 64, 1 <= k <= 64, k <= V <= CORAL_LOGITS_MAX_V.
+ */
+size_t coral_logits_topk_workspace_bytes(int M, int V, int k);
+
+coral_status coral_logits_topk(const void *logits, const coral_logit_rules *rules, int M, int V,
+                               int k, coral_dtype dt, int32_t *topk_ids, float *topk_logprob,
+                               void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * Measurement variants: identical to coral_lmhead_grouped / coral_lmhead_grouped_logprob /
  * coral_lmhead_dense (same operation of section 3.3, same arguments, same results), and in addition
  * bind two caller-created HIP events (hipEvent_t passed as void*, created with

@@ -37,6 +37,13 @@ class _GroupIndexStruct(ctypes.Structure):
                 ("group_rows", ctypes.c_void_p)]
 
 
+class _LogitRulesStruct(ctypes.Structure):
+    _fields_ = [("history", ctypes.c_void_p), ("history_ranges", ctypes.c_void_p),
+                ("penalties", ctypes.c_void_p), ("bias_ids", ctypes.c_void_p),
+                ("bias_values", ctypes.c_void_p), ("bias_ranges", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("n_history", ctypes.c_int32), ("n_biases", ctypes.c_int32)]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -91,6 +98,15 @@ def _load():
     L.coral_lmhead_grouped_routed.argtypes = [c.c_void_p] * 5 + [c.POINTER(_GroupIndexStruct)] + \
                                              [c.c_int] * 7 + [c.c_void_p] * 4 + \
                                              [c.c_size_t, c.c_void_p]
+    L.coral_matvec_w4.restype = c.c_int
+    L.coral_matvec_w4.argtypes = [c.c_void_p] * 6 + [c.c_int] * 8 + [c.c_void_p] * 2
+    L.coral_logits_adjust.restype = c.c_int
+    L.coral_logits_adjust.argtypes = [c.c_void_p, c.POINTER(_LogitRulesStruct)] + [c.c_int] * 3 + [c.c_void_p] * 2
+    L.coral_logits_topk_workspace_bytes.restype = c.c_size_t
+    L.coral_logits_topk_workspace_bytes.argtypes = [c.c_int] * 3
+    L.coral_logits_topk.restype = c.c_int
+    L.coral_logits_topk.argtypes = [c.c_void_p, c.POINTER(_LogitRulesStruct)] + [c.c_int] * 4 + \
+                                   [c.c_void_p] * 3 + [c.c_size_t, c.c_void_p]
     return L
 
 
@@ -458,3 +474,175 @@ def coral_lmhead_dense(hidden: torch.Tensor, lm_W: torch.Tensor, k: int,
         st = _L.coral_lmhead_dense_profiled(*args, events[0], events[1])
     _raise(st)
     return topk_ids, topk_logits
+
+
+# ---------------------------------------------------------------- 4-bit products, rules on logits
+def _same_device_ptr(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> Optional[int]:
+    """Pointer of a contiguous tensor of this type, shape (-1: any) and device; None stays None."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, got {t.device}")
+    if len(shape) != t.dim() or any(n != have and n != -1 for n, have in zip(shape, t.shape)):
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous (row-major, no padding)")
+    return t.data_ptr()
+
+
+def _enqueue(fn, device, stream, *args) -> None:
+    """Calls the library on the tensors' device and the given stream (None: the device's current one)."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif stream.device != device:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+    if device.index == torch.cuda.current_device():
+        st = fn(*args, stream.cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = fn(*args, stream.cuda_stream)
+    if st:
+        _raise(st)
+
+
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """An output tensor whose memory the caching allocator holds for the stream that writes it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+W4_CODES = {"int": 0, "e2m1": 1}
+W4_MAX_K = 1 << 20                   # CORAL_W4_MAX_K of the header
+
+
+def coral_matvec_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = None,
+                    group: int = 128, code_type: str = "int", bias: Optional[torch.Tensor] = None,
+                    residual: Optional[torch.Tensor] = None, act: str = "identity",
+                    out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """coral_matvec_w4 of the C ABI: act(x W^T + bias) + residual with W [N,K] in 4 bits.
+
+    codes [N,K/2] uint8, column 2j in the low half of byte j; scales [N,ceil(K/group)] in x's dtype;
+    zeros the same shape in uint8 (None: 8; none for code_type "e2m1").  out_dtype: float32 (the
+    default) or x's dtype."""
+    dt = _dtype_code(x)
+    if not x.is_cuda:
+        raise ValueError("x must live in device memory")
+    if x.dim() != 2 or codes.dim() != 2:
+        raise ValueError("x and codes must be 2-D")
+    if code_type not in W4_CODES:
+        raise ValueError(f"unknown code type {code_type!r}")
+    if act not in ACTIVATIONS:
+        raise ValueError(f"unknown activation {act!r}")
+    group = int(group)
+    if group < 1:
+        raise ValueError("group must be positive")
+    M, K = x.shape
+    N = codes.shape[0]
+    n_groups = -(-K // group)
+    if out is not None:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out must be {out_dtype}, got {out.dtype}")
+        out_dtype = out.dtype
+    elif out_dtype is None:
+        out_dtype = torch.float32
+    if out_dtype != torch.float32 and out_dtype != x.dtype:
+        raise TypeError(f"the output must be float32 or {x.dtype}, got {out_dtype}")
+    dev = x.device
+    args = (_same_device_ptr(x, "x", dev, x.dtype, (M, K)),
+            _same_device_ptr(codes, "codes", dev, torch.uint8, (N, K // 2)),
+            _same_device_ptr(scales, "scales", dev, x.dtype, (N, n_groups)),
+            _same_device_ptr(zeros, "zeros", dev, torch.uint8, (N, n_groups)),
+            _same_device_ptr(bias, "bias", dev, torch.float32, (N,)),
+            _same_device_ptr(residual, "residual", dev, x.dtype, (M, N)),
+            M, N, K, group, W4_CODES[code_type], dt, ACTIVATIONS[act],
+            CORAL_F32 if out_dtype == torch.float32 else dt)
+    if out is None:
+        out = _new((M, N), out_dtype, dev, stream)
+    _enqueue(_L.coral_matvec_w4, dev, stream, *args, _same_device_ptr(out, "out", dev, out_dtype, (M, N)))
+    return out
+
+
+def _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias_ranges, mask):
+    """The checked arguments of the calls on logits: (pointer, rules or None, M, V, storage type)."""
+    dt = _dtype_code(logits)
+    if not logits.is_cuda:
+        raise ValueError("logits must live in device memory")
+    if logits.dim() != 2:
+        raise ValueError("logits must be [M,V]")
+    if (history is None) != (ranges is None) or (history is None) != (penalties is None):
+        raise ValueError("history, ranges and penalties go together")
+    if (bias_ids is None) != (bias_values is None) or (bias_ids is None) != (bias_ranges is None):
+        raise ValueError("bias_ids, bias_values and bias_ranges go together")
+    M, V = logits.shape
+    dev = logits.device
+    rules = None
+    if history is not None or bias_ids is not None or mask is not None:
+        i32, f32 = torch.int32, torch.float32
+        n_history = 0 if history is None else history.numel()
+        n_biases = 0 if bias_ids is None else bias_ids.numel()
+        if max(n_history, n_biases) > 1 << 30:
+            raise ValueError("at most 2^30 tokens of history, and biases")
+        rules = ctypes.byref(_LogitRulesStruct(
+            _same_device_ptr(history, "history", dev, i32, (-1,)),
+            _same_device_ptr(ranges, "ranges", dev, i32, (M, 4)),
+            _same_device_ptr(penalties, "penalties", dev, f32, (M, 3)),
+            _same_device_ptr(bias_ids, "bias_ids", dev, i32, (-1,)),
+            _same_device_ptr(bias_values, "bias_values", dev, f32, (n_biases,)),
+            _same_device_ptr(bias_ranges, "bias_ranges", dev, i32, (M, 2)),
+            _same_device_ptr(mask, "mask", dev, i32, (M, -(-V // 32))), n_history, n_biases))
+    return _same_device_ptr(logits, "logits", dev, logits.dtype, (M, V)), rules, M, V, dt
+
+
+def coral_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
+                        ranges: Optional[torch.Tensor] = None, penalties: Optional[torch.Tensor] = None,
+                        bias_ids: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                        bias_ranges: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """coral_logits_adjust of the C ABI: logits [M,V] under their rules, in their dtype.
+
+    history [T] int32 token ids with ranges [M,4] int32 (prompt begin and end, output begin and end)
+    and penalties [M,3] float32 (repetition, frequency, presence); bias_ids [B] int32 and bias_values
+    [B] float32 with bias_ranges [M,2] int32; mask [M,ceil(V/32)] int32, bit v % 32 of word v // 32.
+    out may be logits itself."""
+    ptr, rules, M, V, dt = _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias_ranges, mask)
+    if out is None:
+        out = _new((M, V), logits.dtype, logits.device, stream)
+    _enqueue(_L.coral_logits_adjust, logits.device, stream, ptr, rules, M, V, dt,
+             _same_device_ptr(out, "out", logits.device, logits.dtype, (M, V)))
+    return out
+
+
+def coral_logits_topk_workspace_bytes(M: int, V: int, k: int) -> int:
+    return int(_L.coral_logits_topk_workspace_bytes(M, V, k))
+
+
+def coral_logits_topk(logits: torch.Tensor, k: int, history: Optional[torch.Tensor] = None,
+                      ranges: Optional[torch.Tensor] = None, penalties: Optional[torch.Tensor] = None,
+                      bias_ids: Optional[torch.Tensor] = None, bias_values: Optional[torch.Tensor] = None,
+                      bias_ranges: Optional[torch.Tensor] = None, mask: Optional[torch.Tensor] = None,
+                      topk_ids: Optional[torch.Tensor] = None, topk_logprob: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """coral_logits_topk of the C ABI: (ids, log-probabilities), each [M,k], of the k best tokens per
+    row under the rules (arguments as for coral_logits_adjust); (-1, -inf) behind a row's last
+    candidate.  workspace: prepared by coral_lmhead_workspace_init or zeros, and not shared by calls
+    that may overlap; None allocates one."""
+    ptr, rules, M, V, dt = _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias_ranges, mask)
+    k = int(k)
+    dev = logits.device
+    if topk_ids is None:
+        topk_ids = _new((M, max(k, 0)), torch.int32, dev, stream)
+    if topk_logprob is None:
+        topk_logprob = _new((M, max(k, 0)), torch.float32, dev, stream)
+    if workspace is None:
+        workspace = _new((max(coral_logits_topk_workspace_bytes(M, V, k), 1 << 15),), torch.uint8, dev, stream)
+        _enqueue(_L.coral_lmhead_workspace_init, dev, stream, workspace.data_ptr(), workspace.numel())
+    ws = _same_device_ptr(workspace, "workspace", dev, torch.uint8, (-1,))
+    _enqueue(_L.coral_logits_topk, dev, stream, ptr, rules, M, V, k, dt,
+             _same_device_ptr(topk_ids, "topk_ids", dev, torch.int32, (M, k)),
+             _same_device_ptr(topk_logprob, "topk_logprob", dev, torch.float32, (M, k)), ws, workspace.numel())
+    return topk_ids, topk_logprob

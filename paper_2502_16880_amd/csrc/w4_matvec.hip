@@ -1,0 +1,65 @@
+// Entry point of the products with 4-bit weights (kernels: w4_matvec.h).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "coral_lmhead.h"
+#include "device_utils.h"
+#include "w4_matvec.h"
+
+namespace {
+
+typedef void (*w4_fn)(W4Params);
+
+template <int DT>
+w4_fn pick_kind(int kind) {
+    return kind == kW4Sym ? k_w4<DT, kW4Sym> : kind == kW4Zero ? k_w4<DT, kW4Zero> : k_w4<DT, kW4E2M1>;
+}
+
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+
+}  // namespace
+
+extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const void* scales, const void* zeros,
+                                        const float* bias, const void* residual, int M, int N, int K, int group,
+                                        coral_w4_code code, coral_dtype dt, coral_activation act, coral_dtype out_dt,
+                                        void* y, void* hip_stream) {
+    if (!x || !codes || !scales || !y) return CORAL_ERR_NULL;
+    if (dt != CORAL_F32 && dt != CORAL_BF16 && dt != CORAL_F16) return CORAL_ERR_SHAPE;
+    if (out_dt != CORAL_F32 && out_dt != dt) return CORAL_ERR_SHAPE;
+    if (act != CORAL_ACT_SILU && act != CORAL_ACT_RELU && act != CORAL_ACT_IDENTITY) return CORAL_ERR_SHAPE;
+    if (code != CORAL_W4_INT && code != CORAL_W4_E2M1) return CORAL_ERR_SHAPE;
+    if (code == CORAL_W4_E2M1 && zeros) return CORAL_ERR_SHAPE;
+    if (M < 1 || N < 1 || K < 1 || group < 1) return CORAL_ERR_SHAPE;
+    if (M > kMaxM || K % 8 != 0 || K > CORAL_W4_MAX_K) return CORAL_ERR_UNSUPPORTED;
+    if (group != 32 && group != 64 && group % 128 != 0) return CORAL_ERR_UNSUPPORTED;
+    if (((uintptr_t)x | (uintptr_t)codes) & 15u) return CORAL_ERR_UNSUPPORTED;
+    const size_t w = dt == CORAL_F32 ? 4 : 2, out_w = out_dt == CORAL_F32 ? 4 : 2;
+    if (((uintptr_t)scales & (w - 1)) || ((uintptr_t)residual & (w - 1)) || ((uintptr_t)bias & 3u) || ((uintptr_t)y & (out_w - 1)))
+        return CORAL_ERR_UNSUPPORTED;
+    W4Params p = {};
+    p.n_groups = (int)(((int64_t)K + group - 1) / group);
+    const size_t y_bytes = (size_t)M * N * out_w, n_scales = (size_t)N * p.n_groups;
+    // results are written while other workgroups still read the operands; the residual is read and
+    // its place written by the same thread, so y may be the residual itself
+    if (overlap(y, y_bytes, x, (size_t)M * K * w) || overlap(y, y_bytes, codes, (size_t)N * (K / 2)) ||
+        overlap(y, y_bytes, scales, n_scales * w) || overlap(y, y_bytes, zeros, n_scales) ||
+        overlap(y, y_bytes, bias, (size_t)N * 4) ||
+        (overlap(y, y_bytes, residual, (size_t)M * N * w) && (y != residual || out_w != w)))
+        return CORAL_ERR_UNSUPPORTED;
+    p.x = x;
+    p.codes = static_cast<const unsigned char*>(codes);
+    p.scales = scales;
+    p.zeros = static_cast<const unsigned char*>(zeros);
+    p.bias = bias;
+    p.residual = residual;
+    p.y = y;
+    p.M = M; p.N = N; p.K = K; p.group = group; p.act = (int)act;
+    p.out_f32 = out_dt == CORAL_F32;
+    const int kind = code == CORAL_W4_E2M1 ? kW4E2M1 : zeros ? kW4Zero : kW4Sym;
+    const w4_fn fn = dt == CORAL_F32 ? pick_kind<kF32>(kind) : dt == CORAL_BF16 ? pick_kind<kBF16>(kind) : pick_kind<kF16>(kind);
+    hipLaunchKernelGGL(fn, dim3((N - 1) / 16 + 1, (M + 15) / 16), dim3(kW4Waves * kWave), 0, static_cast<hipStream_t>(hip_stream), p);
+    return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
+}

@@ -1,0 +1,178 @@
+"""The 4-bit products and the rules on logits without a GPU: refusals of the C ABI and of the binding,
+and the oracle against values worked out by hand and against torch."""
+import ctypes
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_16880_amd as coral
+from oracle import operators as plain
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, NULL, SHAPE, GROUP_INDEX, UNSUPPORTED, WORKSPACE, HIP = range(7)
+F32, BF16, F16 = 0, 1, 2
+FAKE = 0x7000_0000_1000          # never dereferenced: every check below fails before a launch
+
+
+def test_header_and_library_agree_on_names_with_digits():
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "coral_lmhead.h")).read(), flags=re.S)
+    names = set(re.findall(r"\b(coral_[a-z0-9_]+)\s*\(", text))
+    assert {"coral_matvec_w4", "coral_logits_adjust", "coral_logits_topk", "coral_logits_topk_workspace_bytes"} <= names
+    lib = ctypes.CDLL(coral.LIB_PATH)
+    assert all(hasattr(lib, n) for n in names)
+
+
+# ---------------------------------------------------------------- refusals
+def matvec(**kw):
+    a = dict(x=FAKE, codes=FAKE + (1 << 30), scales=FAKE + (2 << 30), zeros=None, bias=None, residual=None, M=4, N=64, K=256,
+             group=128, code=0, dt=BF16, act=2, out=F32, y=FAKE + (3 << 30))
+    a.update(kw)
+    return coral._L.coral_matvec_w4(*(a[n] for n in ("x", "codes", "scales", "zeros", "bias", "residual", "M", "N", "K", "group",
+                                                     "code", "dt", "act", "out", "y")), None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(x=None), NULL), (dict(codes=None), NULL), (dict(scales=None), NULL), (dict(y=None), NULL),
+    (dict(dt=3), SHAPE), (dict(act=3), SHAPE), (dict(code=2), SHAPE), (dict(out=F16), SHAPE), (dict(out=7), SHAPE),
+    (dict(code=1, zeros=FAKE), SHAPE), (dict(M=0), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(group=0), SHAPE),
+    (dict(M=-1), SHAPE), (dict(group=-128), SHAPE), (dict(M=65), UNSUPPORTED), (dict(K=252), UNSUPPORTED),
+    (dict(K=(1 << 20) + 8), UNSUPPORTED), (dict(group=16), UNSUPPORTED), (dict(group=96), UNSUPPORTED), (dict(group=192), UNSUPPORTED),
+    (dict(x=FAKE + 8), UNSUPPORTED), (dict(codes=FAKE + (1 << 30) + 4), UNSUPPORTED), (dict(scales=FAKE + (2 << 30) + 1), UNSUPPORTED),
+    (dict(y=FAKE + (3 << 30) + 2), UNSUPPORTED), (dict(bias=FAKE + (4 << 30) + 2), UNSUPPORTED),
+    (dict(residual=FAKE + (4 << 30) + 1), UNSUPPORTED),
+    (dict(y=FAKE), UNSUPPORTED), (dict(y=FAKE + 4 * 256 * 2 - 4), UNSUPPORTED), (dict(y=FAKE + (1 << 30)), UNSUPPORTED),
+    (dict(y=FAKE + (2 << 30)), UNSUPPORTED), (dict(zeros=FAKE + (3 << 30)), UNSUPPORTED), (dict(bias=FAKE + (3 << 30)), UNSUPPORTED),
+    (dict(residual=FAKE + (3 << 30)), UNSUPPORTED),                  # y may be the residual where their types agree only
+    (dict(residual=FAKE + (3 << 30) + 2, out=BF16), UNSUPPORTED),
+])
+def test_matvec_w4_refuses(kw, want):
+    assert matvec(**kw) == want
+
+
+def rules(**kw):
+    a = dict(history=FAKE + (4 << 30), history_ranges=FAKE + (5 << 30), penalties=FAKE + (6 << 30), bias_ids=FAKE + (7 << 30),
+             bias_values=FAKE + (8 << 30), bias_ranges=FAKE + (9 << 30), mask=FAKE + (10 << 30), n_history=100, n_biases=10)
+    a.update(kw)
+    return ctypes.byref(coral._LogitRulesStruct(**a))
+
+
+RULE_REFUSALS = [
+    (dict(history=None), NULL), (dict(history_ranges=None), NULL), (dict(penalties=None), NULL), (dict(bias_ids=None), NULL),
+    (dict(bias_values=None), NULL), (dict(bias_ranges=None), NULL), (dict(n_history=-1), SHAPE), (dict(n_biases=-1), SHAPE),
+    (dict(n_history=(1 << 30) + 1), UNSUPPORTED), (dict(n_biases=(1 << 30) + 1), UNSUPPORTED), (dict(mask=FAKE + 2), UNSUPPORTED),
+    (dict(history=FAKE + 1), UNSUPPORTED), (dict(penalties=FAKE + 2), UNSUPPORTED), (dict(bias_ranges=FAKE + 1), UNSUPPORTED)]
+
+
+def adjust(r=None, **kw):
+    a = dict(logits=FAKE, M=4, V=1000, dt=F32, out=FAKE + (1 << 30))
+    a.update(kw)
+    return coral._L.coral_logits_adjust(a["logits"], r, a["M"], a["V"], a["dt"], a["out"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(logits=None), NULL), (dict(out=None), NULL), (dict(dt=5), SHAPE), (dict(M=0), SHAPE), (dict(V=0), SHAPE),
+    (dict(M=65), UNSUPPORTED), (dict(V=1000001), UNSUPPORTED), (dict(logits=FAKE + 4), UNSUPPORTED),
+    (dict(out=FAKE + (1 << 30) + 4), UNSUPPORTED), (dict(out=FAKE + 16), UNSUPPORTED), (dict(out=FAKE - 16), UNSUPPORTED)])
+def test_logits_adjust_refuses(kw, want):
+    assert adjust(**kw) == want
+
+
+@pytest.mark.parametrize("kw,want", RULE_REFUSALS)
+def test_logits_adjust_refuses_rules(kw, want):
+    assert adjust(rules(**kw)) == want
+    assert topk(rules(**kw)) == want
+
+
+@pytest.mark.parametrize("part", ["history", "history_ranges", "penalties", "bias_ids", "bias_values", "bias_ranges", "mask"])
+def test_outputs_over_the_rules_are_refused(part):
+    assert adjust(rules(**{part: FAKE + (1 << 30) + 64})) == UNSUPPORTED
+    assert topk(rules(**{part: FAKE + (1 << 30)})) == UNSUPPORTED              # the ids
+    assert topk(rules(**{part: FAKE + (3 << 30) + 256})) == UNSUPPORTED        # the workspace
+
+
+def topk(r=None, **kw):
+    a = dict(logits=FAKE, M=4, V=1000, k=8, dt=F32, ids=FAKE + (1 << 30), logp=FAKE + (2 << 30), ws=(FAKE + (3 << 30)) & ~255,
+             ws_bytes=1 << 20)
+    a.update(kw)
+    return coral._L.coral_logits_topk(a["logits"], r, a["M"], a["V"], a["k"], a["dt"], a["ids"], a["logp"], a["ws"], a["ws_bytes"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(logits=None), NULL), (dict(ids=None), NULL), (dict(logp=None), NULL), (dict(dt=-1), SHAPE), (dict(k=0), SHAPE),
+    (dict(V=7), SHAPE), (dict(k=65), UNSUPPORTED), (dict(M=65), UNSUPPORTED), (dict(V=1000001), UNSUPPORTED),
+    (dict(ids=FAKE + (1 << 30) + 2), UNSUPPORTED), (dict(ws=None), WORKSPACE), (dict(ws=FAKE + (3 << 30) + 8), WORKSPACE),
+    (dict(ws_bytes=1 << 10), WORKSPACE), (dict(ids=FAKE), UNSUPPORTED), (dict(logp=FAKE + (1 << 30)), UNSUPPORTED),
+    (dict(ws=FAKE & ~255), UNSUPPORTED), (dict(logp=(FAKE + (3 << 30)) & ~255), UNSUPPORTED)])
+def test_logits_topk_refuses(kw, want):
+    assert topk(**kw) == want
+
+
+def test_topk_workspace_bytes():
+    wb = coral.coral_logits_topk_workspace_bytes
+    assert wb(0, 100, 5) == wb(4, 100, 101) == wb(4, 0, 1) == wb(65, 100, 5) == wb(1, 100, 0) == wb(1, 1000, 65) == wb(1, 1000001, 1) == 0
+    for V, k in ((1, 1), (5000, 10), (152064, 64), (1000000, 64)):
+        sizes = [wb(M, V, k) for M in range(1, 65)]
+        assert all(n % 256 == 0 for n in sizes) and sizes == sorted(sizes)     # it serves fewer rows too
+        assert topk(M=64, V=V, k=k, ws_bytes=sizes[-1] - 1, ids=FAKE + (20 << 30), logp=FAKE + (21 << 30), ws=(FAKE + (30 << 30)) & ~255) == WORKSPACE
+
+
+def test_binding_refuses_host_tensors_and_wrong_types():
+    x, codes, scales = torch.zeros(2, 64), torch.zeros(3, 32, dtype=torch.uint8), torch.zeros(3, 1)
+    with pytest.raises(ValueError, match="device memory"):
+        coral.coral_matvec_w4(x, codes, scales)
+    with pytest.raises(TypeError):
+        coral.coral_matvec_w4(x.double(), codes, scales)
+    with pytest.raises(ValueError, match="device memory"):
+        coral.coral_logits_adjust(torch.zeros(2, 64))
+    with pytest.raises(ValueError, match="device memory"):
+        coral.coral_logits_topk(torch.zeros(2, 64), 4)
+    with pytest.raises(TypeError):
+        coral.coral_logits_topk(torch.zeros(2, 64, dtype=torch.int32), 4)
+
+
+# ---------------------------------------------------------------- the oracle
+def test_oracle_codes_and_weights_by_hand():
+    codes = np.array([[0x10, 0x98, 0xFE, 0x37]], dtype=np.uint8)               # columns 0 1 8 9 14 15 7 3
+    assert plain.unpack(codes).tolist() == [[0, 1, 8, 9, 14, 15, 7, 3]]
+    scales, zeros = np.array([[2.0, 10.0]]), np.array([[1, 3]], dtype=np.uint8)
+    assert plain.w4_weights(codes, scales, None, 4, "int").tolist() == [[-16, -14, 0, 2, 60, 70, -10, -50]]
+    assert plain.w4_weights(codes, scales, zeros, 4, "int").tolist() == [[-2, 0, 14, 16, 110, 120, 40, 0]]
+    assert plain.w4_weights(codes, scales, None, 4, "e2m1").tolist() == [[0, 1, 0, -1, -40, -60, 60, 15]]
+    x = np.zeros((1, 8))
+    x[0, 5] = 3.0
+    assert plain.matvec_w4(x, codes, scales, None, 4).tolist() == [[210.0]]
+    assert plain.matvec_w4(-x, codes, scales, None, 4, act="relu", residual=np.array([[5.0]]), bias=np.array([1.0])).tolist() == [[5.0]]
+    y = plain.matvec_w4(x / 70, codes, scales, None, 4, act="silu")
+    assert math.isclose(y[0, 0], 3 / (1 + math.exp(-3)))
+
+
+def test_oracle_rules_by_hand():
+    z = np.array([[4.0, -4.0, 1.0, 2.0, 3.0, np.nan]])
+    history = np.array([0, 1, 1, 9, 3, -1], dtype=np.int32)                    # prompt 0, output 1 1 9 3
+    got, _ = plain.logit_rules(z, history, np.array([[0, 1, 1, 5]]), np.array([[2.0, 0.5, 0.25]]), np.array([2, 2, 77], np.int32),
+                               np.array([9.0, -1.0, 5.0]), np.array([[0, 99]]), np.array([[0b001111]]))
+    assert got.tolist() == [[2.0, -8.0 - 1.0 - 0.25, 0.0, 1.0 - 0.5 - 0.25, -np.inf, -np.inf]]
+    ids, logp = plain.topk_logprob(got, 5)
+    assert ids.tolist() == [[0, 3, 2, 1, -1]] and logp[0, 4] == -np.inf
+    assert math.isclose(np.exp(logp[0, :4]).sum(), 1.0)
+    ids, logp = plain.topk_logprob(np.array([[1.0, 1.0, 0.0], [-np.inf, np.nan, -np.inf]]), 2)
+    assert ids.tolist() == [[0, 1], [-1, -1]] and np.all(logp[1] == -np.inf)
+
+
+def test_oracle_against_torch():
+    rng = np.random.default_rng(0)
+    z = rng.standard_normal((3, 200)) * 3
+    ids, logp = plain.topk_logprob(z, 7)
+    want = torch.log_softmax(torch.from_numpy(z), dim=1).topk(7, dim=1)
+    assert np.array_equal(ids, want.indices.numpy()) and np.allclose(logp, want.values.numpy(), rtol=0, atol=1e-12)
+    history = rng.integers(0, 200, 60).astype(np.int32)
+    got, err = plain.logit_rules(z, history, np.array([[0, 20, 20, 40]] * 3), np.array([[1.3, 0.2, 0.1]] * 3))
+    prompt, output = (torch.bincount(torch.from_numpy(h).long(), minlength=200) for h in (history[:20], history[20:40]))
+    output = output.double()
+    t = torch.from_numpy(z)
+    t = torch.where((prompt + output) > 0, torch.where(t > 0, t / 1.3, t * 1.3), t) - 0.2 * output - 0.1 * (output > 0).double()
+    assert np.allclose(got, t.numpy(), rtol=0, atol=1e-12) and (err >= 0).all() and err.max() < 5 * 2.0 ** -24 * 20      # five roundings of values below 20
