@@ -1,0 +1,5 @@
+// k_w4_held for fp16 activations.
+#include "coral_lmhead.h"
+#include "w4_kernels.h"
+
+const void* coral_w4_held_f16(int kind, bool fine, int t, int nb) { return w4_held<kF16>(kind, fine, t, nb); }

@@ -24,6 +24,7 @@ struct W4Params {
     const void* residual;       // [M,N] storage type or null
     void* y;                    // [M,N] fp32 or storage type
     int M, N, K, group, n_groups, act, out_f32;
+    unsigned per_group, per_group_inv;           // units of a group (at least one), 2^32 / that, rounded up
 };
 
 constexpr int kW4Waves = 4;
@@ -33,6 +34,13 @@ template <int DT>
 constexpr int kW4Op = DT == kF16 ? kF16 : kBF16; // operand type of the products
 template <int DT>
 constexpr int kW4Parts = DT == kF32 ? 3 : 1;     // operands that an activation is split into
+
+// (w & mask) | bits in one instruction (of two constants the compiler makes two).
+__device__ __forceinline__ unsigned w4_and_or(unsigned w, unsigned mask, unsigned bits) {
+    unsigned o;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(o) : "v"(w), "s"(mask), "v"(bits));
+    return o;
+}
 
 // Eight codes of a dword as 16-bit operands.  Integers: 16 + code, in the order 0 4 1 5 2 6 3 7.
 template <int OP, int KIND>
@@ -52,16 +60,16 @@ __device__ __forceinline__ uint4 w4_operand(unsigned w) {
         }
     } else if constexpr (OP == kF16) {           // four bits at the top of a ten-bit mantissa
         constexpr unsigned kMask = 0x03C003C0u, kSixteen = 0x4C004C00u;
-        o.x = ((w << 6) & kMask) | kSixteen;
-        o.y = ((w << 2) & kMask) | kSixteen;
-        o.z = ((w >> 2) & kMask) | kSixteen;
-        o.w = ((w >> 6) & kMask) | kSixteen;
+        o.x = w4_and_or(w << 6, kMask, kSixteen);
+        o.y = w4_and_or(w << 2, kMask, kSixteen);
+        o.z = w4_and_or(w >> 2, kMask, kSixteen);
+        o.w = w4_and_or(w >> 6, kMask, kSixteen);
     } else {                                     // ... of a seven-bit mantissa
         constexpr unsigned kMask = 0x00780078u, kSixteen = 0x41804180u;
-        o.x = ((w << 3) & kMask) | kSixteen;
-        o.y = ((w >> 1) & kMask) | kSixteen;
-        o.z = ((w >> 5) & kMask) | kSixteen;
-        o.w = ((w >> 9) & kMask) | kSixteen;
+        o.x = w4_and_or(w << 3, kMask, kSixteen);
+        o.y = w4_and_or(w >> 1, kMask, kSixteen);
+        o.z = w4_and_or(w >> 5, kMask, kSixteen);
+        o.w = w4_and_or(w >> 9, kMask, kSixteen);
     }
     return o;
 }
@@ -126,6 +134,278 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
         if (p.out_f32) static_cast<float*>(p.y)[at] = y;
         else static_cast<unsigned short*>(p.y)[at] = narrow16<DT>(y);
     }
+}
+
+// ---------------------------------------------------------------- activations held in registers
+// A workgroup of eight waves streams tiles of 16 weight rows; the waves share the columns in units of
+// 128 (wave w: NB units from w NB on), so a wave's activations are the same for every tile and stay in
+// its registers.  The codes are loaded in the order of memory, several rows a load, and exchanged
+// through a slice of LDS of the wave's own: loaded in the layout of the products, 16 bytes of 16 rows
+// each, a load kept the address unit busy for 130 cycles and the kernel at 4.9 TB/s.  A load's registers
+// are loaded again, with the next tile's codes, as soon as they are in LDS: the wave always has about
+// NB KB on the way.  The tile's scales and zero points, which lie scattered for a lane, are loaded row
+// by row by the whole workgroup one tile ahead and kept in LDS as fp32.  The waves' sums meet in LDS
+// once a tile.
+//
+// Lane 16 q + r takes the 16 bytes of row r that hold columns 32 q to 32 q + 31 of a unit, and product
+// s their dword s: columns 32 q + 8 s ... + 7 of the four chunks q, which is a group or part of one
+// where a group has 128 columns or more.  With finer groups it takes dword q of the four chunks, and
+// product s columns 32 s to 32 s + 31.
+//
+// The operands are read through buffer descriptors, which drop what lies behind their end: rows behind
+// the last one, and tokens and columns behind the activations, read as zero without a comparison.
+// Codes behind a row's last column are another row's and meet activations of zero.
+constexpr int kW4Block = 512;
+constexpr int kW4Held = kW4Block / kWave;
+
+typedef __amdgpu_buffer_rsrc_t w4_buffer;
+// The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed).
+__device__ __forceinline__ w4_buffer w4_view(const void* base, size_t first, size_t bytes) {
+    const size_t left = bytes - first;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,
+                                             left < 0xffffffffu ? (unsigned)left : 0xffffffffu, 0x00020000);
+}
+constexpr int kW4Stream = 2;                     // non-temporal: what is read once
+template <int AUX = 0>
+__device__ __forceinline__ uint4 w4_read16(w4_buffer b, unsigned at, unsigned uniform_at = 0) {
+    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, (int)uniform_at, AUX);
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+// Group of a unit where groups are whole units: unit / (group / 128) by the host's reciprocal.
+__device__ __forceinline__ unsigned w4_group_of(const W4Params& p, unsigned unit) {
+    return p.per_group == 1 ? unit : __umulhi(unit, p.per_group_inv);
+}
+
+// What decides how many workgroups fit a compute unit: the registers that the activations take, in 16s
+// (and room to split fp32 activations).
+constexpr int w4_held_regs(int dt, int t, int nb) { return dt == kF32 ? (t * nb > 1 ? 8 : 4) : t * nb; }
+
+// T tiles of 16 tokens (the next T of them: the next row of workgroups), NB units a wave.
+template <int DT, int KIND, bool FINE, int T, int NB>
+__global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) void k_w4_held(W4Params p) {
+    constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>, XV = DT == kF32 ? 2 : 1;
+    constexpr bool PAIR = KIND == kW4Zero && DT != kF32;     // scale and zero as two 16-bit values of one word
+    constexpr int PER = KIND == kW4Zero && DT == kF32 ? 2 : 1;
+    // A slot is the columns that share a scale: a product's 32 where groups are finer than a unit, else
+    // a unit's.  SL: slots of a row that a thread brings for a tile (the last ones may lie behind the row).
+    constexpr int SLOTS = FINE ? 4 : 1, SL = (NB * kW4Held * SLOTS + 31) / 32, STRIDE = (SL * 32 + 1) * PER;
+    __shared__ float sums[2][kW4Held][T * 256];
+    __shared__ float scales[2][16][STRIDE];                  // (scale, 1 + zero / 16); rows start on different banks
+    __shared__ uint4 codes[kW4Held][16][NB * 4 + 1];         // a wave's own; rows start on different banks
+    __shared__ f32x4_t x_sums[KIND != kW4E2M1 ? kW4Held : 1][NB][SLOTS][T][4];     // of a slot's x, 16 tokens
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane & 15, q = lane >> 4;
+    const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, m0 = blockIdx.y * (T * 16), mine = p.M - m0 < T * 16 ? p.M - m0 : T * 16;
+    const int each = tiles / gridDim.x, more_of = tiles % gridDim.x, wg = blockIdx.x;
+    const int first = wg * each + (wg < more_of ? wg : more_of), end = first + each + (wg < more_of ? 1 : 0);
+
+    // scales: thread (row tid / 32, slots tid % 32 + 32 i)
+    const int s_row = threadIdx.x / 32, s_slot = threadIdx.x % 32;
+    unsigned s_raw[SL], z_raw[SL];
+    const unsigned s_first = (unsigned)s_row * p.n_groups, s_last = s_first + (p.n_groups - 1);
+    auto s_at = [&](int i) {                                 // of the row's slots from the step's first one on
+        const unsigned slot = s_slot + 32 * i;
+        const unsigned at = s_first + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
+        return at < s_last ? at : s_last;
+    };
+    constexpr unsigned W = DT == kF32 ? 4u : 2u;
+    auto load_scales = [&](int tile) {
+        const size_t first_group = (size_t)tile * 16 * p.n_groups, all = (size_t)p.N * p.n_groups;
+        const w4_buffer view = w4_view(p.scales, first_group * W, all * W);
+        const w4_buffer z_view = w4_view(p.zeros, first_group, all);
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            if constexpr (DT == kF32) s_raw[i] = __builtin_amdgcn_raw_buffer_load_b32(view, (int)(s_at(i) * W), 0, 0);
+            else s_raw[i] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(view, (int)(s_at(i) * W), 0, 0);
+            if constexpr (KIND == kW4Zero) z_raw[i] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(z_view, (int)s_at(i), 0, 0);
+        }
+    };
+    auto put_scales = [&](int parity) {
+        float* dst = scales[parity][s_row] + s_slot * PER;
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            const float zero = KIND == kW4Zero ? fmaf((float)z_raw[i], 0.0625f, 1.0f) : 0.f;       // (exact in fp16 too)
+            if constexpr (PAIR) dst[i * 32] = __uint_as_float(s_raw[i] << 16 | __builtin_bit_cast(unsigned short, (_Float16)zero));
+            else dst[i * 32 * PER] = DT == kF32 ? __uint_as_float(s_raw[i]) : widen16<DT>((unsigned short)s_raw[i]);
+            if constexpr (PER == 2) dst[i * 32 * PER + 1] = zero;
+        }
+    };
+    // codes: the wave's 4 NB chunks of 16 rows, dealt to the lanes of its NB loads in the order of memory
+    constexpr int CHUNKS = NB * 4;
+    constexpr bool EVEN = kWave % CHUNKS == 0;               // a load takes whole rows: the next one's are so many rows on
+    uint4 w[NB];
+    unsigned at[EVEN ? 1 : NB];
+#pragma unroll
+    for (int j = 0; j < (EVEN ? 1 : NB); ++j) {
+        const int e = j * kWave + lane;
+        at[j] = (unsigned)(e / CHUNKS) * (unsigned)row_bytes + (unsigned)(wave * CHUNKS + e % CHUNKS) * 16u;
+    }
+    auto read_codes = [&](const w4_buffer& view, int j) {
+        if constexpr (EVEN) return w4_read16<kW4Stream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
+        else return w4_read16<kW4Stream>(view, at[EVEN ? 0 : j]);
+    };
+    auto code_view = [&](int tile) { return w4_view(p.codes, (size_t)tile * 16 * row_bytes, (size_t)p.N * row_bytes); };
+    auto put = [&](int j) {
+        const int e = j * kWave + lane;
+        store_vec(&codes[wave][e / CHUNKS][e % CHUNKS], w[j]);
+    };
+    load_scales(first);
+    uint4 x[T][NB][4][XV];
+    const w4_buffer x_view = w4_view(p.x, 0, (size_t)p.M * p.K * W);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int col = (wave * NB + j) * kW4UnitCols + (FINE ? s * 32 + q * 8 : q * 32 + s * 8);
+                const unsigned off = col < p.K ? ((unsigned)(m0 + t * 16 + r) * (unsigned)p.K + col) * W : 0xffffffe0u;      // (behind the end)
+#pragma unroll
+                for (int v = 0; v < XV; ++v) x[t][j][s][v] = w4_read16(x_view, off + 16u * v);
+            }
+    {
+        const w4_buffer view = code_view(first);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) w[j] = read_codes(view, j);
+    }
+    put_scales(0);
+    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS]) {
+        if constexpr (DT == kF32) {
+            const uint4 a = v[0], b = v[XV - 1];
+            const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                                __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+            w4_split(f, part);
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) part[c] = w4_order<KIND>(part[c]);
+        } else {
+            part[0] = v[0];
+        }
+    };
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    // the offset's part of the sums: of -24 x where every zero point is 8, else of -16 x, times 1 + zero / 16
+    constexpr unsigned kMinus = KIND == kW4Sym ? (OP == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u) : OP == kF16 ? 0xCC00CC00u : 0xC180C180u;
+    const uint4 minus = make_uint4(kMinus, kMinus, kMinus, kMinus);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            f32x4_t sum = zero4;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if constexpr (DT != kF32) x[t][j][s][0] = w4_order<KIND>(x[t][j][s][0]);
+                if constexpr (KIND != kW4E2M1) {
+                    uint4 part[PARTS];
+                    parts_of(x[t][j][s], part);
+                    if (FINE) sum = zero4;
+#pragma unroll
+                    for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(part[c], minus, sum);
+                    if (r == 0 && (FINE || s == 3)) x_sums[wave][j][FINE ? s : 0][t][q] = sum;      // (read by this wave only)
+                }
+            }
+        }
+    __syncthreads();                                         // scales and x_sums are there
+    auto step = [&](int tile, int parity, bool more) {
+        const int next = tile + 1;
+        if (more) load_scales(next);
+        const w4_buffer next_codes = code_view(more ? next : tile);
+        const float* my_scales = scales[parity][r] + wave * (NB * SLOTS * PER);
+        if constexpr (DT == kF32) {                          // (or the parts of all activations are kept in registers)
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s)
+#pragma unroll
+                        for (int v = 0; v < XV; ++v) asm volatile("" : "+v"(x[t][j][s][v].x), "+v"(x[t][j][s][v].y), "+v"(x[t][j][s][v].z), "+v"(x[t][j][s][v].w));
+        }
+        f32x4_t y[T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) y[t] = zero4;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            put(j);
+            if (more) w[j] = read_codes(next_codes, j);      // the registers are free again
+        }
+        // A wave's LDS accesses complete in order; the compiler has to keep the order too, though no
+        // lane reads what it wrote itself.
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            uint4 v;
+            if constexpr (FINE) {                            // dword q of the four chunks: their transposition
+                const unsigned* d = reinterpret_cast<const unsigned*>(&codes[wave][r][j * 4]) + q;
+                v = make_uint4(d[0], d[4], d[8], d[12]);
+            } else {
+                v = load_vec(&codes[wave][r][j * 4 + q]);
+            }
+            f32x4_t acc[T];
+            float scale = 0.f;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                if (FINE || s == 0) {                        // the sums start at the offset's part
+                    const int slot = j * SLOTS + s;
+                    scale = my_scales[slot * PER];
+                    float zero = 0.f;
+                    if constexpr (PER == 2) zero = my_scales[slot * PER + 1];
+                    if constexpr (PAIR) {
+                        const unsigned pair = __float_as_uint(scale);
+                        scale = widen16<DT>((unsigned short)(pair >> 16));
+                        zero = (float)__builtin_bit_cast(_Float16, (unsigned short)pair);
+                    }
+#pragma unroll
+                    for (int t = 0; t < T; ++t) {
+                        acc[t] = zero4;
+                        if constexpr (KIND != kW4E2M1) acc[t] = x_sums[wave][j][s][t][q];
+                        if constexpr (KIND == kW4Zero) {
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) acc[t][v] *= zero;
+                        }
+                    }
+                }
+                const uint4 op = w4_operand<OP, KIND>(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w);
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    uint4 part[PARTS];
+                    parts_of(x[t][j][s], part);
+#pragma unroll
+                    for (int c = PARTS - 1; c >= 0; --c) acc[t] = mfma_tile<OP>(part[c], op, acc[t]);      // the small parts first
+                }
+                if (!FINE && s != 3) continue;
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) y[t][v] = fmaf(scale, acc[t][v], y[t][v]);
+                if constexpr (FINE) __builtin_amdgcn_sched_barrier(0);
+            }
+            // (summed here: left to itself the compiler keeps every product's result until the sums are stored)
+#pragma unroll
+            for (int t = 0; t < T; ++t) asm volatile("" : "+v"(y[t]));
+            __builtin_amdgcn_sched_barrier(0);               // units one after the other: side by side they take too many registers
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // (before the next tile's codes)
+        if (more) put_scales(parity ^ 1);
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) sums[parity][wave][(t * 16 + 4 * q + v) * 16 + r] = y[t][v];
+        // (the other buffers are written next: who still reads them is past that at the next barrier)
+        __syncthreads();
+        int o = threadIdx.x;
+        asm volatile("" : "+v"(o));                       // (what follows from it is not kept through the products)
+        for (; o < mine * 16; o += kW4Block) {
+            float sum = 0.f;
+#pragma unroll
+            for (int v = 0; v < kW4Held; ++v) sum += sums[parity][v][o];
+            const int n = tile * 16 + o % 16;
+            if (n < p.N) w4_store<DT>(p, m0 + o / 16, n, sum);
+        }
+    };
+    int tile = first, parity = 0;
+    for (; tile + 1 < end; ++tile, parity ^= 1) step(tile, parity, true);
+    step(tile, parity, false);
 }
 
 // 16 weight rows and 16 tokens a workgroup; its waves share the columns in units of 128 and their
