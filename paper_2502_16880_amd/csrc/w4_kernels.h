@@ -7,16 +7,20 @@ namespace {
 typedef void (*w4_fn)(W4Params);
 }
 
-// k_w4_held for T tiles of 16 tokens and nb units a wave, null if there is none.
-__attribute__((visibility("hidden"))) const void* coral_w4_held_bf16(int kind, bool fine, int t, int nb);
-__attribute__((visibility("hidden"))) const void* coral_w4_held_f16(int kind, bool fine, int t, int nb);
-__attribute__((visibility("hidden"))) const void* coral_w4_held_f32(int kind, bool fine, int t, int nb);
+// k_w4_held for t tiles of 16 tokens and nb units a wave (in passes: the most there are).
+__attribute__((visibility("hidden"))) const void* coral_w4_held_bf16(int kind, bool fine, int t, int nb, bool passes);
+__attribute__((visibility("hidden"))) const void* coral_w4_held_f16(int kind, bool fine, int t, int nb, bool passes);
+__attribute__((visibility("hidden"))) const void* coral_w4_held_f32(int kind, bool fine, int t, int nb, bool passes);
 
 namespace {
 
 template <int DT, int KIND, bool FINE>
-w4_fn w4_pick_held(int t, int nb) {
+w4_fn w4_pick_held(int t, int nb, bool passes) {
     constexpr bool k16 = DT != kF32;             // fp32 activations take twice the registers
+    if (passes) {                                // as many units as the registers hold
+        constexpr int NB = k16 ? 8 : 4;
+        return t == 1 ? k_w4_held<DT, KIND, FINE, 1, NB, true> : t == 2 ? k_w4_held<DT, KIND, FINE, 2, NB / 2, true> : k_w4_held<DT, KIND, FINE, 4, NB / 4, true>;
+    }
     switch (t * 16 + nb) {
         case 17: return k_w4_held<DT, KIND, FINE, 1, 1>;
         case 18: return k_w4_held<DT, KIND, FINE, 1, 2>;
@@ -38,10 +42,10 @@ w4_fn w4_pick_held(int t, int nb) {
 }
 
 template <int DT>
-const void* w4_held(int kind, bool fine, int t, int nb) {
+const void* w4_held(int kind, bool fine, int t, int nb, bool passes) {
     w4_fn fn = nullptr;
-    if (fine) fn = kind == kW4E2M1 ? w4_pick_held<DT, kW4E2M1, true>(t, nb) : kind == kW4Sym ? w4_pick_held<DT, kW4Sym, true>(t, nb) : w4_pick_held<DT, kW4Zero, true>(t, nb);
-    else fn = kind == kW4E2M1 ? w4_pick_held<DT, kW4E2M1, false>(t, nb) : kind == kW4Sym ? w4_pick_held<DT, kW4Sym, false>(t, nb) : w4_pick_held<DT, kW4Zero, false>(t, nb);
+    if (fine) fn = kind == kW4E2M1 ? w4_pick_held<DT, kW4E2M1, true>(t, nb, passes) : kind == kW4Sym ? w4_pick_held<DT, kW4Sym, true>(t, nb, passes) : w4_pick_held<DT, kW4Zero, true>(t, nb, passes);
+    else fn = kind == kW4E2M1 ? w4_pick_held<DT, kW4E2M1, false>(t, nb, passes) : kind == kW4Sym ? w4_pick_held<DT, kW4Sym, false>(t, nb, passes) : w4_pick_held<DT, kW4Zero, false>(t, nb, passes);
     return reinterpret_cast<const void*>(fn);
 }
 

@@ -27,7 +27,6 @@ struct W4Params {
     unsigned per_group, per_group_inv;           // units of a group (at least one), 2^32 / that, rounded up
 };
 
-constexpr int kW4Waves = 4;
 constexpr int kW4UnitCols = 128;                 // columns of a unit: four products of 32
 
 template <int DT>
@@ -155,13 +154,14 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // The operands are read through buffer descriptors, which drop what lies behind their end: rows behind
 // the last one, and tokens and columns behind the activations, read as zero without a comparison.
 // Codes behind a row's last column are another row's and meet activations of zero.
+#define W4_INLINE __attribute__((always_inline))       // what works on registers that a lambda captures
 constexpr int kW4Block = 512;
 constexpr int kW4Held = kW4Block / kWave;
 
 typedef __amdgpu_buffer_rsrc_t w4_buffer;
-// The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed).
-__device__ __forceinline__ w4_buffer w4_view(const void* base, size_t first, size_t bytes) {
-    const size_t left = bytes - first;
+// The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed), or none.
+__device__ __forceinline__ w4_buffer w4_view(const void* base, size_t first, size_t bytes, bool any = true) {
+    const size_t left = any ? bytes - first : 0;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,
                                              left < 0xffffffffu ? (unsigned)left : 0xffffffffu, 0x00020000);
 }
@@ -172,6 +172,10 @@ __device__ __forceinline__ uint4 w4_read16(w4_buffer b, unsigned at, unsigned un
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 
+// The value is wanted in registers here: what makes it is neither moved behind this point nor, with a
+// value that a loop does not change, in front of the loop.
+__device__ __forceinline__ void w4_settle(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
+
 // Group of a unit where groups are whole units: unit / (group / 128) by the host's reciprocal.
 __device__ __forceinline__ unsigned w4_group_of(const W4Params& p, unsigned unit) {
     return p.per_group == 1 ? unit : __umulhi(unit, p.per_group_inv);
@@ -181,10 +185,14 @@ __device__ __forceinline__ unsigned w4_group_of(const W4Params& p, unsigned unit
 // (and room to split fp32 activations).
 constexpr int w4_held_regs(int dt, int t, int nb) { return dt == kF32 ? (t * nb > 1 ? 8 : 4) : t * nb; }
 
-// T tiles of 16 tokens (the next T of them: the next row of workgroups), NB units a wave.
-template <int DT, int KIND, bool FINE, int T, int NB>
+// T tiles of 16 tokens, NB units a wave.  PASSES: the columns are more than the waves hold and are taken
+// in passes; the workgroup goes through a block of tiles once a pass, adding the tiles' sums up in
+// LDS, before the next block.  Codes are still read once, activations once a block.
+template <int DT, int KIND, bool FINE, int T, int NB, bool PASSES = false>
 __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) void k_w4_held(W4Params p) {
-    constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>, XV = DT == kF32 ? 2 : 1;
+    // fp32 activations are held as their parts where the registers allow it, else split at every use
+    constexpr bool SPLIT = DT == kF32 && T * NB > 3;
+    constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>, XR = DT == kF32 ? 2 : 1, XV = SPLIT ? 2 : PARTS;
     constexpr bool PAIR = KIND == kW4Zero && DT != kF32;     // scale and zero as two 16-bit values of one word
     constexpr int PER = KIND == kW4Zero && DT == kF32 ? 2 : 1;
     // A slot is the columns that share a scale: a product's 32 where groups are finer than a unit, else
@@ -192,12 +200,20 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     constexpr int SLOTS = FINE ? 4 : 1, SL = (NB * kW4Held * SLOTS + 31) / 32, STRIDE = (SL * 32 + 1) * PER;
     __shared__ float sums[2][kW4Held][T * 256];
     __shared__ float scales[2][16][STRIDE];                  // (scale, 1 + zero / 16); rows start on different banks
-    __shared__ uint4 codes[kW4Held][16][NB * 4 + 1];         // a wave's own; rows start on different banks
+    // a wave's own: rows of codes that start on different banks, and before that the exchange of activations
+    constexpr int CHUNKS = NB * 4, CODE_ROW = CHUNKS + 1, X_ROW = 17;
+    constexpr int SLICE = 16 * CODE_ROW > 8 * X_ROW ? 16 * CODE_ROW : 8 * X_ROW;
+    __shared__ uint4 slices[kW4Held][SLICE];
     __shared__ f32x4_t x_sums[KIND != kW4E2M1 ? kW4Held : 1][NB][SLOTS][T][4];     // of a slot's x, 16 tokens
+    // sums of the passes so far, a block of tiles (as many as fit beside the rest)
+    constexpr int kUsed = sizeof(sums) + sizeof(scales) + sizeof(slices) + sizeof(x_sums);
+    constexpr int BLOCK = !PASSES ? 1 : (160 * 1024 - kUsed) / (T * 1024) < 24 ? (160 * 1024 - kUsed) / (T * 1024) : 24;
+    __shared__ float so_far[PASSES ? BLOCK : 1][PASSES ? T * 256 : 1];
+    constexpr int PASS_COLS = kW4Held * NB * kW4UnitCols;
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane & 15, q = lane >> 4;
-    const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, m0 = blockIdx.y * (T * 16), mine = p.M - m0 < T * 16 ? p.M - m0 : T * 16;
+    const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, passes = PASSES ? (p.K + PASS_COLS - 1) / PASS_COLS : 1;
     const int each = tiles / gridDim.x, more_of = tiles % gridDim.x, wg = blockIdx.x;
     const int first = wg * each + (wg < more_of ? wg : more_of), end = first + each + (wg < more_of ? 1 : 0);
 
@@ -205,24 +221,24 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     const int s_row = threadIdx.x / 32, s_slot = threadIdx.x % 32;
     unsigned s_raw[SL], z_raw[SL];
     const unsigned s_first = (unsigned)s_row * p.n_groups, s_last = s_first + (p.n_groups - 1);
-    auto s_at = [&](int i) {                                 // of the row's slots from the step's first one on
-        const unsigned slot = s_slot + 32 * i;
+    auto s_at = [&](int pass, int i) W4_INLINE {
+        const unsigned slot = pass * (kW4Held * NB * SLOTS) + s_slot + 32 * i;
         const unsigned at = s_first + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
         return at < s_last ? at : s_last;
     };
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
-    auto load_scales = [&](int tile) {
+    auto load_scales = [&](int tile, int pass, bool any) W4_INLINE {
         const size_t first_group = (size_t)tile * 16 * p.n_groups, all = (size_t)p.N * p.n_groups;
-        const w4_buffer view = w4_view(p.scales, first_group * W, all * W);
-        const w4_buffer z_view = w4_view(p.zeros, first_group, all);
+        const w4_buffer view = w4_view(p.scales, first_group * W, all * W, any);
+        const w4_buffer z_view = w4_view(p.zeros, first_group, all, any);
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
-            if constexpr (DT == kF32) s_raw[i] = __builtin_amdgcn_raw_buffer_load_b32(view, (int)(s_at(i) * W), 0, 0);
-            else s_raw[i] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(view, (int)(s_at(i) * W), 0, 0);
-            if constexpr (KIND == kW4Zero) z_raw[i] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(z_view, (int)s_at(i), 0, 0);
+            if constexpr (DT == kF32) s_raw[i] = __builtin_amdgcn_raw_buffer_load_b32(view, (int)(s_at(pass, i) * W), 0, 0);
+            else s_raw[i] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(view, (int)(s_at(pass, i) * W), 0, 0);
+            if constexpr (KIND == kW4Zero) z_raw[i] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(z_view, (int)s_at(pass, i), 0, 0);
         }
     };
-    auto put_scales = [&](int parity) {
+    auto put_scales = [&](int parity) W4_INLINE {
         float* dst = scales[parity][s_row] + s_slot * PER;
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
@@ -233,7 +249,6 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         }
     };
     // codes: the wave's 4 NB chunks of 16 rows, dealt to the lanes of its NB loads in the order of memory
-    constexpr int CHUNKS = NB * 4;
     constexpr bool EVEN = kWave % CHUNKS == 0;               // a load takes whole rows: the next one's are so many rows on
     uint4 w[NB];
     unsigned at[EVEN ? 1 : NB];
@@ -242,76 +257,145 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         const int e = j * kWave + lane;
         at[j] = (unsigned)(e / CHUNKS) * (unsigned)row_bytes + (unsigned)(wave * CHUNKS + e % CHUNKS) * 16u;
     }
-    auto read_codes = [&](const w4_buffer& view, int j) {
+    auto read_codes = [&](const w4_buffer& view, int j) W4_INLINE {
         if constexpr (EVEN) return w4_read16<kW4Stream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
         else return w4_read16<kW4Stream>(view, at[EVEN ? 0 : j]);
     };
-    auto code_view = [&](int tile) { return w4_view(p.codes, (size_t)tile * 16 * row_bytes, (size_t)p.N * row_bytes); };
-    auto put = [&](int j) {
-        const int e = j * kWave + lane;
-        store_vec(&codes[wave][e / CHUNKS][e % CHUNKS], w[j]);
+    auto code_view = [&](int tile, int pass, bool any) W4_INLINE {
+        return w4_view(p.codes, (size_t)tile * 16 * row_bytes + pass * (PASS_COLS / 2), (size_t)p.N * row_bytes, any);
     };
-    load_scales(first);
+    auto put = [&](int j) W4_INLINE {
+        const int e = j * kWave + lane;
+        store_vec(&slices[wave][e / CHUNKS * CODE_ROW + e % CHUNKS], w[j]);
+    };
     uint4 x[T][NB][4][XV];
     const w4_buffer x_view = w4_view(p.x, 0, (size_t)p.M * p.K * W);
+    // 16-bit activations: in the order of memory first, lane 16 a + c the eight columns c of a unit of
+    // token 4 i + a in register i (the products' own layout, 64 bytes of 16 tokens a load, made the first
+    // tile of 32 tokens wait for several us)
+    auto load_x = [&](int pass) W4_INLINE {
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+        for (int t = 0; t < T; ++t)
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int unit = pass * PASS_COLS + (wave * NB + j) * kW4UnitCols;
+                    const int col = unit + (DT != kF32 ? r * 8 : FINE ? s * 32 + q * 8 : q * 32 + s * 8);
+                    const int token = t * 16 + (DT != kF32 ? 4 * s + q : r);
+                    const unsigned off = col < p.K ? ((unsigned)token * (unsigned)p.K + col) * W : 0xffffffe0u;    // (behind the end)
+#pragma unroll
+                    for (int v = 0; v < XR; ++v) x[t][j][s][v] = w4_read16(x_view, off + 16u * v);
+                }
+    };
+    // ... then lane 16 q + r token r, chunk q and eight columns s in register s (fine groups: chunk s,
+    // eight columns q), through the wave's slice: as many tokens at a time as it holds
+    constexpr int HALVES = SLICE >= 16 * X_ROW ? 1 : 2, X_MASK = 16 / HALVES - 1;
+    auto exchange = [&](uint4 (&v)[4][XV]) W4_INLINE {
+        u32x4_t o[4] = {};
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
+#pragma unroll
+            for (int i = 0; i < 4 / HALVES; ++i) store_vec(&slices[wave][(4 * i + q) * X_ROW + r], v[4 / HALVES * h + i][0]);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                const int col = (wave * NB + j) * kW4UnitCols + (FINE ? s * 32 + q * 8 : q * 32 + s * 8);
-                const unsigned off = col < p.K ? ((unsigned)(m0 + t * 16 + r) * (unsigned)p.K + col) * W : 0xffffffe0u;      // (behind the end)
-#pragma unroll
-                for (int v = 0; v < XV; ++v) x[t][j][s][v] = w4_read16(x_view, off + 16u * v);
+                const uint4 got = load_vec(&slices[wave][(r & X_MASK) * X_ROW + (FINE ? 4 * s + q : 4 * q + s)]);
+                const bool take = h == 0 || r >= 8;
+                o[s].x = take ? got.x : o[s].x;
+                o[s].y = take ? got.y : o[s].y;
+                o[s].z = take ? got.z : o[s].z;
+                o[s].w = take ? got.w : o[s].w;
             }
-    {
-        const w4_buffer view = code_view(first);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        }
 #pragma unroll
-        for (int j = 0; j < NB; ++j) w[j] = read_codes(view, j);
-    }
-    put_scales(0);
-    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS]) {
+        for (int s = 0; s < 4; ++s) v[s][0] = make_uint4(o[s].x, o[s].y, o[s].z, o[s].w);
+    };
+    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS], bool split) W4_INLINE {
         if constexpr (DT == kF32) {
-            const uint4 a = v[0], b = v[XV - 1];
-            const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                                __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-            w4_split(f, part);
+            if (split) {
+                const uint4 a = v[0], b = v[1];
+                const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                                    __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+                w4_split(f, part);
 #pragma unroll
-            for (int c = 0; c < PARTS; ++c) part[c] = w4_order<KIND>(part[c]);
-        } else {
-            part[0] = v[0];
+                for (int c = 0; c < PARTS; ++c) part[c] = w4_order<KIND>(part[c]);
+                return;
+            }
+        }
+        if constexpr (!SPLIT) {
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) part[c] = v[c];
         }
     };
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     // the offset's part of the sums: of -24 x where every zero point is 8, else of -16 x, times 1 + zero / 16
     constexpr unsigned kMinus = KIND == kW4Sym ? (OP == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u) : OP == kF16 ? 0xCC00CC00u : 0xC180C180u;
     const uint4 minus = make_uint4(kMinus, kMinus, kMinus, kMinus);
+    auto arrange_x = [&]() W4_INLINE {
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
+        for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            f32x4_t sum = zero4;
+            for (int t = 0; t < T; ++t) {
+                if constexpr (DT != kF32) exchange(x[t][j]);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                if constexpr (DT != kF32) x[t][j][s][0] = w4_order<KIND>(x[t][j][s][0]);
-                if constexpr (KIND != kW4E2M1) {
-                    uint4 part[PARTS];
-                    parts_of(x[t][j][s], part);
-                    if (FINE) sum = zero4;
+                for (int s = 0; s < 4; ++s) {
+                    if constexpr (DT != kF32) x[t][j][s][0] = w4_order<KIND>(x[t][j][s][0]);
+                    if constexpr (DT == kF32 && !SPLIT) {
+                        uint4 part[PARTS];
+                        parts_of(x[t][j][s], part, true);
 #pragma unroll
-                    for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(part[c], minus, sum);
-                    if (r == 0 && (FINE || s == 3)) x_sums[wave][j][FINE ? s : 0][t][q] = sum;      // (read by this wave only)
+                        for (int c = 0; c < PARTS; ++c) x[t][j][s][c] = part[c];
+                    }
                 }
+                if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
             }
+        // (arranged here, not at every use)
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+#pragma unroll
+                    for (int v = 0; v < XV; ++v) w4_settle(x[t][j][s][v]);
+        if constexpr (KIND != kW4E2M1) {
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    f32x4_t sum = zero4;
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        uint4 part[PARTS];
+                        parts_of(x[t][j][s], part, SPLIT);
+                        if (FINE) sum = zero4;
+#pragma unroll
+                        for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(part[c], minus, sum);
+                        if (r == 0 && (FINE || s == 3)) x_sums[wave][j][FINE ? s : 0][t][q] = sum;      // (read by this wave only)
+                    }
+                    if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
+                }
         }
-    __syncthreads();                                         // scales and x_sums are there
-    auto step = [&](int tile, int parity, bool more) {
-        const int next = tile + 1;
-        if (more) load_scales(next);
-        const w4_buffer next_codes = code_view(more ? next : tile);
+    };
+    load_scales(first, 0, true);
+    if constexpr (!PASSES) load_x(0);
+    {
+        const w4_buffer view = code_view(first, 0, true);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) w[j] = read_codes(view, j);
+    }
+    put_scales(0);
+    if constexpr (!PASSES) arrange_x();
+    __syncthreads();                                         // the first tile's scales are there
+    // one tile of a pass, which requests the scales and codes of the next one; more: there is one (else the
+    // requests find nothing: a branch around them would wait for them where it ends)
+    auto step = [&](int tile, int pass, int in_block, int parity, bool more, int next_tile, int next_pass) W4_INLINE {
+        load_scales(next_tile, next_pass, more);
+        const w4_buffer next_codes = code_view(next_tile, next_pass, more);
         const float* my_scales = scales[parity][r] + wave * (NB * SLOTS * PER);
-        if constexpr (DT == kF32) {                          // (or the parts of all activations are kept in registers)
+        if constexpr (SPLIT) {                               // (or the parts of all activations are kept in registers)
 #pragma unroll
             for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -319,7 +403,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                     for (int s = 0; s < 4; ++s)
 #pragma unroll
-                        for (int v = 0; v < XV; ++v) asm volatile("" : "+v"(x[t][j][s][v].x), "+v"(x[t][j][s][v].y), "+v"(x[t][j][s][v].z), "+v"(x[t][j][s][v].w));
+                        for (int v = 0; v < XV; ++v) w4_settle(x[t][j][s][v]);
         }
         f32x4_t y[T];
 #pragma unroll
@@ -327,7 +411,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
             put(j);
-            if (more) w[j] = read_codes(next_codes, j);      // the registers are free again
+            w[j] = read_codes(next_codes, j);                // the registers are free again
         }
         // A wave's LDS accesses complete in order; the compiler has to keep the order too, though no
         // lane reads what it wrote itself.
@@ -336,10 +420,10 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         for (int j = 0; j < NB; ++j) {
             uint4 v;
             if constexpr (FINE) {                            // dword q of the four chunks: their transposition
-                const unsigned* d = reinterpret_cast<const unsigned*>(&codes[wave][r][j * 4]) + q;
+                const unsigned* d = reinterpret_cast<const unsigned*>(&slices[wave][r * CODE_ROW + j * 4]) + q;
                 v = make_uint4(d[0], d[4], d[8], d[12]);
             } else {
-                v = load_vec(&codes[wave][r][j * 4 + q]);
+                v = load_vec(&slices[wave][r * CODE_ROW + j * 4 + q]);
             }
             f32x4_t acc[T];
             float scale = 0.f;
@@ -369,7 +453,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
                     uint4 part[PARTS];
-                    parts_of(x[t][j][s], part);
+                    parts_of(x[t][j][s], part, SPLIT);
 #pragma unroll
                     for (int c = PARTS - 1; c >= 0; --c) acc[t] = mfma_tile<OP>(part[c], op, acc[t]);      // the small parts first
                 }
@@ -386,7 +470,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
             __builtin_amdgcn_sched_barrier(0);               // units one after the other: side by side they take too many registers
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // (before the next tile's codes)
-        if (more) put_scales(parity ^ 1);
+        put_scales(parity ^ 1);
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -395,90 +479,38 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         __syncthreads();
         int o = threadIdx.x;
         asm volatile("" : "+v"(o));                       // (what follows from it is not kept through the products)
-        for (; o < mine * 16; o += kW4Block) {
+        for (; o < p.M * 16; o += kW4Block) {
             float sum = 0.f;
 #pragma unroll
             for (int v = 0; v < kW4Held; ++v) sum += sums[parity][v][o];
+            if constexpr (PASSES) {                          // (a place of so_far is one thread's own)
+                if (pass > 0) sum += so_far[in_block][o];
+                if (pass + 1 < passes) {
+                    so_far[in_block][o] = sum;
+                    continue;
+                }
+            }
             const int n = tile * 16 + o % 16;
-            if (n < p.N) w4_store<DT>(p, m0 + o / 16, n, sum);
+            if (n < p.N) w4_store<DT>(p, o / 16, n, sum);
         }
     };
-    int tile = first, parity = 0;
-    for (; tile + 1 < end; ++tile, parity ^= 1) step(tile, parity, true);
-    step(tile, parity, false);
-}
-
-// 16 weight rows and 16 tokens a workgroup; its waves share the columns in units of 128 and their
-// sums meet in LDS.
-template <int DT, int KIND>
-__global__ __launch_bounds__(kW4Waves * kWave) void k_w4(W4Params p) {
-    constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>;
-    __shared__ float sums[kW4Waves][256];
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int r = lane & 15, q = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16;
-    const int n = n0 + r < p.N ? n0 + r : p.N - 1;           // what is read twice is not stored
-    const int m = m0 + r < p.M ? m0 + r : p.M - 1;
-    const unsigned char* codes = p.codes + (size_t)n * (p.K / 2);
-    const size_t scales = (size_t)n * p.n_groups;
-    const uint4* x = static_cast<const uint4*>(p.x) + (size_t)m * p.K / (DT == kF32 ? 4 : 8);
-    uint4 minus;                                             // sums of (16 + zero) x: the zero comes later
-    minus.x = minus.y = minus.z = minus.w = OP == kF16 ? 0xCC00CC00u : 0xC180C180u;        // -16.0
-    if (KIND == kW4Sym) minus.x = minus.y = minus.z = minus.w = OP == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u;   // -24.0
-    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = wave * kW4UnitCols; c0 < p.K; c0 += kW4Waves * kW4UnitCols) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            const int col = c0 + s * 32 + q * 8;
-            if (c0 + s * 32 >= p.K) break;                   // wave-uniform
-            const bool in = col < p.K;                       // (K is a multiple of 8)
-            unsigned w = 0u;
-            uint4 part[PARTS];
-            if constexpr (DT == kF32) {
-                float f[8];
-                uint4 a = make_uint4(0, 0, 0, 0), b = a;
-                if (in) {
-                    a = load_vec(x + col / 4);
-                    b = load_vec(x + col / 4 + 1);
+    int parity = 0;
+    if constexpr (!PASSES) {
+        for (int tile = first; tile < end; ++tile, parity ^= 1) step(tile, 0, 0, parity, tile + 1 < end, tile + 1, 0);
+    } else {
+        for (int from = first; from < end; from += BLOCK) {
+            const int to = from + BLOCK < end ? from + BLOCK : end;
+            for (int pass = 0; pass < passes; ++pass) {
+                load_x(pass);
+                arrange_x();
+                for (int tile = from; tile < to; ++tile, parity ^= 1) {
+                    const bool last = tile + 1 == to, last_pass = last && pass + 1 == passes;
+                    const int next_tile = !last ? tile + 1 : !last_pass ? from : to, next_pass = !last ? pass : !last_pass ? pass + 1 : 0;
+                    step(tile, pass, tile - from, parity, next_tile < end, next_tile, next_pass);
                 }
-                f[0] = __uint_as_float(a.x); f[1] = __uint_as_float(a.y);
-                f[2] = __uint_as_float(a.z); f[3] = __uint_as_float(a.w);
-                f[4] = __uint_as_float(b.x); f[5] = __uint_as_float(b.y);
-                f[6] = __uint_as_float(b.z); f[7] = __uint_as_float(b.w);
-                w4_split(f, part);
-            } else {
-                part[0] = in ? load_vec(x + col / 8) : make_uint4(0, 0, 0, 0);
             }
-            if (in) w = *reinterpret_cast<const unsigned*>(codes + col / 2);
-            const uint4 op = w4_operand<OP, KIND>(w);
-            const int g = (c0 + s * 32) / p.group;
-            const float scale = w4_load<DT>(p.scales, scales + g);
-            f32x4_t acc = {0.f, 0.f, 0.f, 0.f}, ones = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = PARTS - 1; c >= 0; --c) {           // the small parts first
-                const uint4 a = w4_order<KIND>(part[c]);
-                if constexpr (KIND == kW4Sym) acc = mfma_tile<OP>(a, minus, acc);
-                if constexpr (KIND == kW4Zero) ones = mfma_tile<OP>(a, minus, ones);
-                acc = mfma_tile<OP>(a, op, acc);
-            }
-            if constexpr (KIND == kW4Zero) {
-                const float zero = 1.0f + (float)p.zeros[scales + g] * 0.0625f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[i] = fmaf(zero, ones[i], acc[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = fmaf(scale, acc[i], y[i]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sums[wave][(4 * q + i) * 16 + r] = y[i];
-    __syncthreads();
-    const int at = threadIdx.x;                              // token at / 16, weight row at % 16
-    float sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < kW4Waves; ++w) sum += sums[w][at];
-    if (m0 + at / 16 < p.M && n0 + at % 16 < p.N) w4_store<DT>(p, m0 + at / 16, n0 + at % 16, sum);
 }
 
 }  // namespace

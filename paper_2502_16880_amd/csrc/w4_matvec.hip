@@ -8,25 +8,20 @@
 
 namespace {
 
-template <int DT>
-w4_fn pick_kind(int kind) {
-    return kind == kW4Sym ? k_w4<DT, kW4Sym> : kind == kW4Zero ? k_w4<DT, kW4Zero> : k_w4<DT, kW4E2M1>;
-}
-
 struct W4Plan {
-    int t, nb;                  // k_w4_held's parameters; nb = 0: k_w4
+    int t, nb;                  // k_w4_held's parameters
+    bool passes;
 };
 
-// The columns that eight waves' registers hold for 16, 32 or 64 tokens; fewer tokens a workgroup, and the
-// weights read once for each, where all of them do not fit.
+// Registers hold eight units of 128 columns a wave for 16 tokens, four for 32, two for 64; half as many
+// of fp32 activations.  More columns are taken in passes.
 W4Plan plan_held(const W4Params& p, coral_dtype dt) {
-    const int wide = dt == CORAL_F32 ? 2 : 1, units = (p.K + kW4UnitCols - 1) / kW4UnitCols;
-    int t = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4, nb = (units + kW4Held - 1) / kW4Held;
-    nb = nb <= 4 ? nb : nb <= 6 ? 6 : 8;
-    if (units > 8 * kW4Held) return {1, 0};
-    while (t > 1 && (nb == 3 ? 4 : nb) * t * wide > 8) t /= 2;
-    if (t > 1 && nb == 3) nb = 4;
-    return nb * t * wide > 8 ? W4Plan{1, 0} : W4Plan{t, nb};
+    const int units = (p.K + kW4UnitCols - 1) / kW4UnitCols;
+    const int t = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4, most = (dt == CORAL_F32 ? 4 : 8) / t;
+    int nb = (units + kW4Held - 1) / kW4Held;
+    if (nb > most) return {t, most, true};
+    nb = nb == 5 ? 6 : nb == 7 ? 8 : t > 1 && nb == 3 ? 4 : nb;
+    return {t, nb, false};
 }
 
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
@@ -77,19 +72,13 @@ extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const 
     const int kind = code == CORAL_W4_E2M1 ? kW4E2M1 : zeros ? kW4Zero : kW4Sym;
     const W4Plan plan = plan_held(p, dt);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (plan.nb > 0) {
-        const bool fine = group < kW4UnitCols;
-        const void* held = dt == CORAL_F32    ? coral_w4_held_f32(kind, fine, plan.t, plan.nb)
-                           : dt == CORAL_BF16 ? coral_w4_held_bf16(kind, fine, plan.t, plan.nb)
-                                              : coral_w4_held_f16(kind, fine, plan.t, plan.nb);
-        // as many workgroups as stay resident: their registers allow four, two or one a compute unit
-        const int held_regs = w4_held_regs(dt == CORAL_F32 ? kF32 : kBF16, plan.t, plan.nb);
-        const int tiles = (N - 1) / 16 + 1, most = 256 * (held_regs <= 2 ? 4 : held_regs <= 4 ? 2 : 1);
-        hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(held)), dim3(tiles < most ? tiles : most, (M - 1) / (plan.t * 16) + 1),
-                           dim3(kW4Block), 0, stream, p);
-        return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
-    }
-    const w4_fn fn = dt == CORAL_F32 ? pick_kind<kF32>(kind) : dt == CORAL_BF16 ? pick_kind<kBF16>(kind) : pick_kind<kF16>(kind);
-    hipLaunchKernelGGL(fn, dim3((N - 1) / 16 + 1, (M + 15) / 16), dim3(kW4Waves * kWave), 0, stream, p);
+    const bool fine = group < kW4UnitCols;
+    const void* held = dt == CORAL_F32    ? coral_w4_held_f32(kind, fine, plan.t, plan.nb, plan.passes)
+                       : dt == CORAL_BF16 ? coral_w4_held_bf16(kind, fine, plan.t, plan.nb, plan.passes)
+                                          : coral_w4_held_f16(kind, fine, plan.t, plan.nb, plan.passes);
+    // as many workgroups as stay resident: their registers allow four, two or one a compute unit
+    const int regs = w4_held_regs(dt == CORAL_F32 ? kF32 : kBF16, plan.t, plan.nb);
+    const int tiles = (N - 1) / 16 + 1, most = 256 * (regs <= 2 ? 4 : regs <= 4 ? 2 : 1);
+    hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(held)), dim3(tiles < most ? tiles : most), dim3(kW4Block), 0, stream, p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }
