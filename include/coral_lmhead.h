@@ -390,7 +390,7 @@ typedef struct {
     const float *bias_values;
     const int32_t *bias_ranges;
     const uint32_t *mask;
-    int32_t n_history;                  /* at most 2^30, as n_biases */
+    int32_t n_history;                  /* at most 2^29, as n_biases */
     int32_t n_biases;
 } coral_logit_rules;
 

@@ -478,31 +478,40 @@ def coral_lmhead_dense(hidden: torch.Tensor, lm_W: torch.Tensor, k: int,
 
 # ---------------------------------------------------------------- 4-bit products, rules on logits
 def _same_device_ptr(t: Optional[torch.Tensor], name: str, device, dtype, shape) -> Optional[int]:
-    """Pointer of a contiguous tensor of this type, shape (-1: any) and device; None stays None."""
+    """Pointer of a contiguous tensor of this type, device and shape (None: any 1-D one); None stays None."""
     if t is None:
         return None
+    if t.dtype == dtype and t.device == device and (t.shape == shape if shape is not None else t.dim() == 1) \
+            and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must live on {device}, got {t.device}")
-    if len(shape) != t.dim() or any(n != have and n != -1 for n, have in zip(shape, t.shape)):
-        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous (row-major, no padding)")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be {'1-D' if shape is None else list(shape)}, got {list(t.shape)}")
+
+
+# The device's current stream as a raw handle: without the object that torch.cuda.current_stream makes
+# (1.8 of the 11 us that a call cost the host) where this PyTorch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _enqueue(fn, device, stream, *args) -> None:
     """Calls the library on the tensors' device and the given stream (None: the device's current one)."""
     if stream is None:
-        stream = torch.cuda.current_stream(device)
+        handle = _raw_stream(device.index)
     elif stream.device != device:
         raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
+    else:
+        handle = stream.cuda_stream
     if device.index == torch.cuda.current_device():
-        st = fn(*args, stream.cuda_stream)
+        st = fn(*args, handle)
     else:
         with torch.cuda.device(device):
-            st = fn(*args, stream.cuda_stream)
+            st = fn(*args, handle)
     if st:
         _raise(st)
 
@@ -585,13 +594,13 @@ def _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias
         i32, f32 = torch.int32, torch.float32
         n_history = 0 if history is None else history.numel()
         n_biases = 0 if bias_ids is None else bias_ids.numel()
-        if max(n_history, n_biases) > 1 << 30:
-            raise ValueError("at most 2^30 tokens of history, and biases")
+        if max(n_history, n_biases) > 1 << 29:
+            raise ValueError("at most 2^29 tokens of history, and biases")
         rules = ctypes.byref(_LogitRulesStruct(
-            _same_device_ptr(history, "history", dev, i32, (-1,)),
+            _same_device_ptr(history, "history", dev, i32, None),
             _same_device_ptr(ranges, "ranges", dev, i32, (M, 4)),
             _same_device_ptr(penalties, "penalties", dev, f32, (M, 3)),
-            _same_device_ptr(bias_ids, "bias_ids", dev, i32, (-1,)),
+            _same_device_ptr(bias_ids, "bias_ids", dev, i32, None),
             _same_device_ptr(bias_values, "bias_values", dev, f32, (n_biases,)),
             _same_device_ptr(bias_ranges, "bias_ranges", dev, i32, (M, 2)),
             _same_device_ptr(mask, "mask", dev, i32, (M, -(-V // 32))), n_history, n_biases))
@@ -641,7 +650,7 @@ def coral_logits_topk(logits: torch.Tensor, k: int, history: Optional[torch.Tens
     if workspace is None:
         workspace = _new((max(coral_logits_topk_workspace_bytes(M, V, k), 1 << 15),), torch.uint8, dev, stream)
         _enqueue(_L.coral_lmhead_workspace_init, dev, stream, workspace.data_ptr(), workspace.numel())
-    ws = _same_device_ptr(workspace, "workspace", dev, torch.uint8, (-1,))
+    ws = _same_device_ptr(workspace, "workspace", dev, torch.uint8, None)
     _enqueue(_L.coral_logits_topk, dev, stream, ptr, rules, M, V, k, dt,
              _same_device_ptr(topk_ids, "topk_ids", dev, torch.int32, (M, k)),
              _same_device_ptr(topk_logprob, "topk_logprob", dev, torch.float32, (M, k)), ws, workspace.numel())

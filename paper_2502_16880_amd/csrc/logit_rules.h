@@ -11,7 +11,7 @@
 // biases' places are marked the same way.  So neither a count array in memory nor a second pass over
 // the logits is needed, and rows of any number share their prompts by reading the same range.
 #pragma once
-#include "device_utils.h"
+#include "buffer_loads.h"
 #include "wave_topk.h"
 
 namespace {
@@ -33,6 +33,7 @@ constexpr int kRuleWaves = 4;
 constexpr int kRuleThreads = kRuleWaves * kWave;
 constexpr int kRulePerLane = 16;                            // values a lane holds of a batch
 constexpr int kRuleBatch = kRulePerLane * kWave;            // 1024
+constexpr int kRuleAhead = 4;                               // loads of four tokens that a thread has on their way
 constexpr unsigned kInPrompt = 0x80000000u;                 // the rest of a word counts the output
 
 template <int DT>
@@ -52,39 +53,57 @@ __device__ __forceinline__ int vec_place(int first, int wave, int lane, int u) {
     return first + ((wave * NB + u / U) * U + u % U) * (kWave * E) + lane * E;
 }
 
-// The lane's logits of the slice (-inf where there is none).
+// The lane's logits of the slice, as they lie in memory, and the mask bits that go with them (the words
+// of a vector's first and last value; values of the row's neighbours among them are dropped later).
 template <int DT, int NB>
-__device__ __forceinline__ void load_slice(const RuleParams& p, int m, int lead, int first, int wave, int lane,
-                                           float (&z)[NB * kRulePerLane]) {
-    constexpr int E = kRuleVec<DT>, VECS = NB * kRulePerLane / E;
-    const size_t row = (size_t)m * p.V;
+struct SliceData {
+    static constexpr int kVecs = NB * kRulePerLane / kRuleVec<DT>;
+    uint4 v[kVecs];
+    unsigned lo[kVecs], hi[kVecs];
+};
+template <int DT, int NB>
+__device__ __forceinline__ void load_slice(const RuleParams& p, int m, int lead, int first, int wave, int lane, SliceData<DT, NB>& d) {
+    constexpr size_t W = DT == kF32 ? 4 : 2;
+    const Buffer logits = buffer_view(p.logits, ((size_t)m * p.V - lead) * W, (size_t)p.M * p.V * W);
 #pragma unroll
-    for (int u = 0; u < VECS; ++u) {
-        const int id = vec_place<DT, NB>(first, wave, lane, u) - lead;
-        if (id >= 0 && id + E <= p.V) {
-            if constexpr (DT == kF32) {
-                const uint4 v = load_vec(reinterpret_cast<const uint4*>(static_cast<const float*>(p.logits) + row + id));
-                z[u * 4] = __uint_as_float(v.x);
-                z[u * 4 + 1] = __uint_as_float(v.y);
-                z[u * 4 + 2] = __uint_as_float(v.z);
-                z[u * 4 + 3] = __uint_as_float(v.w);
-            } else {
-                const uint4 v = load_vec(reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.logits) + row + id));
-                const unsigned w[4] = {v.x, v.y, v.z, v.w};
+    for (int u = 0; u < d.kVecs; ++u) d.v[u] = buffer_read16<kBufferStream>(logits, (unsigned)(vec_place<DT, NB>(first, wave, lane, u) * W));
+    if (p.mask) {                                            // uniform
+        const Buffer mask = buffer_view(p.mask, (size_t)m * p.mask_words * 4, (size_t)p.M * p.mask_words * 4);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) z[u * 8 + e] = widen16<DT>((unsigned short)(w[e / 2] >> (e % 2 * 16)));
-            }
-        } else {
+        for (int u = 0; u < d.kVecs; ++u) {
+            const int id = vec_place<DT, NB>(first, wave, lane, u) - lead;       // (before the row: dropped, as behind the end)
+            d.lo[u] = buffer_read4(mask, (unsigned)(id >> 5) * 4u);
+            d.hi[u] = buffer_read4(mask, (unsigned)((id + kRuleVec<DT> - 1) >> 5) * 4u);
+        }
+    }
+}
+
+// The values as fp32; -inf for those that are not the row's.
+template <int DT, int NB>
+__device__ __forceinline__ void slice_values(const RuleParams& p, int m, int lead, int first, int wave, int lane, const SliceData<DT, NB>& d,
+                                             float (&z)[NB * kRulePerLane]) {
+    constexpr int E = kRuleVec<DT>, SLICE = NB * kRuleBatch * kRuleWaves;
+#pragma unroll
+    for (int u = 0; u < d.kVecs; ++u) {
+        const unsigned w[4] = {d.v[u].x, d.v[u].y, d.v[u].z, d.v[u].w};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            if constexpr (DT == kF32) z[u * E + e] = __uint_as_float(w[e]);
+            else z[u * E + e] = widen16<DT>((unsigned short)(w[e / 2] >> (e % 2 * 16)));
+        }
+    }
+    if (first < lead || first + SLICE > p.V + lead) {        // uniform: the row's first or last slice
+        // (half a dword at the very end of the operand is dropped by the load of a vector)
+        float end = 0.f;
+        if constexpr (DT != kF32) end = widen16<DT>(static_cast<const unsigned short*>(p.logits)[(size_t)p.M * p.V - 1]);
+#pragma unroll
+        for (int u = 0; u < d.kVecs; ++u)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                float v = -INFINITY;
-                if (id + e >= 0 && id + e < p.V) {
-                    if constexpr (DT == kF32) v = static_cast<const float*>(p.logits)[row + id + e];
-                    else v = widen16<DT>(static_cast<const unsigned short*>(p.logits)[row + id + e]);
-                }
-                z[u * E + e] = v;
+                const int id = vec_place<DT, NB>(first, wave, lane, u) - lead + e;
+                if (DT != kF32 && id == p.V - 1 && m == p.M - 1) z[u * E + e] = end;
+                z[u * E + e] = id >= 0 && id < p.V ? z[u * E + e] : -INFINITY;
             }
-        }
     }
 }
 
@@ -113,7 +132,7 @@ __device__ __forceinline__ float rule_penalty(float z, unsigned seen, float rep,
 // of the workgroup comes here; barriers are reached by all.
 template <int DT, int NB>
 __device__ __forceinline__ void apply_rules(const RuleParams& p, int m, int lead, int first, int wave, int lane,
-                                            unsigned* words, float (&z)[NB * kRulePerLane]) {
+                                            unsigned* words, const SliceData<DT, NB>& d, float (&z)[NB * kRulePerLane]) {
     constexpr int E = kRuleVec<DT>, VECS = NB * kRulePerLane / E, SLICE = NB * kRuleBatch * kRuleWaves;
     auto clear = [&]() {
         for (int i = threadIdx.x; i < SLICE; i += kRuleThreads) words[i] = 0u;
@@ -122,20 +141,34 @@ __device__ __forceinline__ void apply_rules(const RuleParams& p, int m, int lead
     if (p.ranges) {                                          // uniform
         clear();
         const int32_t* r = p.ranges + (size_t)m * 4;
+        const float rep = p.penalties[m * 3], freq = p.penalties[m * 3 + 1], pres = p.penalties[m * 3 + 2];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
+            // the tokens four at a time, several loads on their way; behind the range: token -1
             const Span s = clamp_span(r[2 * which], r[2 * which + 1], p.n_history);
-            for (int i = s.begin + (int)threadIdx.x; i < s.end; i += kRuleThreads) {
-                const int id = p.history[i];
-                const unsigned at = (unsigned)id + (unsigned)(lead - first);
-                if (id >= 0 && id < p.V && at < (unsigned)SLICE) {
-                    if (which == 0) atomicOr(words + at, kInPrompt);
-                    else atomicAdd(words + at, 1u);
+            const Buffer tokens = buffer_view(p.history, (size_t)s.begin * 4, (size_t)s.end * 4);
+            const int n = s.end - s.begin;
+            for (int i = 0; i < n; i += kRuleThreads * 4 * kRuleAhead) {         // uniform
+                uint4 t[kRuleAhead];
+#pragma unroll
+                for (int a = 0; a < kRuleAhead; ++a) t[a] = buffer_read16(tokens, (unsigned)(i + (a * kRuleThreads + (int)threadIdx.x) * 4) * 4u);
+#pragma unroll
+                for (int a = 0; a < kRuleAhead; ++a) {
+                    const unsigned id[4] = {t[a].x, t[a].y, t[a].z, t[a].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned at = id[e] + (unsigned)(lead - first);
+                        const bool in = i + (a * kRuleThreads + (int)threadIdx.x) * 4 + e < n;
+                        if (in && at < (unsigned)SLICE && id[e] < (unsigned)p.V) {
+                            if (which == 0) atomicOr(words + at, kInPrompt);
+                            else atomicAdd(words + at, 1u);
+                        }
+                    }
                 }
             }
         }
         __syncthreads();
-        const float rep = p.penalties[m * 3], freq = p.penalties[m * 3 + 1], pres = p.penalties[m * 3 + 2];
+        slice_values<DT, NB>(p, m, lead, first, wave, lane, d, z);
 #pragma unroll
         for (int u = 0; u < VECS; ++u) {
             const int at = vec_place<DT, NB>(0, wave, lane, u);
@@ -143,6 +176,8 @@ __device__ __forceinline__ void apply_rules(const RuleParams& p, int m, int lead
             for (int e = 0; e < E; ++e) z[u * E + e] = rule_penalty(z[u * E + e], words[at + e], rep, freq, pres);
         }
         __syncthreads();
+    } else {
+        slice_values<DT, NB>(p, m, lead, first, wave, lane, d, z);
     }
     if (p.bias_ranges) {                                     // uniform
         clear();
@@ -164,16 +199,12 @@ __device__ __forceinline__ void apply_rules(const RuleParams& p, int m, int lead
         }
     }
     if (p.mask) {                                            // uniform
-        const unsigned* mask = p.mask + (size_t)m * p.mask_words;
 #pragma unroll
         for (int u = 0; u < VECS; ++u) {
             const int id = vec_place<DT, NB>(first, wave, lane, u) - lead;
+            const unsigned bits = __builtin_amdgcn_alignbit(d.hi[u], d.lo[u], (unsigned)(id & 31));
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int i = id + e;
-                const bool in = i >= 0 && i < p.V;
-                if (!in || !(mask[i >> 5] >> (i & 31) & 1u)) z[u * E + e] = -INFINITY;
-            }
+            for (int e = 0; e < E; ++e) z[u * E + e] = bits >> e & 1u ? z[u * E + e] : -INFINITY;
         }
     }
 }
@@ -186,9 +217,10 @@ __global__ __launch_bounds__(kRuleThreads) void k_logits_adjust(RuleParams p, vo
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int m = blockIdx.y, lead = row_lead<DT>(m, p.V), first = blockIdx.x * SLICE;
+    SliceData<DT, NB> d;
+    load_slice<DT, NB>(p, m, lead, first, wave, lane, d);
     float z[NB * kRulePerLane];
-    load_slice<DT, NB>(p, m, lead, first, wave, lane, z);
-    apply_rules<DT, NB>(p, m, lead, first, wave, lane, words, z);
+    apply_rules<DT, NB>(p, m, lead, first, wave, lane, words, d, z);
     const size_t row = (size_t)m * p.V;
 #pragma unroll
     for (int u = 0; u < VECS; ++u) {
@@ -258,9 +290,10 @@ __global__ __launch_bounds__(kRuleThreads) void k_logits_topk(RuleParams p, Topk
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int m = blockIdx.y, lead = row_lead<DT>(m, p.V), slice = blockIdx.x, first = slice * SLICE, k = t.k;
+    SliceData<DT, NB> d;
+    load_slice<DT, NB>(p, m, lead, first, wave, lane, d);
     float z[NB * kRulePerLane];
-    load_slice<DT, NB>(p, m, lead, first, wave, lane, z);
-    apply_rules<DT, NB>(p, m, lead, first, wave, lane, lds.words, z);
+    apply_rules<DT, NB>(p, m, lead, first, wave, lane, lds.words, d, z);
     __syncthreads();                                         // the words' memory is taken again below
     float top = -INFINITY;
 #pragma unroll

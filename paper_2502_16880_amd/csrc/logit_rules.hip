@@ -13,7 +13,7 @@ namespace {
 
 constexpr size_t kLists = coral_ctrl::kPreparedWords * sizeof(unsigned);     // published lists start behind the control words
 constexpr int kMaxSlices = 256;                                              // lists that one merge takes
-constexpr int kMaxList = 1 << 30;                                            // entries of the flat lists
+constexpr int kMaxList = 1 << 29;                                            // entries of the flat lists
 
 size_t align_256(size_t x) { return (x + 255) / 256 * 256; }
 

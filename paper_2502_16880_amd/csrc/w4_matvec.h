@@ -9,7 +9,7 @@
 // fp32 sum, never a 16-bit weight.  fp32 activations are split into three bf16 values whose sum they
 // are, and every product is taken three times: the sums are fp32 sums of exact products in all types.
 #pragma once
-#include "device_utils.h"
+#include "buffer_loads.h"
 
 namespace {
 
@@ -158,20 +158,6 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 constexpr int kW4Block = 512;
 constexpr int kW4Held = kW4Block / kWave;
 
-typedef __amdgpu_buffer_rsrc_t w4_buffer;
-// The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed), or none.
-__device__ __forceinline__ w4_buffer w4_view(const void* base, size_t first, size_t bytes, bool any = true) {
-    const size_t left = any ? bytes - first : 0;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,
-                                             left < 0xffffffffu ? (unsigned)left : 0xffffffffu, 0x00020000);
-}
-constexpr int kW4Stream = 2;                     // non-temporal: what is read once
-template <int AUX = 0>
-__device__ __forceinline__ uint4 w4_read16(w4_buffer b, unsigned at, unsigned uniform_at = 0) {
-    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, (int)uniform_at, AUX);
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
-
 // The value is wanted in registers here: what makes it is neither moved behind this point nor, with a
 // value that a loop does not change, in front of the loop.
 __device__ __forceinline__ void w4_settle(uint4& v) { asm volatile("" : "+v"(v.x), "+v"(v.y), "+v"(v.z), "+v"(v.w)); }
@@ -229,13 +215,13 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
     auto load_scales = [&](int tile, int pass, bool any) W4_INLINE {
         const size_t first_group = (size_t)tile * 16 * p.n_groups, all = (size_t)p.N * p.n_groups;
-        const w4_buffer view = w4_view(p.scales, first_group * W, all * W, any);
-        const w4_buffer z_view = w4_view(p.zeros, first_group, all, any);
+        const Buffer view = buffer_view(p.scales, first_group * W, all * W, any);
+        const Buffer z_view = buffer_view(p.zeros, first_group, all, any);
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
-            if constexpr (DT == kF32) s_raw[i] = __builtin_amdgcn_raw_buffer_load_b32(view, (int)(s_at(pass, i) * W), 0, 0);
-            else s_raw[i] = (unsigned short)__builtin_amdgcn_raw_buffer_load_b16(view, (int)(s_at(pass, i) * W), 0, 0);
-            if constexpr (KIND == kW4Zero) z_raw[i] = (unsigned char)__builtin_amdgcn_raw_buffer_load_b8(z_view, (int)s_at(pass, i), 0, 0);
+            if constexpr (DT == kF32) s_raw[i] = buffer_read4(view, s_at(pass, i) * W);
+            else s_raw[i] = buffer_read2(view, s_at(pass, i) * W);
+            if constexpr (KIND == kW4Zero) z_raw[i] = buffer_read1(z_view, s_at(pass, i));
         }
     };
     auto put_scales = [&](int parity) W4_INLINE {
@@ -257,19 +243,19 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         const int e = j * kWave + lane;
         at[j] = (unsigned)(e / CHUNKS) * (unsigned)row_bytes + (unsigned)(wave * CHUNKS + e % CHUNKS) * 16u;
     }
-    auto read_codes = [&](const w4_buffer& view, int j) W4_INLINE {
-        if constexpr (EVEN) return w4_read16<kW4Stream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
-        else return w4_read16<kW4Stream>(view, at[EVEN ? 0 : j]);
+    auto read_codes = [&](const Buffer& view, int j) W4_INLINE {
+        if constexpr (EVEN) return buffer_read16<kBufferStream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
+        else return buffer_read16<kBufferStream>(view, at[EVEN ? 0 : j]);
     };
     auto code_view = [&](int tile, int pass, bool any) W4_INLINE {
-        return w4_view(p.codes, (size_t)tile * 16 * row_bytes + pass * (PASS_COLS / 2), (size_t)p.N * row_bytes, any);
+        return buffer_view(p.codes, (size_t)tile * 16 * row_bytes + pass * (PASS_COLS / 2), (size_t)p.N * row_bytes, any);
     };
     auto put = [&](int j) W4_INLINE {
         const int e = j * kWave + lane;
         store_vec(&slices[wave][e / CHUNKS * CODE_ROW + e % CHUNKS], w[j]);
     };
     uint4 x[T][NB][4][XV];
-    const w4_buffer x_view = w4_view(p.x, 0, (size_t)p.M * p.K * W);
+    const Buffer x_view = buffer_view(p.x, 0, (size_t)p.M * p.K * W);
     // 16-bit activations: in the order of memory first, lane 16 a + c the eight columns c of a unit of
     // token 4 i + a in register i (the products' own layout, 64 bytes of 16 tokens a load, made the first
     // tile of 32 tokens wait for several us)
@@ -285,7 +271,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                     const int token = t * 16 + (DT != kF32 ? 4 * s + q : r);
                     const unsigned off = col < p.K ? ((unsigned)token * (unsigned)p.K + col) * W : 0xffffffe0u;    // (behind the end)
 #pragma unroll
-                    for (int v = 0; v < XR; ++v) x[t][j][s][v] = w4_read16(x_view, off + 16u * v);
+                    for (int v = 0; v < XR; ++v) x[t][j][s][v] = buffer_read16(x_view, off + 16u * v);
                 }
     };
     // ... then lane 16 q + r token r, chunk q and eight columns s in register s (fine groups: chunk s,
@@ -382,7 +368,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     load_scales(first, 0, true);
     if constexpr (!PASSES) load_x(0);
     {
-        const w4_buffer view = code_view(first, 0, true);
+        const Buffer view = code_view(first, 0, true);
 #pragma unroll
         for (int j = 0; j < NB; ++j) w[j] = read_codes(view, j);
     }
@@ -393,7 +379,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // requests find nothing: a branch around them would wait for them where it ends)
     auto step = [&](int tile, int pass, int in_block, int parity, bool more, int next_tile, int next_pass) W4_INLINE {
         load_scales(next_tile, next_pass, more);
-        const w4_buffer next_codes = code_view(next_tile, next_pass, more);
+        const Buffer next_codes = code_view(next_tile, next_pass, more);
         const float* my_scales = scales[parity][r] + wave * (NB * SLOTS * PER);
         if constexpr (SPLIT) {                               // (or the parts of all activations are kept in registers)
 #pragma unroll

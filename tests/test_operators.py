@@ -63,7 +63,7 @@ def rules(**kw):
 RULE_REFUSALS = [
     (dict(history=None), NULL), (dict(history_ranges=None), NULL), (dict(penalties=None), NULL), (dict(bias_ids=None), NULL),
     (dict(bias_values=None), NULL), (dict(bias_ranges=None), NULL), (dict(n_history=-1), SHAPE), (dict(n_biases=-1), SHAPE),
-    (dict(n_history=(1 << 30) + 1), UNSUPPORTED), (dict(n_biases=(1 << 30) + 1), UNSUPPORTED), (dict(mask=FAKE + 2), UNSUPPORTED),
+    (dict(n_history=(1 << 29) + 1), UNSUPPORTED), (dict(n_biases=(1 << 29) + 1), UNSUPPORTED), (dict(mask=FAKE + 2), UNSUPPORTED),
     (dict(history=FAKE + 1), UNSUPPORTED), (dict(penalties=FAKE + 2), UNSUPPORTED), (dict(bias_ranges=FAKE + 1), UNSUPPORTED)]
 
 
