@@ -3,6 +3,9 @@
 #pragma once
 #include "device_utils.h"
 
+// A lambda that works on registers it captures (they are in memory where it is not inlined).
+#define CORAL_INLINE __attribute__((always_inline))
+
 namespace {
 
 typedef __amdgpu_buffer_rsrc_t Buffer;

@@ -32,6 +32,11 @@ constexpr int kGateScores = kWords;
 constexpr int kGateScoreWords = 4096;
 constexpr int kPreparedWords = kWords + kGateScoreWords;
 
+// The k best under rules on logits count the workgroups of a row that have published in the same words (no
+// call uses them for both): one word a row, each in a 256-byte block of its own.
+constexpr int kRowArrival = kGateScores;
+constexpr int kRowArrivalStride = 64;
+
 constexpr Entry kMap[] = {
     {"fused_arrival", kFusedArrival, 1},
     {"gate_select_arrival", kGateSelectArrival, kGateSelectArrivalWords},

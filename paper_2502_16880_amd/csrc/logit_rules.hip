@@ -12,18 +12,11 @@
 namespace {
 
 constexpr size_t kLists = coral_ctrl::kPreparedWords * sizeof(unsigned);     // published lists start behind the control words
-constexpr int kMaxSlices = 256;                                              // lists that one merge takes
 constexpr int kMaxList = 1 << 29;                                            // entries of the flat lists
 
 size_t align_256(size_t x) { return (x + 255) / 256 * 256; }
 
-// Batches of 1024 values that a wave takes of a row: two where one would give more than four
-// workgroups for every compute unit.
-int batches(int M, int V) { return (int64_t)M * V > (int64_t)1024 * kRuleWaves * kRuleBatch ? 2 : 1; }
-int slices(int M, int V) {
-    const int slice = batches(M, V) * kRuleWaves * kRuleBatch;
-    return (V + 7 + slice - 1) / slice;                                      // up to seven values lead a row
-}
+int slices(int V) { return (V + 7 + kRuleSlice - 1) / kRuleSlice; }          // up to seven values lead a row
 
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
@@ -80,17 +73,6 @@ bool touches_rules(const RuleParams& p, const void* at, size_t bytes) {
            overlap(at, bytes, p.mask, (size_t)p.M * p.mask_words * 4);
 }
 
-template <int DT>
-void launch_adjust(const RuleParams& p, void* out, int nb, dim3 grid, hipStream_t stream) {
-    if (nb == 1) hipLaunchKernelGGL((k_logits_adjust<DT, 1>), grid, dim3(kRuleThreads), 0, stream, p, out);
-    else hipLaunchKernelGGL((k_logits_adjust<DT, 2>), grid, dim3(kRuleThreads), 0, stream, p, out);
-}
-template <int DT>
-void launch_topk(const RuleParams& p, const TopkParams& t, int nb, dim3 grid, hipStream_t stream) {
-    if (nb == 1) hipLaunchKernelGGL((k_logits_topk<DT, 1>), grid, dim3(kRuleThreads), 0, stream, p, t);
-    else hipLaunchKernelGGL((k_logits_topk<DT, 2>), grid, dim3(kRuleThreads), 0, stream, p, t);
-}
-
 struct TopkLayout {
     size_t sums, total;
 };
@@ -101,8 +83,8 @@ TopkLayout topk_layout(int M, int n_slices, int k) {
 
 }  // namespace
 
-static_assert(coral_ctrl::kLpGroupArrivalWords >= kMaxM, "one arrival counter per row");
-static_assert((CORAL_LOGITS_MAX_V + 7 + kRuleWaves * kRuleBatch - 1) / (kRuleWaves * kRuleBatch) <= kMaxSlices, "");
+static_assert(coral_ctrl::kRowArrivalStride * kMaxM <= coral_ctrl::kGateScoreWords, "one arrival counter per row");
+static_assert((CORAL_LOGITS_MAX_V + 7 + kRuleSlice - 1) / (kRuleSlice) <= kMaxSlices, "");
 
 extern "C" coral_status coral_logits_adjust(const void* logits, const coral_logit_rules* rules, int M, int V,
                                             coral_dtype dt, void* out, void* hip_stream) {
@@ -113,23 +95,17 @@ extern "C" coral_status coral_logits_adjust(const void* logits, const coral_logi
     if ((uintptr_t)out & 15u) return CORAL_ERR_UNSUPPORTED;
     const size_t bytes = (size_t)M * V * (dt == CORAL_F32 ? 4 : 2);
     if ((out != logits && overlap(out, bytes, logits, bytes)) || touches_rules(p, out, bytes)) return CORAL_ERR_UNSUPPORTED;
-    const int nb = batches(M, V);
-    const dim3 grid(slices(M, V), M);
+    const dim3 grid(slices(V), M), block(kRuleThreads);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (dt == CORAL_F32) launch_adjust<kF32>(p, out, nb, grid, stream);
-    else if (dt == CORAL_BF16) launch_adjust<kBF16>(p, out, nb, grid, stream);
-    else launch_adjust<kF16>(p, out, nb, grid, stream);
+    if (dt == CORAL_F32) hipLaunchKernelGGL(k_logits_adjust<kF32>, grid, block, 0, stream, p, out);
+    else if (dt == CORAL_BF16) hipLaunchKernelGGL(k_logits_adjust<kBF16>, grid, block, 0, stream, p, out);
+    else hipLaunchKernelGGL(k_logits_adjust<kF16>, grid, block, 0, stream, p, out);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }
 
 extern "C" size_t coral_logits_topk_workspace_bytes(int M, int V, int k) {
     if (M < 1 || V < 1 || k < 1 || k > V || M > kMaxM || k > kMaxK || V > CORAL_LOGITS_MAX_V) return 0;
-    size_t most = 0;
-    for (int m = 1; m <= M; ++m) {                                           // it serves fewer rows too
-        const size_t n = topk_layout(m, slices(m, V), k).total;
-        most = n > most ? n : most;
-    }
-    return most;
+    return topk_layout(M, slices(V), k).total;               // it serves fewer rows too
 }
 
 extern "C" coral_status coral_logits_topk(const void* logits, const coral_logit_rules* rules, int M, int V, int k,
@@ -142,7 +118,7 @@ extern "C" coral_status coral_logits_topk(const void* logits, const coral_logit_
     if (k < 1 || k > V) return CORAL_ERR_SHAPE;
     if (k > kMaxK) return CORAL_ERR_UNSUPPORTED;
     if (((uintptr_t)topk_ids | (uintptr_t)topk_logprob) & 3u) return CORAL_ERR_UNSUPPORTED;
-    const int n_slices = slices(M, V);
+    const int n_slices = slices(V);
     const TopkLayout L = topk_layout(M, n_slices, k);
     if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < L.total) return CORAL_ERR_WORKSPACE;
     const size_t out_bytes = (size_t)M * k * 4, in_bytes = (size_t)M * V * (dt == CORAL_F32 ? 4 : 2);
@@ -156,16 +132,15 @@ extern "C" coral_status coral_logits_topk(const void* logits, const coral_logit_
     TopkParams t = {};
     t.part = reinterpret_cast<Cand*>(ws + kLists);
     t.sums = reinterpret_cast<unsigned long long*>(ws + L.sums);
-    t.arrived = reinterpret_cast<unsigned*>(ws) + coral_ctrl::kLpGroupArrival;
+    t.arrived = reinterpret_cast<unsigned*>(ws) + coral_ctrl::kRowArrival;
     t.ids = topk_ids;
     t.logprob = topk_logprob;
     t.k = k;
     t.slices = n_slices;
-    const int nb = batches(M, V);
-    const dim3 grid(n_slices, M);
+    const dim3 grid(n_slices, M), block(kRuleThreads);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    if (dt == CORAL_F32) launch_topk<kF32>(p, t, nb, grid, stream);
-    else if (dt == CORAL_BF16) launch_topk<kBF16>(p, t, nb, grid, stream);
-    else launch_topk<kF16>(p, t, nb, grid, stream);
+    if (dt == CORAL_F32) hipLaunchKernelGGL(k_logits_topk<kF32>, grid, block, 0, stream, p, t);
+    else if (dt == CORAL_BF16) hipLaunchKernelGGL(k_logits_topk<kBF16>, grid, block, 0, stream, p, t);
+    else hipLaunchKernelGGL(k_logits_topk<kF16>, grid, block, 0, stream, p, t);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }

@@ -154,7 +154,6 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // The operands are read through buffer descriptors, which drop what lies behind their end: rows behind
 // the last one, and tokens and columns behind the activations, read as zero without a comparison.
 // Codes behind a row's last column are another row's and meet activations of zero.
-#define W4_INLINE __attribute__((always_inline))       // what works on registers that a lambda captures
 constexpr int kW4Block = 512;
 constexpr int kW4Held = kW4Block / kWave;
 
@@ -207,13 +206,13 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     const int s_row = threadIdx.x / 32, s_slot = threadIdx.x % 32;
     unsigned s_raw[SL], z_raw[SL];
     const unsigned s_first = (unsigned)s_row * p.n_groups, s_last = s_first + (p.n_groups - 1);
-    auto s_at = [&](int pass, int i) W4_INLINE {
+    auto s_at = [&](int pass, int i) CORAL_INLINE {
         const unsigned slot = pass * (kW4Held * NB * SLOTS) + s_slot + 32 * i;
         const unsigned at = s_first + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
         return at < s_last ? at : s_last;
     };
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
-    auto load_scales = [&](int tile, int pass, bool any) W4_INLINE {
+    auto load_scales = [&](int tile, int pass, bool any) CORAL_INLINE {
         const size_t first_group = (size_t)tile * 16 * p.n_groups, all = (size_t)p.N * p.n_groups;
         const Buffer view = buffer_view(p.scales, first_group * W, all * W, any);
         const Buffer z_view = buffer_view(p.zeros, first_group, all, any);
@@ -224,7 +223,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
             if constexpr (KIND == kW4Zero) z_raw[i] = buffer_read1(z_view, s_at(pass, i));
         }
     };
-    auto put_scales = [&](int parity) W4_INLINE {
+    auto put_scales = [&](int parity) CORAL_INLINE {
         float* dst = scales[parity][s_row] + s_slot * PER;
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
@@ -243,14 +242,14 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         const int e = j * kWave + lane;
         at[j] = (unsigned)(e / CHUNKS) * (unsigned)row_bytes + (unsigned)(wave * CHUNKS + e % CHUNKS) * 16u;
     }
-    auto read_codes = [&](const Buffer& view, int j) W4_INLINE {
+    auto read_codes = [&](const Buffer& view, int j) CORAL_INLINE {
         if constexpr (EVEN) return buffer_read16<kBufferStream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
         else return buffer_read16<kBufferStream>(view, at[EVEN ? 0 : j]);
     };
-    auto code_view = [&](int tile, int pass, bool any) W4_INLINE {
+    auto code_view = [&](int tile, int pass, bool any) CORAL_INLINE {
         return buffer_view(p.codes, (size_t)tile * 16 * row_bytes + pass * (PASS_COLS / 2), (size_t)p.N * row_bytes, any);
     };
-    auto put = [&](int j) W4_INLINE {
+    auto put = [&](int j) CORAL_INLINE {
         const int e = j * kWave + lane;
         store_vec(&slices[wave][e / CHUNKS * CODE_ROW + e % CHUNKS], w[j]);
     };
@@ -259,7 +258,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // 16-bit activations: in the order of memory first, lane 16 a + c the eight columns c of a unit of
     // token 4 i + a in register i (the products' own layout, 64 bytes of 16 tokens a load, made the first
     // tile of 32 tokens wait for several us)
-    auto load_x = [&](int pass) W4_INLINE {
+    auto load_x = [&](int pass) CORAL_INLINE {
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -277,7 +276,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // ... then lane 16 q + r token r, chunk q and eight columns s in register s (fine groups: chunk s,
     // eight columns q), through the wave's slice: as many tokens at a time as it holds
     constexpr int HALVES = SLICE >= 16 * X_ROW ? 1 : 2, X_MASK = 16 / HALVES - 1;
-    auto exchange = [&](uint4 (&v)[4][XV]) W4_INLINE {
+    auto exchange = [&](uint4 (&v)[4][XV]) CORAL_INLINE {
         u32x4_t o[4] = {};
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
         for (int s = 0; s < 4; ++s) v[s][0] = make_uint4(o[s].x, o[s].y, o[s].z, o[s].w);
     };
-    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS], bool split) W4_INLINE {
+    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS], bool split) CORAL_INLINE {
         if constexpr (DT == kF32) {
             if (split) {
                 const uint4 a = v[0], b = v[1];
@@ -319,7 +318,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // the offset's part of the sums: of -24 x where every zero point is 8, else of -16 x, times 1 + zero / 16
     constexpr unsigned kMinus = KIND == kW4Sym ? (OP == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u) : OP == kF16 ? 0xCC00CC00u : 0xC180C180u;
     const uint4 minus = make_uint4(kMinus, kMinus, kMinus, kMinus);
-    auto arrange_x = [&]() W4_INLINE {
+    auto arrange_x = [&]() CORAL_INLINE {
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -377,7 +376,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     __syncthreads();                                         // the first tile's scales are there
     // one tile of a pass, which requests the scales and codes of the next one; more: there is one (else the
     // requests find nothing: a branch around them would wait for them where it ends)
-    auto step = [&](int tile, int pass, int in_block, int parity, bool more, int next_tile, int next_pass) W4_INLINE {
+    auto step = [&](int tile, int pass, int in_block, int parity, bool more, int next_tile, int next_pass) CORAL_INLINE {
         load_scales(next_tile, next_pass, more);
         const Buffer next_codes = code_view(next_tile, next_pass, more);
         const float* my_scales = scales[parity][r] + wave * (NB * SLOTS * PER);
