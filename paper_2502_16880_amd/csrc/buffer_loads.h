@@ -11,14 +11,15 @@ namespace {
 typedef __amdgpu_buffer_rsrc_t Buffer;
 // The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed), or none.
 __device__ __forceinline__ Buffer buffer_view(const void* base, size_t first, size_t bytes, bool any = true) {
-    const size_t left = any ? bytes - first : 0;
+    const size_t left = any && first < bytes ? bytes - first : 0;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,
                                              left < 0xffffffffu ? (unsigned)left : 0xffffffffu, 0x00020000);
 }
+// An offset is a lane's own: a part in a scalar register of its own is not compared with the view's end.
 constexpr int kBufferStream = 2;                 // non-temporal: what is read once
 template <int AUX = 0>
-__device__ __forceinline__ uint4 buffer_read16(Buffer b, unsigned at, unsigned uniform_at = 0) {
-    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, (int)uniform_at, AUX);
+__device__ __forceinline__ uint4 buffer_read16(Buffer b, unsigned at) {
+    const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(b, (int)at, 0, AUX);
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 __device__ __forceinline__ unsigned buffer_read4(Buffer b, unsigned at) { return (unsigned)__builtin_amdgcn_raw_buffer_load_b32(b, (int)at, 0, 0); }

@@ -243,7 +243,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         at[j] = (unsigned)(e / CHUNKS) * (unsigned)row_bytes + (unsigned)(wave * CHUNKS + e % CHUNKS) * 16u;
     }
     auto read_codes = [&](const Buffer& view, int j) CORAL_INLINE {
-        if constexpr (EVEN) return buffer_read16<kBufferStream>(view, at[0], (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
+        if constexpr (EVEN) return buffer_read16<kBufferStream>(view, at[0] + (unsigned)(j * (kWave / CHUNKS)) * (unsigned)row_bytes);
         else return buffer_read16<kBufferStream>(view, at[EVEN ? 0 : j]);
     };
     auto code_view = [&](int tile, int pass, bool any) CORAL_INLINE {
