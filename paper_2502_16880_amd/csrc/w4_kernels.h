@@ -1,5 +1,6 @@
 // Host side of the products with 4-bit weights: which kernel a call takes (w4_matvec.hip), and the
-// kernels' instantiations by storage type (w4_held_{bf16,f16,f32}.hip, compiled side by side).
+// kernels' instantiations by storage type (w4_held_{bf16,f16,f32}.hip, w4_rows_{bf16,f16}.hip, compiled side
+// by side).
 #pragma once
 #include "w4_matvec.h"
 
@@ -12,7 +13,23 @@ __attribute__((visibility("hidden"))) const void* coral_w4_held_bf16(int kind, b
 __attribute__((visibility("hidden"))) const void* coral_w4_held_f16(int kind, bool fine, int t, int nb, bool passes);
 __attribute__((visibility("hidden"))) const void* coral_w4_held_f32(int kind, bool fine, int t, int nb, bool passes);
 
+// k_w4_rows for r tiles of 16 rows a wave.
+__attribute__((visibility("hidden"))) const void* coral_w4_rows_bf16(int kind, bool fine, int r);
+__attribute__((visibility("hidden"))) const void* coral_w4_rows_f16(int kind, bool fine, int r);
+
 namespace {
+
+template <int DT, int KIND, bool FINE>
+w4_fn w4_pick_rows(int r) {
+    return r == 2 ? k_w4_rows<DT, KIND, FINE, 2> : r == 3 ? k_w4_rows<DT, KIND, FINE, 3> : k_w4_rows<DT, KIND, FINE, 4>;
+}
+template <int DT>
+const void* w4_rows(int kind, bool fine, int r) {
+    w4_fn fn = nullptr;
+    if (fine) fn = kind == kW4E2M1 ? w4_pick_rows<DT, kW4E2M1, true>(r) : kind == kW4Sym ? w4_pick_rows<DT, kW4Sym, true>(r) : w4_pick_rows<DT, kW4Zero, true>(r);
+    else fn = kind == kW4E2M1 ? w4_pick_rows<DT, kW4E2M1, false>(r) : kind == kW4Sym ? w4_pick_rows<DT, kW4Sym, false>(r) : w4_pick_rows<DT, kW4Zero, false>(r);
+    return reinterpret_cast<const void*>(fn);
+}
 
 template <int DT, int KIND, bool FINE>
 w4_fn w4_pick_held(int t, int nb, bool passes) {

@@ -205,22 +205,25 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // scales: thread (row tid / 32, slots tid % 32 + 32 i)
     const int s_row = threadIdx.x / 32, s_slot = threadIdx.x % 32;
     unsigned s_raw[SL], z_raw[SL];
-    const unsigned s_first = (unsigned)s_row * p.n_groups, s_last = s_first + (p.n_groups - 1);
-    auto s_at = [&](int pass, int i) CORAL_INLINE {
-        const unsigned slot = pass * (kW4Held * NB * SLOTS) + s_slot + 32 * i;
-        const unsigned at = s_first + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
-        return at < s_last ? at : s_last;
+    // (of a slot behind the row's columns one behind the operand's end: zero, whatever the last scale is)
+    auto s_at = [&](unsigned tid, int pass, int i, unsigned size) CORAL_INLINE {
+        const unsigned slot = pass * (kW4Held * NB * SLOTS) + tid % 32 + 32 * i;
+        const unsigned at = tid / 32 * p.n_groups + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;
+        return at * size | behind;
     };
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
     auto load_scales = [&](int tile, int pass, bool any) CORAL_INLINE {
         const size_t first_group = (size_t)tile * 16 * p.n_groups, all = (size_t)p.N * p.n_groups;
         const Buffer view = buffer_view(p.scales, first_group * W, all * W, any);
         const Buffer z_view = buffer_view(p.zeros, first_group, all, any);
+        unsigned tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                        // (what follows from it is not kept through the products)
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
-            if constexpr (DT == kF32) s_raw[i] = buffer_read4(view, s_at(pass, i) * W);
-            else s_raw[i] = buffer_read2(view, s_at(pass, i) * W);
-            if constexpr (KIND == kW4Zero) z_raw[i] = buffer_read1(z_view, s_at(pass, i));
+            if constexpr (DT == kF32) s_raw[i] = buffer_read4(view, s_at(tid, pass, i, W));
+            else s_raw[i] = buffer_read2(view, s_at(tid, pass, i, W));
+            if constexpr (KIND == kW4Zero) z_raw[i] = buffer_read1(z_view, s_at(tid, pass, i, 1u));
         }
     };
     auto put_scales = [&](int parity) CORAL_INLINE {
@@ -495,6 +498,265 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                 }
             }
         }
+    }
+}
+
+// ---------------------------------------------------------------- activations shared in LDS
+// Many tokens and many rows, 16-bit activations: a wave takes 16 R weight rows for itself, the columns from
+// first to last, and 16 T tokens.  The activations of a unit of 128 columns lie in LDS, in the layout
+// of the products, for all eight waves; the next unit's are on their way to the other buffer.  So a
+// unit's activations are read from LDS once for R tiles of rows, the sums stay in registers, and no
+// wave waits for another's.  The codes come two units at a time, 128 bytes of eight rows a load, and are
+// exchanged through a slice of LDS of the wave's own, as are the scales.
+template <int DT, int KIND, bool FINE, int R>
+__global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
+    static_assert(DT != kF32, "");
+    constexpr bool INT = KIND != kW4E2M1, ZERO = KIND == kW4Zero, LATE = !ZERO;
+    constexpr int T = kMaxM / 16, ROWS = 16 * R, SLOTS = FINE ? 4 : 1;       // (of a unit)
+    constexpr int STAGE_SLOTS = 2 * SLOTS, ENTRIES = ROWS * STAGE_SLOTS, SL = (ENTRIES + kWave - 1) / kWave, STRIDE = STAGE_SLOTS + 1;
+    constexpr int CODE_ROW = 9, XL = T * 256 / kW4Block;
+    static_assert(XL * kW4Block == T * 256, "");
+    __shared__ uint4 xs[2][2][T][4][kWave];                  // two stages of two units
+    __shared__ uint4 slices[kW4Held][ROWS * CODE_ROW];
+    __shared__ unsigned scales[kW4Held][ROWS * STRIDE];      // fp32 scale, or the 16-bit scale and 1 + zero / 16 in fp16
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int r = lane & 15, q = lane >> 4;
+    const int row_bytes = p.K / 2, units = (p.K + kW4UnitCols - 1) / kW4UnitCols;
+    const size_t row0 = ((size_t)blockIdx.x * kW4Held + wave) * ROWS;
+
+    // (a lane's number anew: addresses are worked out where they are used, not kept through the products)
+    auto fresh_lane = [&]() CORAL_INLINE {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    const size_t code_bytes = (size_t)p.N * row_bytes;
+    uint4 w[2 * R];
+    auto load_codes = [&](int stage, int i) CORAL_INLINE {
+        const int l = fresh_lane();
+        const Buffer view = buffer_view(p.codes, row0 * row_bytes + (size_t)stage * kW4UnitCols, code_bytes, 2 * stage < units);
+        w[i] = buffer_read16<kBufferStream>(view, (unsigned)(i * 8 + l / 8) * (unsigned)row_bytes + (unsigned)(l % 8) * 16u);
+    };
+    auto put_codes = [&]() CORAL_INLINE {
+        const int l = fresh_lane();
+#pragma unroll
+        for (int i = 0; i < 2 * R; ++i) store_vec(&slices[wave][(i * 8 + l / 8) * CODE_ROW + l % 8], w[i]);
+    };
+    const size_t scale_first = row0 * p.n_groups, scale_all = (size_t)p.N * p.n_groups;
+    unsigned s_raw[SL], z_raw[SL];
+    auto load_scales = [&](int stage, int i) CORAL_INLINE {
+        const Buffer view = buffer_view(p.scales, scale_first * 2, scale_all * 2, 2 * stage < units);
+        const Buffer z_view = buffer_view(p.zeros, scale_first, scale_all, 2 * stage < units);
+        const int e = i * kWave + fresh_lane();
+        const unsigned slot = stage * STAGE_SLOTS + e % STAGE_SLOTS, g = FINE ? slot >> (p.group == 64) : w4_group_of(p, slot);
+        const unsigned at = (unsigned)(e / STAGE_SLOTS) * (unsigned)p.n_groups + g;
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;         // (as in k_w4_held)
+        s_raw[i] = buffer_read2(view, at * 2u | behind);
+        if constexpr (ZERO) z_raw[i] = buffer_read1(z_view, at | behind);
+    };
+    // one of a stage's loads
+    constexpr int LOADS = 2 * R + SL;
+    static_assert(LOADS <= 4 * R, "one for every product of a unit");
+    auto load_part = [&](int stage, int i) CORAL_INLINE {
+        if (i < 2 * R) load_codes(stage, i);
+        else if (i < LOADS) load_scales(stage, i - 2 * R);
+    };
+    auto put_scales = [&]() CORAL_INLINE {
+        const int l = fresh_lane();
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            const int e = i * kWave + l;
+            const unsigned zero = ZERO ? __builtin_bit_cast(unsigned short, (_Float16)fmaf((float)z_raw[i], 0.0625f, 1.0f)) : 0u;
+            const unsigned word = ZERO ? s_raw[i] << 16 | zero : __float_as_uint(widen16<DT>((unsigned short)s_raw[i]));
+            if (ENTRIES % kWave == 0 || e < ENTRIES) scales[wave][e / STAGE_SLOTS * STRIDE + e % STAGE_SLOTS] = word;
+        }
+    };
+    const Buffer x_view = buffer_view(p.x, 0, (size_t)p.M * p.K * 2);
+    uint4 x_next[XL];
+    // a wave's load is of eight tokens, 128 bytes each; eight neighbouring lanes write to different banks
+    auto x_token = [&](int i, int l) CORAL_INLINE { return (i * kW4Held + wave) / 2 * 8 + l % 8; };
+    auto x_chunk = [&](int i, int l) CORAL_INLINE { return (i * kW4Held + wave) % 2 * 8 + l / 8; };
+    auto load_x = [&](int unit) CORAL_INLINE {
+        const int l = fresh_lane();
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            const int col = unit * kW4UnitCols + x_chunk(i, l) * 8;
+            x_next[i] = buffer_read16(x_view, col < p.K ? ((unsigned)x_token(i, l) * (unsigned)p.K + (unsigned)col) * 2u : 0xffffffe0u);
+        }
+    };
+    auto put_x = [&](int buffer, int j) CORAL_INLINE {
+        const int l = fresh_lane();
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            const int token = x_token(i, l), c = x_chunk(i, l);
+            const int s = FINE ? c / 4 : c % 4, chunk = FINE ? c % 4 : c / 4;
+            store_vec(&xs[buffer][j][token / 16][s][chunk * 16 + token % 16], w4_order<KIND>(x_next[i]));
+        }
+    };
+    const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
+    constexpr unsigned kMinus = KIND == kW4Sym ? (DT == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u) : DT == kF16 ? 0xCC00CC00u : 0xC180C180u;
+    const uint4 minus = make_uint4(kMinus, kMinus, kMinus, kMinus);
+    f32x4_t y[R][T];
+#pragma unroll
+    for (int a = 0; a < R; ++a)
+#pragma unroll
+        for (int t = 0; t < T; ++t) y[a][t] = zero4;
+    auto scale_word = [&](int a, int slot) CORAL_INLINE { return scales[wave][(a * 16 + r) * STRIDE + slot]; };
+    auto scale_of = [&](unsigned word) CORAL_INLINE { return ZERO ? widen16<DT>((unsigned short)(word >> 16)) : __uint_as_float(word); };
+    // where the sums of a group start: at the offset's part
+    auto start = [&](unsigned word, const f32x4_t (&offset)[T], f32x4_t (&acc)[T]) CORAL_INLINE {
+        const float zero = ZERO ? (float)__builtin_bit_cast(_Float16, (unsigned short)word) : 0.f;
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            acc[t] = offset[t];
+            if constexpr (ZERO) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) acc[t][v] *= zero;
+            }
+        }
+    };
+    auto add = [&](int a, int t, float scale, const f32x4_t& acc) CORAL_INLINE {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) y[a][t][v] = fmaf(scale, acc[v], y[a][t][v]);
+    };
+    // Unit j of a stage.  The products of T token tiles go off together, and while they run the last ones' sums
+    // are scaled and added and the next ones' operand is made: the fences keep it so, or the compiler waits
+    // for each product by itself.
+    auto unit = [&](int buffer, int j, auto meanwhile) CORAL_INLINE {
+        if constexpr (FINE) {
+            uint4 x[T];
+            unsigned code[R], word[R];
+            auto fetch = [&](int s, uint4 (&to)[T], unsigned (&c)[R], unsigned (&w)[R]) CORAL_INLINE {
+#pragma unroll
+                for (int a = 0; a < R; ++a) {
+                    c[a] = reinterpret_cast<const unsigned*>(&slices[wave][(a * 16 + r) * CODE_ROW + j * 4 + s])[q];
+                    w[a] = scale_word(a, j * SLOTS + s);
+                }
+#pragma unroll
+                for (int t = 0; t < T; ++t) to[t] = load_vec(&xs[buffer][j][t][s][lane]);
+            };
+            f32x4_t acc[LATE ? 2 : 1][T];
+            float scale[LATE ? 2 : 1] = {};
+            fetch(0, x, code, word);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                uint4 x_then[T];
+                unsigned code_then[R], word_then[R];
+                if (s < 3) fetch(s + 1, x_then, code_then, word_then);           // on their way during these products
+                f32x4_t offset[T];
+#pragma unroll
+                for (int t = 0; t < T; ++t) offset[t] = INT ? mfma_tile<DT>(x[t], minus, zero4) : zero4;
+                uint4 op = w4_operand<DT, KIND>(code[0]);
+#pragma unroll
+                for (int a = 0; a < R; ++a) {
+                    const int now = LATE ? (s * R + a) & 1 : 0;
+                    start(word[a], offset, acc[now]);
+                    scale[now] = scale_of(word[a]);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < T; ++t) acc[now][t] = mfma_tile<DT>(x[t], op, acc[now][t]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (LATE && s + a > 0) {
+#pragma unroll
+                        for (int t = 0; t < T; ++t) add(a > 0 ? a - 1 : R - 1, t, scale[LATE ? now ^ 1 : 0], acc[LATE ? now ^ 1 : 0][t]);
+                    }
+                    if (a + 1 < R) op = w4_operand<DT, KIND>(code[a + 1]);
+                    meanwhile(s * R + a);
+                    if constexpr (!LATE) {
+#pragma unroll
+                        for (int t = 0; t < T; ++t) add(a, t, scale[now], acc[now][t]);
+                    }
+                }
+                if (s < 3) {
+#pragma unroll
+                    for (int t = 0; t < T; ++t) x[t] = x_then[t];
+#pragma unroll
+                    for (int a = 0; a < R; ++a) {
+                        code[a] = code_then[a];
+                        word[a] = word_then[a];
+                    }
+                }
+            }
+            if constexpr (LATE) {
+#pragma unroll
+                for (int t = 0; t < T; ++t) add(R - 1, t, scale[(4 * R - 1) & 1], acc[(4 * R - 1) & 1][t]);
+            }
+        } else {
+            uint4 x[T][4];
+            f32x4_t offset[T];
+            uint4 code = load_vec(&slices[wave][r * CODE_ROW + j * 4 + q]);
+            unsigned word = scale_word(0, j);
+#pragma unroll
+            for (int t = 0; t < T; ++t) offset[t] = zero4;
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int t = 0; t < T; ++t) x[t][s] = load_vec(&xs[buffer][j][t][s][lane]);
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+                    if constexpr (INT) offset[t] = mfma_tile<DT>(x[t][s], minus, offset[t]);
+            uint4 op = w4_operand<DT, KIND>(code.x);
+#pragma unroll
+            for (int a = 0; a < R; ++a) {
+                f32x4_t acc[T];
+                start(word, offset, acc);
+                const float scale = scale_of(word);
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int t = 0; t < T; ++t) acc[t] = mfma_tile<DT>(x[t][s], op, acc[t]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    op = w4_operand<DT, KIND>(s == 0 ? code.y : s == 1 ? code.z : s == 2 ? code.w : code.x);
+                    if (s == 2 && a + 1 < R) {               // the next tile's
+                        code = load_vec(&slices[wave][((a + 1) * 16 + r) * CODE_ROW + j * 4 + q]);
+                        word = scale_word(a + 1, j);
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < T; ++t) add(a, t, scale, acc[t]);
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_part(0, i);
+    load_x(0);
+    put_x(0, 0);
+    load_x(1);                                               // (behind the last column there is none)
+    put_x(0, 1);
+    __syncthreads();
+    for (int stage = 0; 2 * stage < units; ++stage) {        // uniform, as all here
+        const int buffer = stage & 1;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        put_codes();
+        put_scales();
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        load_x(2 * stage + 2);                               // (in front of the codes, which take longer)
+        if constexpr (!FINE) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) load_part(stage + 1, i);
+        }
+        unit(buffer, 0, [&](int i) CORAL_INLINE { load_part(stage + 1, i); });
+        put_x(buffer ^ 1, 0);
+        load_x(2 * stage + 3);
+        if (2 * stage + 1 < units) unit(buffer, 1, [](int) {});
+        put_x(buffer ^ 1, 1);
+        __syncthreads();
+    }
+#pragma unroll
+    for (int a = 0; a < R; ++a) {
+        const size_t n = row0 + a * 16 + r;
+        if (n >= (size_t)p.N) continue;
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int m = t * 16 + 4 * q + v;
+                if (m < p.M) w4_store<DT>(p, m, (int)n, y[a][t][v]);
+            }
     }
 }
 

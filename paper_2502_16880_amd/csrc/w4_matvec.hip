@@ -24,6 +24,26 @@ W4Plan plan_held(const W4Params& p, coral_dtype dt) {
     return {t, nb, false};
 }
 
+// k_w4_rows' tiles of 16 rows a wave, or 0 where k_w4_held is taken: for up to 32 tokens (32 tokens, 128256 rows
+// of 4096 columns: 75 us held, 82 us shared) and where a round of workgroups would not be full.  A round, one
+// workgroup of 128 r rows for each of 256 compute units, takes about as long as 870 (r + 2) tiles held.
+// Measured with 64 tokens, bf16 (us), held and shared with 2, 3 and 4 tiles: 50257 x 4096 61, 65, 79, 97;
+// 65536 x 4096 69, 67, 77, 92; 100000 x 4096 111, 115, 148, 101; 152064 x 3584 168, 155, 144, 167.
+int plan_rows(const W4Params& p, coral_dtype dt) {
+    if (dt == CORAL_F32 || p.M <= 32) return 0;
+    const int tiles = (p.N - 1) / 16 + 1;
+    int best = 0;
+    int64_t least = tiles;
+    for (int r = 2; r <= 4; ++r) {
+        const int64_t rounds = (tiles - 1) / (256 * kW4Held * r) + 1, cost = rounds * (r + 2) * 870;
+        if (cost < least) {
+            best = r;
+            least = cost;
+        }
+    }
+    return best;
+}
+
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
     return a && b && x < y + b_bytes && y < x + a_bytes;
@@ -70,9 +90,15 @@ extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const 
     p.per_group = group < kW4UnitCols ? 1 : group / kW4UnitCols;
     p.per_group_inv = (unsigned)((((uint64_t)1 << 32) + p.per_group - 1) / p.per_group);
     const int kind = code == CORAL_W4_E2M1 ? kW4E2M1 : zeros ? kW4Zero : kW4Sym;
-    const W4Plan plan = plan_held(p, dt);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool fine = group < kW4UnitCols;
+    if (const int r = plan_rows(p, dt)) {
+        const void* rows = dt == CORAL_BF16 ? coral_w4_rows_bf16(kind, fine, r) : coral_w4_rows_f16(kind, fine, r);
+        const int wg_rows = kW4Held * 16 * r;
+        hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(rows)), dim3((N - 1) / wg_rows + 1), dim3(kW4Block), 0, stream, p);
+        return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
+    }
+    const W4Plan plan = plan_held(p, dt);
     const void* held = dt == CORAL_F32    ? coral_w4_held_f32(kind, fine, plan.t, plan.nb, plan.passes)
                        : dt == CORAL_BF16 ? coral_w4_held_bf16(kind, fine, plan.t, plan.nb, plan.passes)
                                           : coral_w4_held_f16(kind, fine, plan.t, plan.nb, plan.passes);

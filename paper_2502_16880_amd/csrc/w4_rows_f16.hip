@@ -1,0 +1,5 @@
+// k_w4_rows for fp16 activations.
+#include "coral_lmhead.h"
+#include "w4_kernels.h"
+
+const void* coral_w4_rows_f16(int kind, bool fine, int r) { return w4_rows<kF16>(kind, fine, r); }

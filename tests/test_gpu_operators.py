@@ -98,6 +98,54 @@ def test_matvec_w4(coral, dtype, kind, zeros, M, N, K, group):
     assert torch.equal(c.run(coral), y)                            # the same bits every time
 
 
+# many tokens and many rows: two, three and four tiles of rows a wave, the last ones not full
+MANY = [(64, 55700, 136, 32), (33, 139300, 136, 64), (50, 83600, 392, 128), (63, 83601, 8, 32), (64, 60001, 1032, 256), (40, 90000, 256, 64)]
+
+
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K,group", MANY)
+def test_matvec_w4_many_rows(coral, dtype, kind, zeros, M, N, K, group):
+    c = Product(dtype, M, N, K, group, kind, zeros, seed=5)
+    y, untouched = guarded((M, N), torch.float32)
+    c.run(coral, out=y)
+    rows = np.unique(np.r_[0:700, N - 700:N, 0:N:97])
+    c.check(y, rows=rows)
+    untouched()
+    assert bool(torch.isfinite(y).all()) and torch.equal(c.run(coral), y)
+    few = Product(dtype, 16, N, K, group, kind, zeros, seed=5)     # the same rows through the other kernel
+    few.x, few.codes, few.scales, few.zeros = c.x[:16].contiguous(), c.codes, c.scales, c.zeros
+    want = few.run(coral)
+    assert float((y[:16] - want).abs().max()) <= 1e-4 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_matvec_w4_many_rows_epilogue(coral, dtype):
+    M, N, K = 45, 84000, 200
+    c = Product(dtype, M, N, K, 64, bias=True, residual=True, seed=6)
+    y, untouched = guarded((M, N), TORCH[dtype])
+    c.run(coral, "silu", out=y)
+    c.check(y, "silu", rows=np.r_[0:300, N - 300:N])
+    untouched()
+    same = c.residual.clone()
+    assert torch.equal(c.run(coral, "silu", residual=same, out=same), y)
+
+
+@pytest.mark.parametrize("N", [33, 83600])
+@pytest.mark.parametrize("K,group", [(40, 32), (200, 64), (648, 128)])
+@pytest.mark.parametrize("M", [3, 50])
+def test_matvec_w4_infinite_scales_of_a_rows_last_group(coral, M, N, K, group):
+    c = Product("bf16", M, N, K, group, seed=7)
+    c.scales[1::2, -1] = float("inf")
+    y = c.run(coral)
+    first = (K - 1) // group * group
+    w = torch.from_numpy(plain.unpack(c.codes_host[1::2, first // 2:]).astype(np.float32)).cuda()
+    zero = c.zeros[1::2, -1:].float()
+    last = c.x[:, first:].float() @ (w - zero).t()
+    sure = last.abs() > 1e-3
+    assert torch.equal(y[:, 1::2][sure], (last.sign() * float("inf"))[sure]) and bool(torch.isfinite(y[:, ::2]).all())
+
+
 @pytest.mark.parametrize("act", ["identity", "silu", "relu"])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,N,K", [(1, 512, 512), (9, 131, 1024), (40, 77, 640)])
