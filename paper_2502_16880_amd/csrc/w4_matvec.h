@@ -28,6 +28,8 @@ struct W4Params {
 };
 
 constexpr int kW4UnitCols = 128;                 // columns of a unit: four products of 32
+// A slot is the columns of a unit that share a scale: SLOTS of them, of 32 or 64 columns, where groups are
+// finer than a unit, else one.
 
 template <int DT>
 constexpr int kW4Op = DT == kF16 ? kF16 : kBF16; // operand type of the products
@@ -173,16 +175,16 @@ constexpr int w4_held_regs(int dt, int t, int nb) { return dt == kF32 ? (t * nb 
 // T tiles of 16 tokens, NB units a wave.  PASSES: the columns are more than the waves hold and are taken
 // in passes; the workgroup goes through a block of tiles once a pass, adding the tiles' sums up in
 // LDS, before the next block.  Codes are still read once, activations once a block.
-template <int DT, int KIND, bool FINE, int T, int NB, bool PASSES = false>
+template <int DT, int KIND, int SLOTS, int T, int NB, bool PASSES = false>
 __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) void k_w4_held(W4Params p) {
     // fp32 activations are held as their parts where the registers allow it, else split at every use
     constexpr bool SPLIT = DT == kF32 && T * NB > 3;
     constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>, XR = DT == kF32 ? 2 : 1, XV = SPLIT ? 2 : PARTS;
     constexpr bool PAIR = KIND == kW4Zero && DT != kF32;     // scale and zero as two 16-bit values of one word
     constexpr int PER = KIND == kW4Zero && DT == kF32 ? 2 : 1;
-    // A slot is the columns that share a scale: a product's 32 where groups are finer than a unit, else
-    // a unit's.  SL: slots of a row that a thread brings for a tile (the last ones may lie behind the row).
-    constexpr int SLOTS = FINE ? 4 : 1, SL = (NB * kW4Held * SLOTS + 31) / 32, STRIDE = (SL * 32 + 1) * PER;
+    // SL: slots of a row that a thread brings for a tile (the last ones may lie behind the row).
+    constexpr bool FINE = SLOTS > 1;
+    constexpr int EACH = 4 / SLOTS, SL = (NB * kW4Held * SLOTS + 31) / 32, STRIDE = (SL * 32 + 1) * PER;
     __shared__ float sums[2][kW4Held][T * 256];
     __shared__ float scales[2][16][STRIDE];                  // (scale, 1 + zero / 16); rows start on different banks
     // a wave's own: rows of codes that start on different banks, and before that the exchange of activations
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     // (of a slot behind the row's columns one behind the operand's end: zero, whatever the last scale is)
     auto s_at = [&](unsigned tid, int pass, int i, unsigned size) CORAL_INLINE {
         const unsigned slot = pass * (kW4Held * NB * SLOTS) + tid % 32 + 32 * i;
-        const unsigned at = tid / 32 * p.n_groups + (FINE ? slot >> (p.group == 64) : w4_group_of(p, slot));
+        const unsigned at = tid / 32 * p.n_groups + (FINE ? slot : w4_group_of(p, slot));
         const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;
         return at * size | behind;
     };
@@ -358,10 +360,10 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                     for (int s = 0; s < 4; ++s) {
                         uint4 part[PARTS];
                         parts_of(x[t][j][s], part, SPLIT);
-                        if (FINE) sum = zero4;
+                        if (s % EACH == 0) sum = zero4;
 #pragma unroll
                         for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(part[c], minus, sum);
-                        if (r == 0 && (FINE || s == 3)) x_sums[wave][j][FINE ? s : 0][t][q] = sum;      // (read by this wave only)
+                        if (r == 0 && s % EACH == EACH - 1) x_sums[wave][j][s / EACH][t][q] = sum;      // (read by this wave only)
                     }
                     if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
                 }
@@ -417,8 +419,8 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
             float scale = 0.f;
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
-                if (FINE || s == 0) {                        // the sums start at the offset's part
-                    const int slot = j * SLOTS + s;
+                if (s % EACH == 0) {                         // the sums start at the offset's part
+                    const int slot = j * SLOTS + s / EACH;
                     scale = my_scales[slot * PER];
                     float zero = 0.f;
                     if constexpr (PER == 2) zero = my_scales[slot * PER + 1];
@@ -430,7 +432,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                     for (int t = 0; t < T; ++t) {
                         acc[t] = zero4;
-                        if constexpr (KIND != kW4E2M1) acc[t] = x_sums[wave][j][s][t][q];
+                        if constexpr (KIND != kW4E2M1) acc[t] = x_sums[wave][j][s / EACH][t][q];
                         if constexpr (KIND == kW4Zero) {
 #pragma unroll
                             for (int v = 0; v < 4; ++v) acc[t][v] *= zero;
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                     for (int c = PARTS - 1; c >= 0; --c) acc[t] = mfma_tile<OP>(part[c], op, acc[t]);      // the small parts first
                 }
-                if (!FINE && s != 3) continue;
+                if (s % EACH != EACH - 1) continue;
 #pragma unroll
                 for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -508,11 +510,12 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 // unit's activations are read from LDS once for R tiles of rows, the sums stay in registers, and no
 // wave waits for another's.  The codes come two units at a time, 128 bytes of eight rows a load, and are
 // exchanged through a slice of LDS of the wave's own, as are the scales.
-template <int DT, int KIND, bool FINE, int R>
+template <int DT, int KIND, int SLOTS, int R>
 __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
     static_assert(DT != kF32, "");
-    constexpr bool INT = KIND != kW4E2M1, ZERO = KIND == kW4Zero, LATE = !ZERO;
-    constexpr int T = kMaxM / 16, ROWS = 16 * R, SLOTS = FINE ? 4 : 1;       // (of a unit)
+    constexpr bool INT = KIND != kW4E2M1, ZERO = KIND == kW4Zero, LATE = !INT;
+    constexpr bool FINE = SLOTS > 1;
+    constexpr int T = kMaxM / 16, ROWS = 16 * R, EACH = 4 / SLOTS;
     constexpr int STAGE_SLOTS = 2 * SLOTS, ENTRIES = ROWS * STAGE_SLOTS, SL = (ENTRIES + kWave - 1) / kWave, STRIDE = STAGE_SLOTS + 1;
     constexpr int CODE_ROW = 9, XL = T * 256 / kW4Block;
     static_assert(XL * kW4Block == T * 256, "");
@@ -549,7 +552,7 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
         const Buffer view = buffer_view(p.scales, scale_first * 2, scale_all * 2, 2 * stage < units);
         const Buffer z_view = buffer_view(p.zeros, scale_first, scale_all, 2 * stage < units);
         const int e = i * kWave + fresh_lane();
-        const unsigned slot = stage * STAGE_SLOTS + e % STAGE_SLOTS, g = FINE ? slot >> (p.group == 64) : w4_group_of(p, slot);
+        const unsigned slot = stage * STAGE_SLOTS + e % STAGE_SLOTS, g = FINE ? slot : w4_group_of(p, slot);
         const unsigned at = (unsigned)(e / STAGE_SLOTS) * (unsigned)p.n_groups + g;
         const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;         // (as in k_w4_held)
         s_raw[i] = buffer_read2(view, at * 2u | behind);
@@ -625,62 +628,79 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
     // for each product by itself.
     auto unit = [&](int buffer, int j, auto meanwhile) CORAL_INLINE {
         if constexpr (FINE) {
-            uint4 x[T];
-            unsigned code[R], word[R];
-            auto fetch = [&](int s, uint4 (&to)[T], unsigned (&c)[R], unsigned (&w)[R]) CORAL_INLINE {
+            // a slot's EACH products one after the other, and the next slot's operands on their way where the
+            // registers allow it
+            constexpr bool AHEAD = EACH == 1;
+            uint4 x[EACH][T];
+            unsigned code[EACH][R], word[R];
+            auto fetch = [&](int slot, uint4 (&to)[EACH][T], unsigned (&c)[EACH][R], unsigned (&w)[R]) CORAL_INLINE {
 #pragma unroll
                 for (int a = 0; a < R; ++a) {
-                    c[a] = reinterpret_cast<const unsigned*>(&slices[wave][(a * 16 + r) * CODE_ROW + j * 4 + s])[q];
-                    w[a] = scale_word(a, j * SLOTS + s);
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e)
+                        c[e][a] = reinterpret_cast<const unsigned*>(&slices[wave][(a * 16 + r) * CODE_ROW + j * 4 + slot * EACH + e])[q];
+                    w[a] = scale_word(a, j * SLOTS + slot);
                 }
 #pragma unroll
-                for (int t = 0; t < T; ++t) to[t] = load_vec(&xs[buffer][j][t][s][lane]);
+                for (int e = 0; e < EACH; ++e)
+#pragma unroll
+                    for (int t = 0; t < T; ++t) to[e][t] = load_vec(&xs[buffer][j][t][slot * EACH + e][lane]);
             };
             f32x4_t acc[LATE ? 2 : 1][T];
             float scale[LATE ? 2 : 1] = {};
             fetch(0, x, code, word);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                uint4 x_then[T];
-                unsigned code_then[R], word_then[R];
-                if (s < 3) fetch(s + 1, x_then, code_then, word_then);           // on their way during these products
+            for (int slot = 0; slot < SLOTS; ++slot) {
+                uint4 x_then[EACH][T];
+                unsigned code_then[EACH][R], word_then[R];
+                if (AHEAD && slot + 1 < SLOTS) fetch(slot + 1, x_then, code_then, word_then);
                 f32x4_t offset[T];
 #pragma unroll
-                for (int t = 0; t < T; ++t) offset[t] = INT ? mfma_tile<DT>(x[t], minus, zero4) : zero4;
-                uint4 op = w4_operand<DT, KIND>(code[0]);
+                for (int t = 0; t < T; ++t) {
+                    offset[t] = zero4;
+#pragma unroll
+                    for (int e = 0; e < EACH; ++e)
+                        if constexpr (INT) offset[t] = mfma_tile<DT>(x[e][t], minus, offset[t]);
+                }
+                uint4 op = w4_operand<DT, KIND>(code[0][0]);
 #pragma unroll
                 for (int a = 0; a < R; ++a) {
-                    const int now = LATE ? (s * R + a) & 1 : 0;
+                    const int now = LATE ? (slot * R + a) & 1 : 0;
                     start(word[a], offset, acc[now]);
                     scale[now] = scale_of(word[a]);
-                    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int t = 0; t < T; ++t) acc[now][t] = mfma_tile<DT>(x[t], op, acc[now][t]);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (LATE && s + a > 0) {
+                    for (int e = 0; e < EACH; ++e) {
+                        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                        for (int t = 0; t < T; ++t) add(a > 0 ? a - 1 : R - 1, t, scale[LATE ? now ^ 1 : 0], acc[LATE ? now ^ 1 : 0][t]);
+                        for (int t = 0; t < T; ++t) acc[now][t] = mfma_tile<DT>(x[e][t], op, acc[now][t]);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (LATE && e == 0 && slot + a > 0) {
+#pragma unroll
+                            for (int t = 0; t < T; ++t) add(a > 0 ? a - 1 : R - 1, t, scale[LATE ? now ^ 1 : 0], acc[LATE ? now ^ 1 : 0][t]);
+                        }
+                        if (e + 1 < EACH) op = w4_operand<DT, KIND>(code[e + 1 < EACH ? e + 1 : 0][a]);
+                        else if (a + 1 < R) op = w4_operand<DT, KIND>(code[0][a + 1]);
+                        meanwhile((slot * R + a) * EACH + e);
                     }
-                    if (a + 1 < R) op = w4_operand<DT, KIND>(code[a + 1]);
-                    meanwhile(s * R + a);
                     if constexpr (!LATE) {
 #pragma unroll
                         for (int t = 0; t < T; ++t) add(a, t, scale[now], acc[now][t]);
                     }
                 }
-                if (s < 3) {
+                if (!AHEAD && slot + 1 < SLOTS) fetch(slot + 1, x, code, word);
+                if (AHEAD && slot + 1 < SLOTS) {
 #pragma unroll
-                    for (int t = 0; t < T; ++t) x[t] = x_then[t];
+                    for (int t = 0; t < T; ++t) x[0][t] = x_then[0][t];
 #pragma unroll
                     for (int a = 0; a < R; ++a) {
-                        code[a] = code_then[a];
+                        code[0][a] = code_then[0][a];
                         word[a] = word_then[a];
                     }
                 }
             }
             if constexpr (LATE) {
 #pragma unroll
-                for (int t = 0; t < T; ++t) add(R - 1, t, scale[(4 * R - 1) & 1], acc[(4 * R - 1) & 1][t]);
+                for (int t = 0; t < T; ++t) add(R - 1, t, scale[(SLOTS * R - 1) & 1], acc[(SLOTS * R - 1) & 1][t]);
             }
         } else {
             uint4 x[T][4];

@@ -91,17 +91,17 @@ extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const 
     p.per_group_inv = (unsigned)((((uint64_t)1 << 32) + p.per_group - 1) / p.per_group);
     const int kind = code == CORAL_W4_E2M1 ? kW4E2M1 : zeros ? kW4Zero : kW4Sym;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    const bool fine = group < kW4UnitCols;
+    const int slots = group < kW4UnitCols ? kW4UnitCols / group : 1;
     if (const int r = plan_rows(p, dt)) {
-        const void* rows = dt == CORAL_BF16 ? coral_w4_rows_bf16(kind, fine, r) : coral_w4_rows_f16(kind, fine, r);
+        const void* rows = dt == CORAL_BF16 ? coral_w4_rows_bf16(kind, slots, r) : coral_w4_rows_f16(kind, slots, r);
         const int wg_rows = kW4Held * 16 * r;
         hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(rows)), dim3((N - 1) / wg_rows + 1), dim3(kW4Block), 0, stream, p);
         return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
     }
     const W4Plan plan = plan_held(p, dt);
-    const void* held = dt == CORAL_F32    ? coral_w4_held_f32(kind, fine, plan.t, plan.nb, plan.passes)
-                       : dt == CORAL_BF16 ? coral_w4_held_bf16(kind, fine, plan.t, plan.nb, plan.passes)
-                                          : coral_w4_held_f16(kind, fine, plan.t, plan.nb, plan.passes);
+    const void* held = dt == CORAL_F32    ? coral_w4_held_f32(kind, slots, plan.t, plan.nb, plan.passes)
+                       : dt == CORAL_BF16 ? coral_w4_held_bf16(kind, slots, plan.t, plan.nb, plan.passes)
+                                          : coral_w4_held_f16(kind, slots, plan.t, plan.nb, plan.passes);
     // as many workgroups as stay resident: their registers allow four, two or one a compute unit
     const int regs = w4_held_regs(dt == CORAL_F32 ? kF32 : kBF16, plan.t, plan.nb);
     const int tiles = (N - 1) / 16 + 1, most = 256 * (regs <= 2 ? 4 : regs <= 4 ? 2 : 1);
