@@ -14,21 +14,17 @@ __attribute__((visibility("hidden"))) const void* coral_w4_held_bf16(int kind, i
 __attribute__((visibility("hidden"))) const void* coral_w4_held_f16(int kind, int slots, int t, int nb, bool passes);
 __attribute__((visibility("hidden"))) const void* coral_w4_held_f32(int kind, int slots, int t, int nb, bool passes);
 
-// k_w4_rows for r tiles of 16 rows a wave.
-__attribute__((visibility("hidden"))) const void* coral_w4_rows_bf16(int kind, int slots, int r);
-__attribute__((visibility("hidden"))) const void* coral_w4_rows_f16(int kind, int slots, int r);
+// k_w4_rows.
+__attribute__((visibility("hidden"))) const void* coral_w4_rows_bf16(int kind, int slots);
+__attribute__((visibility("hidden"))) const void* coral_w4_rows_f16(int kind, int slots);
 
 namespace {
 
-template <int DT, int KIND, int SLOTS>
-w4_fn w4_pick_rows(int r) {
-    return r == 2 ? k_w4_rows<DT, KIND, SLOTS, 2> : r == 3 ? k_w4_rows<DT, KIND, SLOTS, 3> : k_w4_rows<DT, KIND, SLOTS, 4>;
-}
 template <int DT>
-const void* w4_rows(int kind, int slots, int r) {
+const void* w4_rows(int kind, int slots) {
     const auto pick = [&](auto k) {
         constexpr int KIND = decltype(k)::value;
-        return slots == 4 ? w4_pick_rows<DT, KIND, 4>(r) : slots == 2 ? w4_pick_rows<DT, KIND, 2>(r) : w4_pick_rows<DT, KIND, 1>(r);
+        return slots == 4 ? k_w4_rows<DT, KIND, 4> : slots == 2 ? k_w4_rows<DT, KIND, 2> : k_w4_rows<DT, KIND, 1>;
     };
     return reinterpret_cast<const void*>(kind == kW4E2M1 ? pick(std::integral_constant<int, kW4E2M1>())
                                          : kind == kW4Sym ? pick(std::integral_constant<int, kW4Sym>()) : pick(std::integral_constant<int, kW4Zero>()));
@@ -36,29 +32,22 @@ const void* w4_rows(int kind, int slots, int r) {
 
 template <int DT, int KIND, int SLOTS>
 w4_fn w4_pick_held(int t, int nb, bool passes) {
-    constexpr bool k16 = DT != kF32;             // fp32 activations take twice the registers
-    if (passes) {                                // as many units as the registers hold
-        constexpr int NB = k16 ? 8 : 4;
-        return t == 1 ? k_w4_held<DT, KIND, SLOTS, 1, NB, true> : t == 2 ? k_w4_held<DT, KIND, SLOTS, 2, NB / 2, true> : k_w4_held<DT, KIND, SLOTS, 4, NB / 4, true>;
-    }
-    switch (t * 16 + nb) {
-        case 17: return k_w4_held<DT, KIND, SLOTS, 1, 1>;
-        case 18: return k_w4_held<DT, KIND, SLOTS, 1, 2>;
-        case 19: return k_w4_held<DT, KIND, SLOTS, 1, 3>;
-        case 20: return k_w4_held<DT, KIND, SLOTS, 1, 4>;
-        case 33: return k_w4_held<DT, KIND, SLOTS, 2, 1>;
-        case 34: return k_w4_held<DT, KIND, SLOTS, 2, 2>;
-        case 65: return k_w4_held<DT, KIND, SLOTS, 4, 1>;
-    }
-    if constexpr (k16) {
-        switch (t * 16 + nb) {
-            case 22: return k_w4_held<DT, KIND, SLOTS, 1, 6>;
-            case 24: return k_w4_held<DT, KIND, SLOTS, 1, 8>;
-            case 36: return k_w4_held<DT, KIND, SLOTS, 2, 4>;
-            case 66: return k_w4_held<DT, KIND, SLOTS, 4, 2>;
+    if constexpr (DT == kF32) {                  // activations take twice the registers, and 16 tokens at a time
+        if (passes) return k_w4_held<DT, KIND, SLOTS, 1, 4, true>;
+        return nb == 1 ? k_w4_held<DT, KIND, SLOTS, 1, 1> : nb == 2 ? k_w4_held<DT, KIND, SLOTS, 1, 2>
+               : nb == 3 ? k_w4_held<DT, KIND, SLOTS, 1, 3> : k_w4_held<DT, KIND, SLOTS, 1, 4>;
+    } else {
+        if (passes) return t == 1 ? k_w4_held<DT, KIND, SLOTS, 1, 8, true> : k_w4_held<DT, KIND, SLOTS, 2, 4, true>;
+        if (t == 2) return nb == 1 ? k_w4_held<DT, KIND, SLOTS, 2, 1> : nb == 2 ? k_w4_held<DT, KIND, SLOTS, 2, 2> : k_w4_held<DT, KIND, SLOTS, 2, 4>;
+        switch (nb) {
+            case 1: return k_w4_held<DT, KIND, SLOTS, 1, 1>;
+            case 2: return k_w4_held<DT, KIND, SLOTS, 1, 2>;
+            case 3: return k_w4_held<DT, KIND, SLOTS, 1, 3>;
+            case 4: return k_w4_held<DT, KIND, SLOTS, 1, 4>;
+            case 6: return k_w4_held<DT, KIND, SLOTS, 1, 6>;
+            default: return k_w4_held<DT, KIND, SLOTS, 1, 8>;
         }
     }
-    return nullptr;
 }
 
 template <int DT>

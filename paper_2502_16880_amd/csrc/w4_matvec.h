@@ -200,6 +200,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane & 15, q = lane >> 4;
+    const int token0 = blockIdx.y * (T * 16), tokens = p.M - token0 < T * 16 ? p.M - token0 : T * 16;
     const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, passes = PASSES ? (p.K + PASS_COLS - 1) / PASS_COLS : 1;
     const int each = tiles / gridDim.x, more_of = tiles % gridDim.x, wg = blockIdx.x;
     const int first = wg * each + (wg < more_of ? wg : more_of), end = first + each + (wg < more_of ? 1 : 0);
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         store_vec(&slices[wave][e / CHUNKS * CODE_ROW + e % CHUNKS], w[j]);
     };
     uint4 x[T][NB][4][XV];
-    const Buffer x_view = buffer_view(p.x, 0, (size_t)p.M * p.K * W);
+    const Buffer x_view = buffer_view(p.x, (size_t)token0 * p.K * W, (size_t)p.M * p.K * W);
     // 16-bit activations: in the order of memory first, lane 16 a + c the eight columns c of a unit of
     // token 4 i + a in register i (the products' own layout, 64 bytes of 16 tokens a load, made the first
     // tile of 32 tokens wait for several us)
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         __syncthreads();
         int o = threadIdx.x;
         asm volatile("" : "+v"(o));                       // (what follows from it is not kept through the products)
-        for (; o < p.M * 16; o += kW4Block) {
+        for (; o < tokens * 16; o += kW4Block) {
             float sum = 0.f;
 #pragma unroll
             for (int v = 0; v < kW4Held; ++v) sum += sums[parity][v][o];
@@ -481,7 +482,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                 }
             }
             const int n = tile * 16 + o % 16;
-            if (n < p.N) w4_store<DT>(p, o / 16, n, sum);
+            if (n < p.N) w4_store<DT>(p, token0 + o / 16, n, sum);
         }
     };
     int parity = 0;
@@ -504,18 +505,19 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 }
 
 // ---------------------------------------------------------------- activations shared in LDS
-// Many tokens and many rows, 16-bit activations: a wave takes 16 R weight rows for itself, the columns from
-// first to last, and 16 T tokens.  The activations of a unit of 128 columns lie in LDS, in the layout
+// Many tokens and many rows, 16-bit activations: a wave takes four tiles of 16 weight rows for itself, the
+// columns from first to last, and all tokens.  The activations of a unit of 128 columns lie in LDS, in the layout
 // of the products, for all eight waves; the next unit's are on their way to the other buffer.  So a
-// unit's activations are read from LDS once for R tiles of rows, the sums stay in registers, and no
+// unit's activations are read from LDS once for four tiles of rows, the sums stay in registers, and no
 // wave waits for another's.  The codes come two units at a time, 128 bytes of eight rows a load, and are
 // exchanged through a slice of LDS of the wave's own, as are the scales.
-template <int DT, int KIND, int SLOTS, int R>
+constexpr int kW4RowTiles = 4, kW4RowsRows = kW4Held * kW4RowTiles * 16;      // of a wave; rows of a workgroup
+template <int DT, int KIND, int SLOTS>
 __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
     static_assert(DT != kF32, "");
     constexpr bool INT = KIND != kW4E2M1, ZERO = KIND == kW4Zero, LATE = !INT;
     constexpr bool FINE = SLOTS > 1;
-    constexpr int T = kMaxM / 16, ROWS = 16 * R, EACH = 4 / SLOTS;
+    constexpr int T = kMaxM / 16, R = kW4RowTiles, ROWS = 16 * R, EACH = 4 / SLOTS;
     constexpr int STAGE_SLOTS = 2 * SLOTS, ENTRIES = ROWS * STAGE_SLOTS, SL = (ENTRIES + kWave - 1) / kWave, STRIDE = STAGE_SLOTS + 1;
     constexpr int CODE_ROW = 9, XL = T * 256 / kW4Block;
     static_assert(XL * kW4Block == T * 256, "");

@@ -13,35 +13,29 @@ struct W4Plan {
     bool passes;
 };
 
-// Registers hold eight units of 128 columns a wave for 16 tokens, four for 32, two for 64; half as many
-// of fp32 activations.  More columns are taken in passes.
+// More than 16 tokens are taken 32 at a time (a workgroup for each 32), fp32 activations 16 at a time: all 64
+// at once need fewer reads of the codes and four times the activations a workgroup.  Measured with 64
+// tokens, bf16 (us), 64, 32 and 16 at a time: 4096 x 4096 18, 11, 12; 16384 x 4096 30, 23, 28; 50257 x
+// 4096 62, 60, 73; 4096 x 14336 48, 34, 33; fp32: 4096 x 4096 69, 46, 33; 32000 x 4096 187, 164, 152.
+// Registers hold eight units of 128 columns a wave for 16 tokens, four for 32; four of fp32 activations.
+// More columns are taken in passes.
 W4Plan plan_held(const W4Params& p, coral_dtype dt) {
     const int units = (p.K + kW4UnitCols - 1) / kW4UnitCols;
-    const int t = p.M <= 16 ? 1 : p.M <= 32 ? 2 : 4, most = (dt == CORAL_F32 ? 4 : 8) / t;
+    const int t = p.M <= 16 || dt == CORAL_F32 ? 1 : 2, most = dt == CORAL_F32 ? 4 : 8 / t;
     int nb = (units + kW4Held - 1) / kW4Held;
     if (nb > most) return {t, most, true};
     nb = nb == 5 ? 6 : nb == 7 ? 8 : t > 1 && nb == 3 ? 4 : nb;
     return {t, nb, false};
 }
 
-// k_w4_rows' tiles of 16 rows a wave, or 0 where k_w4_held is taken: for up to 32 tokens (32 tokens, 128256 rows
-// of 4096 columns: 75 us held, 82 us shared) and where a round of workgroups would not be full.  A round, one
-// workgroup of 128 r rows for each of 256 compute units, takes about as long as 870 (r + 2) tiles held.
-// Measured with 64 tokens, bf16 (us), held and shared with 2, 3 and 4 tiles: 50257 x 4096 61, 65, 79, 97;
-// 65536 x 4096 69, 67, 77, 92; 100000 x 4096 111, 115, 148, 101; 152064 x 3584 168, 155, 144, 167.
-int plan_rows(const W4Params& p, coral_dtype dt) {
-    if (dt == CORAL_F32 || p.M <= 32) return 0;
-    const int tiles = (p.N - 1) / 16 + 1;
-    int best = 0;
-    int64_t least = tiles;
-    for (int r = 2; r <= 4; ++r) {
-        const int64_t rounds = (tiles - 1) / (256 * kW4Held * r) + 1, cost = rounds * (r + 2) * 870;
-        if (cost < least) {
-            best = r;
-            least = cost;
-        }
-    }
-    return best;
+// Whether k_w4_rows is taken: for more than 32 tokens, where the rows fill its rounds of workgroups (one of 512
+// rows for each of 256 compute units), which take as long as 6600 tiles of k_w4_held.  Measured with 48 and
+// 64 tokens, bf16 (us), held and shared: 128256 x 4096 127, 103 and 126, 109 (e2m1, groups of 32: 138, 119);
+// 100000 x 4096, 64 tokens, 100 both; 65536 x 4096 72, 92; 152064 x 3584 143, 167.  32 tokens, 128256 x
+// 4096 75, 82.
+bool plan_rows(const W4Params& p, coral_dtype dt) {
+    const int tiles = (p.N - 1) / 16 + 1, rounds = (p.N - 1) / (256 * kW4RowsRows) + 1;
+    return dt != CORAL_F32 && p.M > 32 && (int64_t)rounds * 6600 < tiles;
 }
 
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
@@ -92,10 +86,9 @@ extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const 
     const int kind = code == CORAL_W4_E2M1 ? kW4E2M1 : zeros ? kW4Zero : kW4Sym;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const int slots = group < kW4UnitCols ? kW4UnitCols / group : 1;
-    if (const int r = plan_rows(p, dt)) {
-        const void* rows = dt == CORAL_BF16 ? coral_w4_rows_bf16(kind, slots, r) : coral_w4_rows_f16(kind, slots, r);
-        const int wg_rows = kW4Held * 16 * r;
-        hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(rows)), dim3((N - 1) / wg_rows + 1), dim3(kW4Block), 0, stream, p);
+    if (plan_rows(p, dt)) {
+        const void* rows = dt == CORAL_BF16 ? coral_w4_rows_bf16(kind, slots) : coral_w4_rows_f16(kind, slots);
+        hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(rows)), dim3((N - 1) / kW4RowsRows + 1), dim3(kW4Block), 0, stream, p);
         return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
     }
     const W4Plan plan = plan_held(p, dt);
@@ -104,7 +97,7 @@ extern "C" coral_status coral_matvec_w4(const void* x, const void* codes, const 
                                           : coral_w4_held_f16(kind, slots, plan.t, plan.nb, plan.passes);
     // as many workgroups as stay resident: their registers allow four, two or one a compute unit
     const int regs = w4_held_regs(dt == CORAL_F32 ? kF32 : kBF16, plan.t, plan.nb);
-    const int tiles = (N - 1) / 16 + 1, most = 256 * (regs <= 2 ? 4 : regs <= 4 ? 2 : 1);
-    hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(held)), dim3(tiles < most ? tiles : most), dim3(kW4Block), 0, stream, p);
+    const int tiles = (N - 1) / 16 + 1, groups = (M - 1) / (16 * plan.t) + 1, most = 256 * (regs <= 2 ? 4 : regs <= 4 ? 2 : 1) / groups;
+    hipLaunchKernelGGL(reinterpret_cast<w4_fn>(const_cast<void*>(held)), dim3(tiles < most ? tiles : most, groups), dim3(kW4Block), 0, stream, p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }

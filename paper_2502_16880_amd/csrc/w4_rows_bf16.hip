@@ -2,4 +2,4 @@
 #include "coral_lmhead.h"
 #include "w4_kernels.h"
 
-const void* coral_w4_rows_bf16(int kind, int slots, int r) { return w4_rows<kBF16>(kind, slots, r); }
+const void* coral_w4_rows_bf16(int kind, int slots) { return w4_rows<kBF16>(kind, slots); }

@@ -2,4 +2,4 @@
 #include "coral_lmhead.h"
 #include "w4_kernels.h"
 
-const void* coral_w4_rows_f16(int kind, int slots, int r) { return w4_rows<kF16>(kind, slots, r); }
+const void* coral_w4_rows_f16(int kind, int slots) { return w4_rows<kF16>(kind, slots); }

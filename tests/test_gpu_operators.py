@@ -98,8 +98,9 @@ def test_matvec_w4(coral, dtype, kind, zeros, M, N, K, group):
     assert torch.equal(c.run(coral), y)                            # the same bits every time
 
 
-# many tokens and many rows: two, three and four tiles of rows a wave, the last ones not full
-MANY = [(64, 55700, 136, 32), (33, 139300, 136, 64), (50, 83600, 392, 128), (63, 83601, 8, 32), (64, 60001, 1032, 256), (40, 90000, 256, 64)]
+# many tokens and many rows, one and two rounds of workgroups, the last ones not full
+MANY = [(64, 55700, 136, 32), (33, 139300, 136, 64), (50, 83600, 392, 128), (63, 83601, 8, 32), (64, 60001, 1032, 256), (40, 90000, 256, 64),
+        (64, 110001, 136, 32), (33, 131072, 264, 64), (50, 106000, 392, 128), (63, 120017, 8, 32), (64, 215000, 40, 256), (49, 105700, 1032, 64)]
 
 
 @pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
@@ -121,7 +122,7 @@ def test_matvec_w4_many_rows(coral, dtype, kind, zeros, M, N, K, group):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_matvec_w4_many_rows_epilogue(coral, dtype):
-    M, N, K = 45, 84000, 200
+    M, N, K = 45, 108000, 200
     c = Product(dtype, M, N, K, 64, bias=True, residual=True, seed=6)
     y, untouched = guarded((M, N), TORCH[dtype])
     c.run(coral, "silu", out=y)
@@ -131,7 +132,7 @@ def test_matvec_w4_many_rows_epilogue(coral, dtype):
     assert torch.equal(c.run(coral, "silu", residual=same, out=same), y)
 
 
-@pytest.mark.parametrize("N", [33, 83600])
+@pytest.mark.parametrize("N", [33, 83600, 110000])
 @pytest.mark.parametrize("K,group", [(40, 32), (200, 64), (648, 128)])
 @pytest.mark.parametrize("M", [3, 50])
 def test_matvec_w4_infinite_scales_of_a_rows_last_group(coral, M, N, K, group):
