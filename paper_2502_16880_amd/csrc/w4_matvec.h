@@ -146,7 +146,14 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // are loaded again, with the next tile's codes, as soon as they are in LDS: the wave always has about
 // NB KB on the way.  The tile's scales and zero points, which lie scattered for a lane, are loaded row
 // by row by the whole workgroup one tile ahead and kept in LDS as fp32.  The waves' sums meet in LDS
-// once a tile.
+// once a tile.  More tokens than T tiles are other workgroups' (the grid's second dimension).
+//
+// Measured (copy 4.9 TB/s, reading alone 6.5 TB/s): bf16, one token, 128256 x 4096, groups of 128: 50 us, 5.4
+// TB/s, bound by memory; e2m1 in groups of 32: 50 us, 5.9 TB/s.  fp16, 16 tokens, 152064 x 3584, groups of 64
+// with zero points: 65 to 73 us, 4.1 TB/s: a product of 32 columns takes a dozen vector instructions beside
+// it (codes to operands, zero point, scale), which are about as long as the reading.  fp32, 7 tokens, 50257 x
+// 2568, groups of 32: 33 us, 2.6 TB/s: three products for one, and one workgroup a compute unit for its
+// registers.  4096 x 4096, one token: 6.1 us, of which the launch is 2.5 and one trip to memory 2.
 //
 // Lane 16 q + r takes the 16 bytes of row r that hold columns 32 q to 32 q + 31 of a unit, and product
 // s their dword s: columns 32 q + 8 s ... + 7 of the four chunks q, which is a group or part of one
@@ -510,7 +517,13 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 // of the products, for all eight waves; the next unit's are on their way to the other buffer.  So a
 // unit's activations are read from LDS once for four tiles of rows, the sums stay in registers, and no
 // wave waits for another's.  The codes come two units at a time, 128 bytes of eight rows a load, and are
-// exchanged through a slice of LDS of the wave's own, as are the scales.
+// exchanged through a slice of LDS of the wave's own, as are the scales.  With slots finer than a unit a
+// stage's loads are spread over its products (all at once they keep the waves waiting: 64 tokens, e2m1, groups
+// of 32, 126 against 118 us); with one slot the registers do not allow it.
+// Measured: bf16, 64 tokens, 128256 x 4096: 109 us with integers in groups of 128, 119 us with e2m1 in groups
+// of 32, 620 and 565 TFLOP/s.  The products alone take 33 us.  Of a stage's 11800 cycles 5100 are products, 3000
+// the issue of its loads, 1200 the barrier, the rest reads of LDS and vector instructions that the two waves
+// of a SIMD, which its registers allow, do not hide from each other.
 constexpr int kW4RowTiles = 4, kW4RowsRows = kW4Held * kW4RowTiles * 16;      // of a wave; rows of a workgroup
 template <int DT, int KIND, int SLOTS>
 __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
