@@ -36,11 +36,13 @@ constexpr int kW4Op = DT == kF16 ? kF16 : kBF16; // operand type of the products
 template <int DT>
 constexpr int kW4Parts = DT == kF32 ? 3 : 1;     // operands that an activation is split into
 
-// (w & mask) | bits in one instruction (of two constants the compiler makes two).
+// (w & mask) | bits.  Of two constants the compiler makes two instructions; with values that it does not know
+// it takes v_and_or_b32.  The instruction itself is not written in asm: the compiler does not see there that
+// what it writes is a product's operand, or was the last one's, and leaves out the waits between them.
 __device__ __forceinline__ unsigned w4_and_or(unsigned w, unsigned mask, unsigned bits) {
-    unsigned o;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(o) : "v"(w), "s"(mask), "v"(bits));
-    return o;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(bits));
+    return (w & mask) | bits;
 }
 
 // Eight codes of a dword as 16-bit operands.  Integers: 16 + code, in the order 0 4 1 5 2 6 3 7.

@@ -98,6 +98,18 @@ def test_matvec_w4(coral, dtype, kind, zeros, M, N, K, group):
     assert torch.equal(c.run(coral), y)                            # the same bits every time
 
 
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K", [(4, 4096), (20, 2048), (7, 1000), (33, 4096)])
+def test_matvec_w4_many_tiles_a_workgroup(coral, dtype, kind, zeros, group, M, K):
+    N = 20011
+    c = Product(dtype, M, N, K, group, kind, zeros, seed=8)
+    runs = [c.run(coral) for _ in range(4)]
+    assert all(torch.equal(y, runs[0]) for y in runs) and bool(torch.isfinite(runs[0]).all())
+    c.check(runs[0], rows=np.unique(np.r_[0:200, N - 200:N, 0:N:53]))
+
+
 # many tokens and many rows, one and two rounds of workgroups, the last ones not full
 MANY = [(64, 55700, 136, 32), (33, 139300, 136, 64), (50, 83600, 392, 128), (63, 83601, 8, 32), (64, 60001, 1032, 256), (40, 90000, 256, 64),
         (64, 110001, 136, 32), (33, 131072, 264, 64), (50, 106000, 392, 128), (63, 120017, 8, 32), (64, 215000, 40, 256), (49, 105700, 1032, 64)]
