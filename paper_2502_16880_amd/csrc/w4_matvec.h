@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                 for (int t = 0; t < T; ++t)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) y[t][v] = fmaf(scale, acc[t][v], y[t][v]);
-                if constexpr (FINE) __builtin_amdgcn_sched_barrier(0);
+                if constexpr (FINE && T > 1) __builtin_amdgcn_sched_barrier(0);
             }
             // (summed here: left to itself the compiler keeps every product's result until the sums are stored)
 #pragma unroll
