@@ -197,6 +197,18 @@ def test_matvec_w4_tokens_are_independent(coral, bad, M):
     assert torch.equal(z[keep], y[keep])
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("kind,zeros,group", [("int", True, 32), ("int", False, 64), ("int", True, 128), ("e2m1", False, 32), ("e2m1", False, 128)])
+def test_matvec_w4_tokens_are_independent_with_many_rows(coral, bad, kind, zeros, group):
+    M = 50
+    c = Product("bf16", M, 110000, 264, group, kind, zeros, seed=9)
+    y = c.run(coral)
+    c.x[M // 2, 100] = bad
+    z = c.run(coral)
+    keep = [m for m in range(M) if m != M // 2]
+    assert torch.equal(z[keep], y[keep])
+
+
 def test_matvec_w4_zero_scales_and_extreme_values(coral):
     c = Product("f32", 3, 40, 256, 32, seed=4)
     c.scales[::2] = 0.0
