@@ -170,17 +170,22 @@ __device__ __forceinline__ void slice_under_rules(const RuleParams& p, int m, in
 #pragma unroll
         for (int a = 0; a < A; ++a) t[a] = buffer_read16(tokens, (unsigned)(i + (a * kRuleThreads + tid) * 4) * 4u);
     };
-    auto count = [&](bool is_output, int n, int i, const uint4 (&t)[A]) {
+    // the slice's ids of the row: first_id ... + n_ids, from word first_word on
+    const unsigned first_id = (unsigned)(first > lead ? first - lead : 0), first_word = (unsigned)(first > lead ? 0 : lead - first);
+    const unsigned in_slice = (unsigned)kRuleSlice - first_word, in_row = first_id < (unsigned)p.V ? (unsigned)p.V - first_id : 0u;
+    const unsigned n_ids = in_slice < in_row ? in_slice : in_row;
+    unsigned* const row_words = words + first_word;
+    auto count = [&](bool is_output, bool whole, int n, int i, const uint4 (&t)[A]) CORAL_INLINE {
 #pragma unroll
         for (int a = 0; a < A; ++a) {
             const unsigned id[4] = {t[a].x, t[a].y, t[a].z, t[a].w};
             const int have = n - (i + (a * kRuleThreads + tid) * 4);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const unsigned at = id[e] + (unsigned)(lead - first);
-                if (e < have && at < (unsigned)kRuleSlice && id[e] < (unsigned)p.V) {
-                    if (is_output) atomicAdd(words + at, 1u);
-                    else atomicOr(words + at, kInPrompt);
+                const unsigned at = id[e] - first_id;
+                if (at < n_ids && (whole || e < have)) {
+                    if (is_output) atomicAdd(row_words + at, 1u);
+                    else atomicOr(row_words + at, kInPrompt);
                 }
             }
         }
@@ -203,21 +208,23 @@ __device__ __forceinline__ void slice_under_rules(const RuleParams& p, int m, in
         __syncthreads();
     }
     if (counts) {
-        count(false, n_prompt, 0, in_prompt);
-        count(true, n_output, 0, in_output);
+        count(false, false, n_prompt, 0, in_prompt);
+        count(true, false, n_output, 0, in_output);
         if (TRIP < n_prompt) {                               // a long prompt: the next tokens on their way
             fetch(prompts, TRIP, in_prompt);
-            for (int i = TRIP; i < n_prompt; i += TRIP) {
+            int i = TRIP;
+            for (; i + TRIP <= n_prompt; i += TRIP) {
                 uint4 next[A];
                 fetch(prompts, i + TRIP, next);              // (behind the range there is none)
-                count(false, n_prompt, i, in_prompt);
+                count(false, true, n_prompt, i, in_prompt);
 #pragma unroll
                 for (int a = 0; a < A; ++a) in_prompt[a] = next[a];
             }
+            count(false, false, n_prompt, i, in_prompt);
         }
         for (int i = TRIP; i < n_output; i += TRIP) {
             fetch(outputs, i, in_output);
-            count(true, n_output, i, in_output);
+            count(true, false, n_output, i, in_output);
         }
         __syncthreads();
     }
