@@ -2,4 +2,4 @@
 #include "coral_lmhead.h"
 #include "w4_kernels.h"
 
-const void* coral_w4_held_f32(int kind, int slots, int t, int nb, bool passes) { return w4_held<kF32>(kind, slots, t, nb, passes); }
+const void* coral_w4_held_f32(int kind, int slots, int t, int nb, bool passes, bool spread) { return w4_held<kF32>(kind, slots, t, nb, passes, spread); }

@@ -33,8 +33,6 @@ constexpr int kW4UnitCols = 128;                 // columns of a unit: four prod
 
 template <int DT>
 constexpr int kW4Op = DT == kF16 ? kF16 : kBF16; // operand type of the products
-template <int DT>
-constexpr int kW4Parts = DT == kF32 ? 3 : 1;     // operands that an activation is split into
 
 // (w & mask) | bits.  Of two constants the compiler makes two instructions; with values that it does not know
 // it takes v_and_or_b32.  The instruction itself is not written in asm: the compiler does not see there that
@@ -89,26 +87,19 @@ __device__ __forceinline__ uint4 w4_order(uint4 v) {
     return o;
 }
 
-// Eight fp32 values as three bf16 values each, x = hi + mid + lo exactly: the significand's 24 bits
-// are cut off in eights.
-__device__ __forceinline__ void w4_split(const float (&f)[8], uint4 (&part)[3]) {
-    unsigned b[3][8];
+// Part c of eight fp32 values, x = hi + mid + lo exactly in bf16: the significand's 24 bits are cut off in
+// eights.
+__device__ __forceinline__ uint4 w4_part(uint4 x, uint4 y, int c) {
+    const unsigned f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    unsigned b[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        float r = f[j];
-#pragma unroll
-        for (int c = 0; c < 3; ++c) {
-            b[c][j] = __float_as_uint(r) & 0xffff0000u;
-            r -= __uint_as_float(b[c][j]);
-        }
+        const float v = __uint_as_float(f[j]), hi = __uint_as_float(f[j] & 0xffff0000u), rest = v - hi;
+        const float mid = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+        b[j] = c == 0 ? f[j] : __float_as_uint(c == 1 ? rest : rest - mid);      // (their upper halves)
     }
-#pragma unroll
-    for (int c = 0; c < 3; ++c) {
-        part[c].x = __builtin_amdgcn_perm(b[c][1], b[c][0], 0x07060302u);
-        part[c].y = __builtin_amdgcn_perm(b[c][3], b[c][2], 0x07060302u);
-        part[c].z = __builtin_amdgcn_perm(b[c][5], b[c][4], 0x07060302u);
-        part[c].w = __builtin_amdgcn_perm(b[c][7], b[c][6], 0x07060302u);
-    }
+    return make_uint4(__builtin_amdgcn_perm(b[1], b[0], 0x07060302u), __builtin_amdgcn_perm(b[3], b[2], 0x07060302u),
+                      __builtin_amdgcn_perm(b[5], b[4], 0x07060302u), __builtin_amdgcn_perm(b[7], b[6], 0x07060302u));
 }
 
 template <int DT>
@@ -148,14 +139,14 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // are loaded again, with the next tile's codes, as soon as they are in LDS: the wave always has about
 // NB KB on the way.  The tile's scales and zero points, which lie scattered for a lane, are loaded row
 // by row by the whole workgroup one tile ahead and kept in LDS as fp32.  The waves' sums meet in LDS
-// once a tile.  More tokens than T tiles are other workgroups' (the grid's second dimension).
+// once a tile.  More tokens than T tiles hold are other workgroups' (the grid's second dimension).
 //
 // Measured (copy 4.9 TB/s, reading alone 6.5 TB/s): bf16, one token, 128256 x 4096, groups of 128: 50 us, 5.4
 // TB/s, bound by memory; e2m1 in groups of 32: 50 us, 5.9 TB/s.  fp16, 16 tokens, 152064 x 3584, groups of 64
 // with zero points: 65 to 73 us, 4.1 TB/s: a product of 32 columns takes a dozen vector instructions beside
-// it (codes to operands, zero point, scale), which are about as long as the reading.  fp32, 7 tokens, 50257 x
-// 2568, groups of 32: 33 us, 2.6 TB/s: three products for one, and one workgroup a compute unit for its
-// registers.  4096 x 4096, one token: 6.1 us, of which the launch is 2.5 and one trip to memory 2.
+// it (codes to operands, zero point, scale), which are about as long as the reading.  fp32, one token, 128256 x
+// 4096: 55 us; 7 tokens, 50257 x 2568, groups of 32: 33 us, 2.6 TB/s: three products for one, and one workgroup
+// a compute unit for its registers.  4096 x 4096, one token: 6.1 us, of which the launch is 2.5 and one trip to memory 2.
 //
 // Lane 16 q + r takes the 16 bytes of row r that hold columns 32 q to 32 q + 31 of a unit, and product
 // s their dword s: columns 32 q + 8 s ... + 7 of the four chunks q, which is a group or part of one
@@ -178,17 +169,20 @@ __device__ __forceinline__ unsigned w4_group_of(const W4Params& p, unsigned unit
 }
 
 // What decides how many workgroups fit a compute unit: the registers that the activations take, in 16s
-// (and room to split fp32 activations).
-constexpr int w4_held_regs(int dt, int t, int nb) { return dt == kF32 ? (t * nb > 1 ? 8 : 4) : t * nb; }
+// (chain: fp32 ones as three products one after the other).
+constexpr int w4_held_regs(bool chain, int t, int nb) { return !chain ? t * nb : nb > 1 ? 8 : 4; }
+// fp32 activations are three rows of the products a token (spread), or, up to three units a wave, three
+// products one after the other.
+constexpr int w4_held_tokens(bool spread, int t) { return spread ? t * 16 / 3 : t * 16; }
 
-// T tiles of 16 tokens, NB units a wave.  PASSES: the columns are more than the waves hold and are taken
+// T tiles of 16 rows of activations, NB units a wave.  PASSES: the columns are more than the waves hold and are taken
 // in passes; the workgroup goes through a block of tiles once a pass, adding the tiles' sums up in
 // LDS, before the next block.  Codes are still read once, activations once a block.
-template <int DT, int KIND, int SLOTS, int T, int NB, bool PASSES = false>
-__global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) void k_w4_held(W4Params p) {
-    // fp32 activations are held as their parts where the registers allow it, else split at every use
-    constexpr bool SPLIT = DT == kF32 && T * NB > 3;
-    constexpr int OP = kW4Op<DT>, PARTS = kW4Parts<DT>, XR = DT == kF32 ? 2 : 1, XV = SPLIT ? 2 : PARTS;
+template <int DT, int KIND, int SLOTS, int T, int NB, bool PASSES = false, bool SPREAD = false>
+__global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB) <= 4 ? 4 : 2) void k_w4_held(W4Params p) {
+    static_assert(DT == kF32 || !SPREAD, "");
+    constexpr bool CHAIN = DT == kF32 && !SPREAD;
+    constexpr int OP = kW4Op<DT>, PARTS = CHAIN ? 3 : 1, ROWS = SPREAD ? 3 : 1, TOKENS = w4_held_tokens(SPREAD, T);
     constexpr bool PAIR = KIND == kW4Zero && DT != kF32;     // scale and zero as two 16-bit values of one word
     constexpr int PER = KIND == kW4Zero && DT == kF32 ? 2 : 1;
     // SL: slots of a row that a thread brings for a tile (the last ones may lie behind the row).
@@ -209,7 +203,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
     const int lane = threadIdx.x & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane & 15, q = lane >> 4;
-    const int token0 = blockIdx.y * (T * 16), tokens = p.M - token0 < T * 16 ? p.M - token0 : T * 16;
+    const int token0 = blockIdx.y * TOKENS, tokens = p.M - token0 < TOKENS ? p.M - token0 : TOKENS;
     const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, passes = PASSES ? (p.K + PASS_COLS - 1) / PASS_COLS : 1;
     const int each = tiles / gridDim.x, more_of = tiles % gridDim.x, wg = blockIdx.x;
     const int first = wg * each + (wg < more_of ? wg : more_of), end = first + each + (wg < more_of ? 1 : 0);
@@ -268,11 +262,11 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         const int e = j * kWave + lane;
         store_vec(&slices[wave][e / CHUNKS * CODE_ROW + e % CHUNKS], w[j]);
     };
-    uint4 x[T][NB][4][XV];
+    uint4 x[T][NB][4][PARTS];
     const Buffer x_view = buffer_view(p.x, (size_t)token0 * p.K * W, (size_t)p.M * p.K * W);
-    // 16-bit activations: in the order of memory first, lane 16 a + c the eight columns c of a unit of
-    // token 4 i + a in register i (the products' own layout, 64 bytes of 16 tokens a load, made the first
-    // tile of 32 tokens wait for several us)
+    // In the order of memory first, lane 16 a + c the eight columns c of a unit of row 4 i + a in register
+    // i (the products' own layout, 64 bytes of 16 rows a load, made the first tile of 32 tokens wait for
+    // several us; three products one after the other keep it).  Spread: row 3 m + c is part c of token m.
     auto load_x = [&](int pass) CORAL_INLINE {
 #pragma unroll
         for (int t = 0; t < T; ++t)
@@ -281,17 +275,29 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
                     const int unit = pass * PASS_COLS + (wave * NB + j) * kW4UnitCols;
-                    const int col = unit + (DT != kF32 ? r * 8 : FINE ? s * 32 + q * 8 : q * 32 + s * 8);
-                    const int token = t * 16 + (DT != kF32 ? 4 * s + q : r);
-                    const unsigned off = col < p.K ? ((unsigned)token * (unsigned)p.K + col) * W : 0xffffffe0u;    // (behind the end)
-#pragma unroll
-                    for (int v = 0; v < XR; ++v) x[t][j][s][v] = buffer_read16(x_view, off + 16u * v);
+                    const int col = unit + (!CHAIN ? r * 8 : FINE ? s * 32 + q * 8 : q * 32 + s * 8);
+                    const int row = t * 16 + (!CHAIN ? 4 * s + q : r), token = row / ROWS;
+                    // (behind the end; the last row of spread ones may be no token's)
+                    const unsigned off = col < p.K && (!SPREAD || token < TOKENS) ? ((unsigned)token * (unsigned)p.K + col) * W : 0xffffffe0u;
+                    const uint4 a = buffer_read16(x_view, off);
+                    if constexpr (DT == kF32) {
+                        const uint4 b = buffer_read16(x_view, off + 16u);
+                        if constexpr (SPREAD) {
+                            x[t][j][s][0] = w4_part(a, b, row - token * 3);
+                            if (s == 3) __builtin_amdgcn_sched_barrier(0);       // (a unit at a time: it takes twice the registers until then)
+                        } else {
+                            x[t][j][s][0] = a;
+                            x[t][j][s][1] = b;
+                        }
+                    } else {
+                        x[t][j][s][0] = a;
+                    }
                 }
     };
-    // ... then lane 16 q + r token r, chunk q and eight columns s in register s (fine groups: chunk s,
-    // eight columns q), through the wave's slice: as many tokens at a time as it holds
+    // ... then lane 16 q + r row r, chunk q and eight columns s in register s (fine groups: chunk s,
+    // eight columns q), through the wave's slice: as many rows at a time as it holds
     constexpr int HALVES = SLICE >= 16 * X_ROW ? 1 : 2, X_MASK = 16 / HALVES - 1;
-    auto exchange = [&](uint4 (&v)[4][XV]) CORAL_INLINE {
+    auto exchange = [&](uint4 (&v)[4][PARTS]) CORAL_INLINE {
         u32x4_t o[4] = {};
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
@@ -312,23 +318,6 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
         for (int s = 0; s < 4; ++s) v[s][0] = make_uint4(o[s].x, o[s].y, o[s].z, o[s].w);
     };
-    auto parts_of = [&](const uint4 (&v)[XV], uint4 (&part)[PARTS], bool split) CORAL_INLINE {
-        if constexpr (DT == kF32) {
-            if (split) {
-                const uint4 a = v[0], b = v[1];
-                const float f[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
-                                    __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
-                w4_split(f, part);
-#pragma unroll
-                for (int c = 0; c < PARTS; ++c) part[c] = w4_order<KIND>(part[c]);
-                return;
-            }
-        }
-        if constexpr (!SPLIT) {
-#pragma unroll
-            for (int c = 0; c < PARTS; ++c) part[c] = v[c];
-        }
-    };
     const f32x4_t zero4 = {0.f, 0.f, 0.f, 0.f};
     // the offset's part of the sums: of -24 x where every zero point is 8, else of -16 x, times 1 + zero / 16
     constexpr unsigned kMinus = KIND == kW4Sym ? (OP == kF16 ? 0xCE00CE00u : 0xC1C0C1C0u) : OP == kF16 ? 0xCC00CC00u : 0xC180C180u;
@@ -338,18 +327,18 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int t = 0; t < T; ++t) {
-                if constexpr (DT != kF32) exchange(x[t][j]);
+                if constexpr (!CHAIN) exchange(x[t][j]);
 #pragma unroll
                 for (int s = 0; s < 4; ++s) {
-                    if constexpr (DT != kF32) x[t][j][s][0] = w4_order<KIND>(x[t][j][s][0]);
-                    if constexpr (DT == kF32 && !SPLIT) {
-                        uint4 part[PARTS];
-                        parts_of(x[t][j][s], part, true);
+                    if constexpr (CHAIN) {
+                        const uint4 a = x[t][j][s][0], b = x[t][j][s][1];
 #pragma unroll
-                        for (int c = 0; c < PARTS; ++c) x[t][j][s][c] = part[c];
+                        for (int c = 0; c < PARTS; ++c) x[t][j][s][c] = w4_part(a, b, c);
                     }
+#pragma unroll
+                    for (int c = 0; c < PARTS; ++c) x[t][j][s][c] = w4_order<KIND>(x[t][j][s][c]);
                 }
-                if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
+                if constexpr (CHAIN) __builtin_amdgcn_sched_barrier(0);
             }
         // (arranged here, not at every use)
 #pragma unroll
@@ -359,7 +348,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
 #pragma unroll
                 for (int s = 0; s < 4; ++s)
 #pragma unroll
-                    for (int v = 0; v < XV; ++v) w4_settle(x[t][j][s][v]);
+                    for (int v = 0; v < PARTS; ++v) w4_settle(x[t][j][s][v]);
         if constexpr (KIND != kW4E2M1) {
 #pragma unroll
             for (int j = 0; j < NB; ++j)
@@ -368,11 +357,9 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                     f32x4_t sum = zero4;
 #pragma unroll
                     for (int s = 0; s < 4; ++s) {
-                        uint4 part[PARTS];
-                        parts_of(x[t][j][s], part, SPLIT);
                         if (s % EACH == 0) sum = zero4;
 #pragma unroll
-                        for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(part[c], minus, sum);
+                        for (int c = PARTS - 1; c >= 0; --c) sum = mfma_tile<OP>(x[t][j][s][c], minus, sum);
                         if (r == 0 && s % EACH == EACH - 1) x_sums[wave][j][s / EACH][t][q] = sum;      // (read by this wave only)
                     }
                     if constexpr (DT == kF32) __builtin_amdgcn_sched_barrier(0);
@@ -395,16 +382,6 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         load_scales(next_tile, next_pass, more);
         const Buffer next_codes = code_view(next_tile, next_pass, more);
         const float* my_scales = scales[parity][r] + wave * (NB * SLOTS * PER);
-        if constexpr (SPLIT) {                               // (or the parts of all activations are kept in registers)
-#pragma unroll
-            for (int t = 0; t < T; ++t)
-#pragma unroll
-                for (int j = 0; j < NB; ++j)
-#pragma unroll
-                    for (int s = 0; s < 4; ++s)
-#pragma unroll
-                        for (int v = 0; v < XV; ++v) w4_settle(x[t][j][s][v]);
-        }
         f32x4_t y[T];
 #pragma unroll
         for (int t = 0; t < T; ++t) y[t] = zero4;
@@ -452,10 +429,8 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
                 const uint4 op = w4_operand<OP, KIND>(s == 0 ? v.x : s == 1 ? v.y : s == 2 ? v.z : v.w);
 #pragma unroll
                 for (int t = 0; t < T; ++t) {
-                    uint4 part[PARTS];
-                    parts_of(x[t][j][s], part, SPLIT);
 #pragma unroll
-                    for (int c = PARTS - 1; c >= 0; --c) acc[t] = mfma_tile<OP>(part[c], op, acc[t]);      // the small parts first
+                    for (int c = PARTS - 1; c >= 0; --c) acc[t] = mfma_tile<OP>(x[t][j][s][c], op, acc[t]);        // the small parts first
                 }
                 if (s % EACH != EACH - 1) continue;
 #pragma unroll
@@ -482,7 +457,9 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT, T, NB) <= 4 ? 4 : 2) voi
         for (; o < tokens * 16; o += kW4Block) {
             float sum = 0.f;
 #pragma unroll
-            for (int v = 0; v < kW4Held; ++v) sum += sums[parity][v][o];
+            for (int c = ROWS - 1; c >= 0; --c)
+#pragma unroll
+                for (int v = 0; v < kW4Held; ++v) sum += sums[parity][v][o / 16 * (ROWS * 16) + c * 16 + o % 16];
             if constexpr (PASSES) {                          // (a place of so_far is one thread's own)
                 if (pass > 0) sum += so_far[in_block][o];
                 if (pass + 1 < passes) {
