@@ -40,7 +40,7 @@ w4_fn w4_pick_held(int t, int nb, bool passes, bool spread) {
                : nb == 3 ? k_w4_held<DT, KIND, SLOTS, 1, 3, false, true> : k_w4_held<DT, KIND, SLOTS, 1, 4, false, true>;
     } else {
         if (passes) return t == 1 ? k_w4_held<DT, KIND, SLOTS, 1, 8, true> : k_w4_held<DT, KIND, SLOTS, 2, 4, true>;
-        if (t == 2) return nb == 1 ? k_w4_held<DT, KIND, SLOTS, 2, 1> : nb == 2 ? k_w4_held<DT, KIND, SLOTS, 2, 2> : k_w4_held<DT, KIND, SLOTS, 2, 4>;
+        if (t == 2) return nb == 1 ? k_w4_held<DT, KIND, SLOTS, 2, 1> : nb == 2 ? k_w4_held<DT, KIND, SLOTS, 2, 2> : nb == 3 ? k_w4_held<DT, KIND, SLOTS, 2, 3> : k_w4_held<DT, KIND, SLOTS, 2, 4>;
         switch (nb) {
             case 1: return k_w4_held<DT, KIND, SLOTS, 1, 1>;
             case 2: return k_w4_held<DT, KIND, SLOTS, 1, 2>;

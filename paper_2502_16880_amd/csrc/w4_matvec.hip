@@ -32,7 +32,7 @@ W4Plan plan_held(const W4Params& p, coral_dtype dt) {
     }
     const int t = p.M <= 16 ? 1 : 2, most = 8 / t;
     if (nb > most) return {t, most, true, false};
-    nb = nb == 5 ? 6 : nb == 7 ? 8 : t > 1 && nb == 3 ? 4 : nb;
+    nb = nb == 5 ? 6 : nb == 7 ? 8 : nb;
     return {t, nb, false, false};
 }
 
