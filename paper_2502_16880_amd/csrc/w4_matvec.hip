@@ -37,13 +37,13 @@ W4Plan plan_held(const W4Params& p, coral_dtype dt) {
 }
 
 // Whether k_w4_rows is taken: for more than 32 tokens, where the rows fill its rounds of workgroups (one of 512
-// rows for each of 256 compute units), which take as long as 6600 tiles of k_w4_held.  Measured with 48 and
-// 64 tokens, bf16 (us), held and shared: 128256 x 4096 127, 103 and 126, 109 (e2m1, groups of 32: 138, 119);
-// 100000 x 4096, 64 tokens, 100 both; 65536 x 4096 72, 92; 152064 x 3584 143, 167.  32 tokens, 128256 x
-// 4096 75, 82.
+// rows for each of 256 compute units), which take as long as 6000 tiles of k_w4_held.  Measured with 64
+// tokens, bf16 (us), held and shared: 128256 rows of 1024 columns 58, 42; 2048 80, 67; 4096 126, 109 (48 tokens 127,
+// 103; e2m1, groups of 32: 138, 119); 8192 245, 208.  100000 x 2048 61, 56; x 4096 100, 99; x 14336 377, 305;
+// 65536 x 2048 44, 52; x 4096 72, 92; 152064 x 1024 62, 67; x 3584 143, 167.  32 tokens, 128256 x 4096 75, 82.
 bool plan_rows(const W4Params& p, coral_dtype dt) {
     const int tiles = (p.N - 1) / 16 + 1, rounds = (p.N - 1) / (256 * kW4RowsRows) + 1;
-    return dt != CORAL_F32 && p.M > 32 && (int64_t)rounds * 6600 < tiles;
+    return dt != CORAL_F32 && p.M > 32 && (int64_t)rounds * 6000 < tiles;
 }
 
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
