@@ -204,7 +204,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int r = lane & 15, q = lane >> 4;
     const int token0 = blockIdx.y * TOKENS, tokens = p.M - token0 < TOKENS ? p.M - token0 : TOKENS;
-    const int row_bytes = p.K / 2, tiles = (p.N + 15) / 16, passes = PASSES ? (p.K + PASS_COLS - 1) / PASS_COLS : 1;
+    const int row_bytes = p.K / 2, tiles = (p.N - 1) / 16 + 1, passes = PASSES ? (p.K + PASS_COLS - 1) / PASS_COLS : 1;
     const int each = tiles / gridDim.x, more_of = tiles % gridDim.x, wg = blockIdx.x;
     const int first = wg * each + (wg < more_of ? wg : more_of), end = first + each + (wg < more_of ? 1 : 0);
 
@@ -510,9 +510,9 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
     constexpr bool INT = KIND != kW4E2M1, ZERO = KIND == kW4Zero, LATE = !INT;
     constexpr bool FINE = SLOTS > 1;
     constexpr int T = kMaxM / 16, R = kW4RowTiles, ROWS = 16 * R, EACH = 4 / SLOTS;
-    constexpr int STAGE_SLOTS = 2 * SLOTS, ENTRIES = ROWS * STAGE_SLOTS, SL = (ENTRIES + kWave - 1) / kWave, STRIDE = STAGE_SLOTS + 1;
+    constexpr int STAGE_SLOTS = 2 * SLOTS, ENTRIES = ROWS * STAGE_SLOTS, SL = ENTRIES / kWave, STRIDE = STAGE_SLOTS + 1;
     constexpr int CODE_ROW = 9, XL = T * 256 / kW4Block;
-    static_assert(XL * kW4Block == T * 256, "");
+    static_assert(SL * kWave == ENTRIES && XL * kW4Block == T * 256, "");
     __shared__ uint4 xs[2][2][T][4][kWave];                  // two stages of two units
     __shared__ uint4 slices[kW4Held][ROWS * CODE_ROW];
     __shared__ unsigned scales[kW4Held][ROWS * STRIDE];      // fp32 scale, or the 16-bit scale and 1 + zero / 16 in fp16
@@ -566,7 +566,7 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
             const int e = i * kWave + l;
             const unsigned zero = ZERO ? __builtin_bit_cast(unsigned short, (_Float16)fmaf((float)z_raw[i], 0.0625f, 1.0f)) : 0u;
             const unsigned word = ZERO ? s_raw[i] << 16 | zero : __float_as_uint(widen16<DT>((unsigned short)s_raw[i]));
-            if (ENTRIES % kWave == 0 || e < ENTRIES) scales[wave][e / STAGE_SLOTS * STRIDE + e % STAGE_SLOTS] = word;
+            scales[wave][e / STAGE_SLOTS * STRIDE + e % STAGE_SLOTS] = word;
         }
     };
     const Buffer x_view = buffer_view(p.x, 0, (size_t)p.M * p.K * 2);
