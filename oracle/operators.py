@@ -137,7 +137,7 @@ def topk_logprob(z, k):
             continue
         order = real[np.lexsort((real, -z[m, real]))][:k]
         top = z[m, real].max()
-        lse = top + np.log(np.exp(z[m, real] - top).sum())
         ids[m, :order.size] = order
-        logp[m, :order.size] = z[m, order] - lse
+        # (not z - (top + log): beside a value of 1e38 the logarithm is nothing)
+        logp[m, :order.size] = (z[m, order] - top) - np.log(np.exp(z[m, real] - top).sum())
     return ids, logp

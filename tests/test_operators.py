@@ -163,6 +163,13 @@ def test_oracle_rules_by_hand():
     assert ids.tolist() == [[0, 1], [-1, -1]] and np.all(logp[1] == -np.inf)
 
 
+def test_oracle_log_probabilities_of_values_far_from_zero():
+    for size in (1.0, 1e17, 3.4e38):
+        ids, logp = plain.topk_logprob(np.array([[-size, -np.inf, -size, -size], [size, size, -np.inf, -np.inf]]), 2)
+        assert ids.tolist() == [[0, 2], [0, 1]]
+        assert np.allclose(logp, [[-math.log(3)] * 2, [-math.log(2)] * 2], rtol=0, atol=1e-15)
+
+
 def test_oracle_against_torch():
     rng = np.random.default_rng(0)
     z = rng.standard_normal((3, 200)) * 3
