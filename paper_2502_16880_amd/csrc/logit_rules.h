@@ -350,6 +350,7 @@ struct TopkParams {
 constexpr int kBoundSpare = 20;
 constexpr int kMaxSlices = 256;                             // lists that a merge takes
 constexpr int kMostCandidates = (kMaxK + kBoundSpare) * kRulePerLane;
+constexpr unsigned kLeastKey = 0x00800000u;                 // upper half of the lowest finite value's key
 
 // A key that at least k of the workgroup's candidates reach, and the candidates of few lanes beside
 // theirs: of the lanes' best keys (one per lane of the workgroup, in LDS; 0 for none) k to k + 20 reach
@@ -369,7 +370,10 @@ __device__ __forceinline__ unsigned long long candidate_bound(const unsigned lon
     }
     // by value first: half the bits
     const unsigned top = wave_max_u32(high);
-    unsigned below = wave_min_u32(low), above = top;         // (the least is reached by all; above + 1 by none)
+    // The least is reached by all, the lowest value's by all that have a candidate; top + 1 by none.  (Not from the
+    // zero of a lane that has none: halfway to it lie the keys of -inf and NaN, which no value compares with.)
+    const unsigned least = wave_min_u32(low);
+    unsigned below = least > kLeastKey ? least : kLeastKey, above = top;
     while (below < above) {                                  // wave-uniform; at most 32 steps
         const unsigned mid = below + (above - below) / 2u + 1u;
         int c = 0;
@@ -383,7 +387,7 @@ __device__ __forceinline__ unsigned long long candidate_bound(const unsigned lon
         }
     }
     // more than the spare have the same one: by ids
-    unsigned long long lo = below != 0u ? (unsigned long long)below << 32 : 1ull;
+    unsigned long long lo = (unsigned long long)below << 32;
     unsigned long long hi = below == 0xffffffffu ? ~0ull : (unsigned long long)(below + 1u) << 32;
     while (hi - lo > 1ull) {
         const unsigned long long mid = lo + ((hi - lo) >> 1);

@@ -440,6 +440,69 @@ def test_lowest_values_are_candidates(coral):
         assert ids.tolist() == [[1234, 0, 1]] and logp[0, 0] == 0 and float(logp[0, 1]) < -6e4
 
 
+# A mask, or biases of -inf, that leave n lanes of a workgroup with a candidate (vectors of 16 bytes are the lanes'), all
+# of very low values: keys next to that of -inf.
+LOW = {"f32": (-3.4028234663852886e38, -2e38, -1.7e38), "bf16": (-3.3895313892515355e38, -2e38), "f16": (-65504.0,)}
+
+
+@pytest.mark.parametrize("how", ["mask", "bias"])
+@pytest.mark.parametrize("k", [1, 10, 64])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_candidates_next_to_minus_infinity(coral, dtype, k, how):
+    lanes, V, E = [1, 2, k, k + 5, k + 20, k + 21], 9000, 4 if dtype == "f32" else 8
+    for low in LOW[dtype]:
+        M = 2 * len(lanes)
+        host = np.full((M, V), low)
+        host[len(lanes):, ::E] *= 1 - 0.004 * np.arange(len(range(0, V, E)))[None, :] % 0.4        # different ones too
+        z, z64 = stored(host, dtype)
+        keep = np.zeros((M, V), dtype=bool)
+        for m in range(M):
+            n = lanes[m % len(lanes)]
+            first = 4096 * (m % 2)                                 # in the first slice, or in the second
+            keep[m, first:first + n * E:E] = True
+        r = Rules(M, V, 0, 0, 0, 1.0)
+        if how == "mask":
+            words = np.zeros((M, -(-V // 32) * 32), dtype=np.uint64)
+            words[:, :V] = keep
+            r.host["mask"] = (words.reshape(M, -1, 32) << np.arange(32, dtype=np.uint64)).sum(2).astype(np.uint32).view(np.int32)
+        else:
+            ids = [np.flatnonzero(~row).astype(np.int32) for row in keep]
+            ends = np.cumsum([len(i) for i in ids])
+            r.host["bias_ids"] = np.concatenate(ids)
+            r.host["bias_values"] = np.full(int(ends[-1]), -np.inf, dtype=np.float32)
+            r.host["bias_ranges"] = np.stack([ends - [len(i) for i in ids], ends], 1).astype(np.int32)
+        ids, logp = coral.coral_logits_topk(z, k, **r.device())
+        want_ids, want_logp = plain.topk_logprob(plain.logit_rules(z64, **r.host)[0], k)
+        assert np.array_equal(ids.cpu().numpy(), want_ids)
+        # equal values' exponentials are 1 and others' 0 (they are 1e35 apart; fp16's 200): the sum is exact, log is off by
+        # 2^-23 at most, the differences by 2^-24 each
+        got, real = logp.double().cpu().numpy(), want_ids >= 0
+        assert np.array_equal(got == -np.inf, ~real)
+        assert (np.abs(got[real] - want_logp[real]) <= 2.0 ** -22 * np.abs(want_logp[real])).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_one_token_of_the_lowest_value(coral, dtype):
+    for low in LOW[dtype]:
+        ids, logp = coral.coral_logits_topk(torch.full((3, 1), low, device="cuda").to(TORCH[dtype]), 1)
+        assert ids.tolist() == [[0]] * 3 and logp.tolist() == [[0.0]] * 3
+
+
+@pytest.mark.parametrize("k", [1, 10, 64])
+def test_few_ordinary_values_among_the_lowest(coral, k):
+    """Fewer lanes than k with an ordinary value, the rest at the type's lowest, and lanes without a candidate."""
+    for lanes in (k, k + 5, k + 20):
+        z = torch.full((2, 3000), -float("inf"), device="cuda")
+        z[:, :lanes * 4:4] = torch.finfo(torch.float32).min
+        z[0, :(k // 2) * 4:4] = torch.linspace(-3, 3, k // 2, device="cuda")
+        want_ids, want_logp = plain.topk_logprob(z.double().cpu().numpy(), k)
+        ids, logp = coral.coral_logits_topk(z, k)
+        assert np.array_equal(ids.cpu().numpy(), want_ids)
+        off = np.abs(logp.double().cpu().numpy() - want_logp)
+        # (as check_topk's: ordinary values and their sum)
+        assert (off <= 2.0 ** -24 * (450 + 4 * np.abs(want_logp))).all()
+
+
 def test_ranges_and_ids_outside_the_arrays_are_passed_over(coral):
     V = 3000
     z, z64 = stored(np.random.default_rng(2).standard_normal((5, V)), "f32")
