@@ -367,7 +367,7 @@ coral_status coral_matvec_w4(const void *x, const void *codes, const void *scale
 /*
  * Rules on a step's logits z[m,v], in this order, each operation rounded to fp32:
  *   repetition  z > 0 ? z / r : z * r   where v is in the row's prompt or output   (r > 0)
- *   frequency   z - count * f           count: how often v is in the row's output
+ *   frequency   z - count * f           where count > 0: how often v is in the row's output
  *   presence    z - p                   where count > 0
  *   bias        z + b                   the last entry for v in the row's list of biases
  *   mask        -inf                    where v's bit is 0

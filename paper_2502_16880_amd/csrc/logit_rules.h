@@ -2,7 +2,7 @@
 //
 // For every token id of a row, in this order and each operation rounded to fp32 by itself:
 //   repetition  z > 0 ? z / r : z * r     where the id is in the row's prompt or output
-//   frequency   z - count * f             count: how often the id is in the row's output
+//   frequency   z - count * f             where count > 0: how often the id is in the row's output
 //   presence    z - p                     where count > 0
 //   bias        z + b                     the last entry of the id in the row's list of biases
 //   mask        -inf                      where the id's bit is 0
@@ -134,9 +134,10 @@ __device__ __forceinline__ float rule_penalty(float z, unsigned seen, float rep,
     if (seen == 0u) return z;
     z = z > 0.f ? z / rep : z * rep;
     const unsigned count = seen & ~kInPrompt;
+    if (count == 0u) return z;                               // (infinite penalties times nothing)
     const float taken = (float)count * freq;
     z = z - taken;
-    return count != 0u ? z - pres : z;
+    return z - pres;
 }
 
 // The lane's values under the rules.  words: one LDS word per place of the slice.  Every thread of the

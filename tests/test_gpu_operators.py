@@ -535,6 +535,20 @@ def test_counts_of_one_token_many_times(coral):
     check_adjusted(coral.coral_logits_adjust(z, **r.device()), z64, r)
 
 
+def test_an_infinite_frequency_penalty_bans_the_outputs_tokens_only(coral):
+    """Tokens of the prompt alone have no count: there is nothing to multiply the penalty with."""
+    V = 5000
+    z, z64 = stored(np.random.default_rng(6).standard_normal((3, V)) * 3, "f32")
+    r = Rules(3, V, 40, 30, 0, 1.0)
+    r.host["penalties"][:, 1] = [np.inf, np.nan, -np.inf]
+    r.host["ranges"][1, 3] = r.host["ranges"][1, 2]               # no output
+    check_adjusted(coral.coral_logits_adjust(z, **r.device()), z64, r)
+    want, _ = plain.logit_rules(z64, **r.host)
+    ids, _ = coral.coral_logits_topk(z[:2].contiguous(), 10, **{n: None if t is None else t[:2].contiguous() if n in ("ranges", "penalties") else t
+                                                                 for n, t in r.device().items()})
+    assert np.array_equal(ids.cpu().numpy(), plain.topk_logprob(want[:2], 10)[0])
+
+
 def test_logits_of_the_widest_rows(coral):
     """As many rows, and as wide, as the calls take (rows that do not start on 16 bytes)."""
     M, V = 64, 1000000 - 3
