@@ -9,11 +9,13 @@
 namespace {
 
 typedef __amdgpu_buffer_rsrc_t Buffer;
-// The bytes from `first` on of an operand of `bytes` (at most 4 GiB of them can be addressed), or none.
+// The bytes from `first` on of an operand of `bytes`, or none: of more than kBufferEnd those before it, so that
+// an offset from kBufferEnd on lies behind every view's end.
+constexpr unsigned kBufferEnd = 0xffffffe0u;
 __device__ __forceinline__ Buffer buffer_view(const void* base, size_t first, size_t bytes, bool any = true) {
     const size_t left = any && first < bytes ? bytes - first : 0;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,
-                                             left < 0xffffffffu ? (unsigned)left : 0xffffffffu, 0x00020000);
+                                             left < kBufferEnd ? (unsigned)left : kBufferEnd, 0x00020000);
 }
 // An offset is a lane's own: a part in a scalar register of its own is not compared with the view's end.
 constexpr int kBufferStream = 2;                 // non-temporal: what is read once

@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
     auto s_at = [&](unsigned tid, int pass, int i, unsigned size) CORAL_INLINE {
         const unsigned slot = pass * (kW4Held * NB * SLOTS) + tid % 32 + 32 * i;
         const unsigned at = tid / 32 * p.n_groups + (FINE ? slot : w4_group_of(p, slot));
-        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferEnd;
         return at * size | behind;
     };
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
                     const int col = unit + (!CHAIN ? r * 8 : FINE ? s * 32 + q * 8 : q * 32 + s * 8);
                     const int row = t * 16 + (!CHAIN ? 4 * s + q : r), token = row / ROWS;
                     // (behind the end; the last row of spread ones may be no token's)
-                    const unsigned off = col < p.K && (!SPREAD || token < TOKENS) ? ((unsigned)token * (unsigned)p.K + col) * W : 0xffffffe0u;
+                    const unsigned off = col < p.K && (!SPREAD || token < TOKENS) ? ((unsigned)token * (unsigned)p.K + col) * W : kBufferEnd;
                     const uint4 a = buffer_read16(x_view, off);
                     if constexpr (DT == kF32) {
                         const uint4 b = buffer_read16(x_view, off + 16u);
@@ -548,7 +548,7 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
         const int e = i * kWave + fresh_lane();
         const unsigned slot = stage * STAGE_SLOTS + e % STAGE_SLOTS, g = FINE ? slot : w4_group_of(p, slot);
         const unsigned at = (unsigned)(e / STAGE_SLOTS) * (unsigned)p.n_groups + g;
-        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : 0xfffffffcu;         // (as in k_w4_held)
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferEnd;         // (as in k_w4_held)
         s_raw[i] = buffer_read2(view, at * 2u | behind);
         if constexpr (ZERO) z_raw[i] = buffer_read1(z_view, at | behind);
     };
@@ -579,7 +579,7 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
 #pragma unroll
         for (int i = 0; i < XL; ++i) {
             const int col = unit * kW4UnitCols + x_chunk(i, l) * 8;
-            x_next[i] = buffer_read16(x_view, col < p.K ? ((unsigned)x_token(i, l) * (unsigned)p.K + (unsigned)col) * 2u : 0xffffffe0u);
+            x_next[i] = buffer_read16(x_view, col < p.K ? ((unsigned)x_token(i, l) * (unsigned)p.K + (unsigned)col) * 2u : kBufferEnd);
         }
     };
     auto put_x = [&](int buffer, int j) CORAL_INLINE {

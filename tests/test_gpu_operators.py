@@ -234,6 +234,23 @@ def test_matvec_w4_beyond_4_gib_of_codes(coral):
     assert (np.abs(y[:, torch.from_numpy(at).cuda()].double().cpu().numpy() - want) <= bound).all()
 
 
+def test_matvec_w4_beyond_4_gib_of_scales(coral):
+    """Columns that the waves hold beyond the row's last one have no scale, however many scales there are: not the
+    one that lies 4 GiB on."""
+    K, group, at = 127 * 8192 + 128, 32, 0x7ffffffe
+    n_groups, N = K // group, 66100
+    assert N * n_groups > at + 2
+    codes = torch.full((N, K // 2), 0x99, dtype=torch.uint8, device="cuda")         # weights of one
+    scales = torch.full((N, n_groups), 0.5, device="cuda", dtype=torch.bfloat16)
+    scales.view(-1)[at] = float("inf")                             # seen from the first row, the last two bytes below 4 GiB
+    x = torch.zeros((2, K), device="cuda", dtype=torch.bfloat16)
+    x[:, ::4096] = 1.0
+    y = coral.coral_matvec_w4(x, codes, scales, group=group)
+    own = at // n_groups                                           # the row whose scale it is
+    y[:, own] = 0.5 * 255
+    assert bool((y == 0.5 * len(range(0, K, 4096))).all()), torch.nonzero(y != 0.5 * 255)[:4].tolist()
+
+
 def test_matvec_w4_on_another_stream_and_in_a_graph(coral):
     c = Product("bf16", 4, 200, 1024, 128, seed=6)
     want = c.run(coral)
