@@ -524,6 +524,9 @@ def _new(shape, dtype, device, stream) -> torch.Tensor:
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+_INT_MAX = 2 ** 31 - 1              # of the library's arguments: ctypes passes the lower half of what is larger
+
+
 W4_CODES = {"int": 0, "e2m1": 1}
 W4_MAX_K = 1 << 20                   # CORAL_W4_MAX_K of the header
 
@@ -552,6 +555,8 @@ def coral_matvec_w4(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, 
         raise ValueError("group must be positive")
     M, K = x.shape
     N = codes.shape[0]
+    if M > _INT_MAX or N > _INT_MAX or K > _INT_MAX or group > _INT_MAX:
+        raise ValueError("sizes and group must fit 32 bits")
     n_groups = -(-K // group)
     if out is not None:
         if out_dtype is not None and out.dtype != out_dtype:
@@ -588,6 +593,8 @@ def _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias
     if (bias_ids is None) != (bias_values is None) or (bias_ids is None) != (bias_ranges is None):
         raise ValueError("bias_ids, bias_values and bias_ranges go together")
     M, V = logits.shape
+    if M > _INT_MAX or V > _INT_MAX:
+        raise ValueError("sizes must fit 32 bits")
     dev = logits.device
     rules = None
     if history is not None or bias_ids is not None or mask is not None:
@@ -627,6 +634,8 @@ def coral_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = 
 
 
 def coral_logits_topk_workspace_bytes(M: int, V: int, k: int) -> int:
+    if not 0 < min(M, V, k) <= max(M, V, k) <= _INT_MAX:
+        return 0
     return int(_L.coral_logits_topk_workspace_bytes(M, V, k))
 
 
@@ -642,6 +651,8 @@ def coral_logits_topk(logits: torch.Tensor, k: int, history: Optional[torch.Tens
     that may overlap; None allocates one."""
     ptr, rules, M, V, dt = _logit_rules(logits, history, ranges, penalties, bias_ids, bias_values, bias_ranges, mask)
     k = int(k)
+    if abs(k) > _INT_MAX:
+        raise ValueError("k must fit 32 bits")
     dev = logits.device
     if topk_ids is None:
         topk_ids = _new((M, max(k, 0)), torch.int32, dev, stream)

@@ -134,6 +134,44 @@ def test_binding_refuses_host_tensors_and_wrong_types():
         coral.coral_logits_topk(torch.zeros(2, 64, dtype=torch.int32), 4)
 
 
+class OnDevice(torch.Tensor):
+    """A tensor without memory that passes for one on the device."""
+    is_cuda = property(lambda self: True)
+
+
+def on_device(*shape, dtype=torch.float32):
+    return torch.Tensor._make_subclass(OnDevice, torch.empty(shape, dtype=dtype, device="meta"))
+
+
+WIDE = 2 ** 32                       # what an argument of 32 bits does not see
+
+
+def test_binding_refuses_sizes_beyond_32_bits(monkeypatch):
+    """Arguments that ctypes would cut to their lower halves, where the operands fit the whole ones."""
+    calls = []
+    monkeypatch.setattr(coral, "_enqueue", lambda *a: calls.append(a))
+    u8, f16 = torch.uint8, torch.float16
+    x, codes = on_device(2, 256), on_device(64, 128, dtype=u8)
+    coral.coral_matvec_w4(x, codes, on_device(64, 2))
+    coral.coral_logits_topk(on_device(2, 100), 5, workspace=on_device(1 << 20, dtype=u8))
+    coral.coral_logits_adjust(on_device(2, 100))
+    assert len(calls) == 3
+    for call in (lambda: coral.coral_matvec_w4(x, codes, on_device(64, 1), group=WIDE + 128),
+                 lambda: coral.coral_matvec_w4(x, on_device(WIDE + 64, 128, dtype=u8), on_device(WIDE + 64, 2)),
+                 lambda: coral.coral_matvec_w4(on_device(WIDE + 2, 8), on_device(64, 4, dtype=u8), on_device(64, 1)),
+                 lambda: coral.coral_matvec_w4(on_device(2, WIDE + 256), on_device(64, WIDE // 2 + 128, dtype=u8), on_device(64, WIDE // 128 + 2)),
+                 lambda: coral.coral_logits_adjust(on_device(1, WIDE + 100, dtype=f16)),
+                 lambda: coral.coral_logits_adjust(on_device(WIDE + 1, 8, dtype=f16)),
+                 lambda: coral.coral_logits_topk(on_device(1, WIDE + 100), 5, workspace=on_device(1 << 20, dtype=u8)),
+                 lambda: coral.coral_logits_topk(on_device(2, 100), WIDE + 5, workspace=on_device(1 << 20, dtype=u8)),
+                 lambda: coral.coral_logits_topk(on_device(2, 100), 5 - WIDE, workspace=on_device(1 << 20, dtype=u8))):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    assert len(calls) == 3
+    wb = coral.coral_logits_topk_workspace_bytes
+    assert wb(2, 100, 5) > 0 and wb(WIDE + 2, 100, 5) == wb(2, WIDE + 100, 5) == wb(2, 100, WIDE + 5) == wb(2 - WIDE, 100, 5) == 0
+
+
 # ---------------------------------------------------------------- the oracle
 def test_oracle_codes_and_weights_by_hand():
     codes = np.array([[0x10, 0x98, 0xFE, 0x37]], dtype=np.uint8)               # columns 0 1 8 9 14 15 7 3
