@@ -10,6 +10,7 @@
 // are, and every product is taken three times: the sums are fp32 sums of exact products in all types.
 #pragma once
 #include "buffer_loads.h"
+#include "w4_plan.h"
 
 namespace {
 
@@ -27,7 +28,6 @@ struct W4Params {
     unsigned per_group, per_group_inv;           // units of a group (at least one), 2^32 / that, rounded up
 };
 
-constexpr int kW4UnitCols = 128;                 // columns of a unit: four products of 32
 // A slot is the columns of a unit that share a scale: SLOTS of them, of 32 or 64 columns, where groups are
 // finer than a unit, else one.
 
@@ -156,8 +156,7 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // The operands are read through buffer descriptors, which drop what lies behind their end: rows behind
 // the last one, and tokens and columns behind the activations, read as zero without a comparison.
 // Codes behind a row's last column are another row's and meet activations of zero.
-constexpr int kW4Block = 512;
-constexpr int kW4Held = kW4Block / kWave;
+constexpr int kW4Block = kW4Held * kWave;
 
 // The value is wanted in registers here: what makes it is neither moved behind this point nor, with a
 // value that a loop does not change, in front of the loop.
@@ -167,13 +166,6 @@ __device__ __forceinline__ void w4_settle(uint4& v) { asm volatile("" : "+v"(v.x
 __device__ __forceinline__ unsigned w4_group_of(const W4Params& p, unsigned unit) {
     return p.per_group == 1 ? unit : __umulhi(unit, p.per_group_inv);
 }
-
-// What decides how many workgroups fit a compute unit: the registers that the activations take, in 16s
-// (chain: fp32 ones as three products one after the other).
-constexpr int w4_held_regs(bool chain, int t, int nb) { return !chain ? t * nb : nb > 1 ? 8 : 4; }
-// fp32 activations are three rows of the products a token (spread), or, up to three units a wave, three
-// products one after the other.
-constexpr int w4_held_tokens(bool spread, int t) { return spread ? t * 16 / 3 : t * 16; }
 
 // T tiles of 16 rows of activations, NB units a wave.  PASSES: the columns are more than the waves hold and are taken
 // in passes; the workgroup goes through a block of tiles once a pass, adding the tiles' sums up in
@@ -503,7 +495,6 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
 // of 32, 620 and 565 TFLOP/s.  The products alone take 33 us.  Of a stage's 11800 cycles 5100 are products, 3000
 // the issue of its loads, 1200 the barrier, the rest reads of LDS and vector instructions that the two waves
 // of a SIMD, which its registers allow, do not hide from each other.
-constexpr int kW4RowTiles = 4, kW4RowsRows = kW4Held * kW4RowTiles * 16;      // of a wave; rows of a workgroup
 template <int DT, int KIND, int SLOTS>
 __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
     static_assert(DT != kF32, "");

@@ -159,6 +159,73 @@ def test_matvec_w4_infinite_scales_of_a_rows_last_group(coral, M, N, K, group):
     assert torch.equal(y[:, 1::2][sure], (last.sign() * float("inf"))[sure]) and bool(torch.isfinite(y[:, ::2]).all())
 
 
+# Every form of the kernel that takes tiles of rows one after the other (units of columns a wave, tiles of tokens, passes,
+# fp32 parts one after the other or spread), few rows and the last of them and of the columns not full.
+FORMS = [(M, K) for M in (1, 5, 16, 20) for K in (1000, 2040, 2568, 4040, 4104, 5000, 7000, 8184, 9000)] + [(11, 4096), (50, 2568), (50, 8200), (64, 4104)]
+
+
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K", FORMS)
+def test_matvec_w4_forms(coral, dtype, kind, zeros, group, M, K):
+    N = 83
+    c = Product(dtype, M, N, K, group, kind, zeros, seed=11)
+    y, untouched = guarded((M, N), torch.float32)
+    c.run(coral, out=y)
+    c.check(y)
+    untouched()
+    assert torch.equal(c.run(coral), y)
+
+
+# Columns in passes, more tiles a workgroup than a block holds the sums of.
+PASSES = [("bf16", 2, 110011, 8328), ("f16", 20, 110011, 4232), ("f32", 3, 200003, 4232), ("f32", 9, 110011, 4232)]
+
+
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("group", [32, 64, 384])
+@pytest.mark.parametrize("dtype,M,N,K", PASSES)
+def test_matvec_w4_passes_over_many_rows(coral, dtype, kind, zeros, group, M, N, K):
+    gen = torch.Generator("cuda").manual_seed(N + K + group)
+    x, x64 = stored(np.random.default_rng(12).standard_normal((M, K)), dtype)
+    codes = torch.randint(0, 256, (N, K // 2), generator=gen, device="cuda", dtype=torch.uint8)
+    scales = ((0.5 + torch.rand((N, -(-K // group)), generator=gen, device="cuda")) * 0.01).to(TORCH[dtype])
+    zero = torch.randint(0, 16, scales.shape, generator=gen, device="cuda", dtype=torch.uint8) if zeros else None
+    runs = [coral.coral_matvec_w4(x, codes, scales, zero, group=group, code_type=kind) for _ in range(3)]
+    assert bool(torch.isfinite(runs[0]).all()) and all(torch.equal(y, runs[0]) for y in runs)
+    at = np.unique(np.r_[0:40, N - 40:N, 0:N:701])
+    on = torch.from_numpy(at).cuda()
+    args = (codes[on].cpu().numpy(), scales[on].double().cpu().numpy(), None if zero is None else zero[on].cpu().numpy(), group, kind)
+    want, bound = plain.matvec_w4(x64, *args), plain.matvec_w4_bound(x64, *args)
+    off = np.abs(runs[0][:, on].double().cpu().numpy() - want)
+    assert (off <= bound).all() and np.linalg.norm(off) <= 2e-6 * np.linalg.norm(want)
+    # a workgroup's first and last tiles, and those at the ends of its blocks: rows of a matrix of ones
+    ones = torch.full_like(codes, 0x99 if kind == "int" else 0x22)
+    flat = torch.ones_like(scales)
+    y = coral.coral_matvec_w4(torch.ones_like(x), ones, flat, None, group=group, code_type=kind)
+    assert bool((y == K).all())
+
+
+# Many tokens and rows that fill the rounds of the kernel for them, beside the shapes above.
+MANY_ROWS = [(64, 96017, 136, 32), (33, 96100, 392, 64), (50, 100003, 264, 128), (63, 131072, 8, 32), (64, 192100, 1032, 256), (40, 200001, 256, 64)]
+
+
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M,N,K,group", MANY_ROWS)
+def test_matvec_w4_many_rows_against_few_tokens(coral, dtype, kind, zeros, M, N, K, group):
+    test_matvec_w4_many_rows(coral, dtype, kind, zeros, M, N, K, group)
+
+
+INFINITE_ROWS = [96033, 192200]
+
+
+@pytest.mark.parametrize("N", INFINITE_ROWS)
+@pytest.mark.parametrize("K,group", [(40, 32), (200, 64), (648, 128)])
+def test_matvec_w4_infinite_scales_with_many_rows(coral, N, K, group):
+    test_matvec_w4_infinite_scales_of_a_rows_last_group(coral, 50, N, K, group)
+
+
 @pytest.mark.parametrize("act", ["identity", "silu", "relu"])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,N,K", [(1, 512, 512), (9, 131, 1024), (40, 77, 640)])

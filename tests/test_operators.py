@@ -26,6 +26,53 @@ def test_header_and_library_agree_on_names_with_digits():
     assert all(hasattr(lib, n) for n in names)
 
 
+# ---------------------------------------------------------------- which kernel a 4-bit product takes
+PLAN = r"""
+#include <cstdio>
+#include <set>
+#include <tuple>
+#include "w4_plan.h"
+int main() {
+    std::set<std::tuple<int, int, int, int, int>> forms;
+    for (int f32 = 0; f32 < 2; ++f32)
+        for (int M = 1; M <= 64; ++M)
+            for (int K = 8; K <= 1 << 20; K += 8) {
+                const W4Plan p = w4_plan_held(M, K, f32 != 0);
+                forms.insert({f32, p.t, p.nb, p.passes, p.spread});
+            }
+    for (auto [f32, t, nb, passes, spread] : forms) std::printf("form %d %d %d %d %d\n", f32, t, nb, passes, spread);
+    int f32, M, N, K;
+    while (std::scanf("%d %d %d %d", &f32, &M, &N, &K) == 4) {
+        const W4Plan p = w4_plan_held(M, K, f32 != 0);
+        const W4Grid g = w4_held_grid(p, M, N, f32 != 0);
+        std::printf("call %d %d %d %d %d %d %d %d\n", w4_plan_rows(M, N, f32 != 0) ? 1 : 0, f32, p.t, p.nb, p.passes, p.spread, g.x, g.y);
+    }
+}
+"""
+
+
+def test_gpu_tests_reach_every_form_of_the_4_bit_products(tmp_path):
+    """The rules (csrc/w4_plan.h) compiled for the host: every form of the kernel that some call takes is one of the GPU
+    tests' calls, and the shapes meant for many rows, and for several blocks of tiles, are such."""
+    import subprocess
+    import test_gpu_operators as gpu
+    (tmp_path / "plan.cpp").write_text(PLAN)
+    exe = str(tmp_path / "plan")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2502_16880_amd", "csrc"), str(tmp_path / "plan.cpp"), "-o", exe], check=True)
+    held = [(f32, M, 83, K) for f32 in (0, 1) for M, K in gpu.FORMS]
+    passes = [(int(dtype == "f32"), M, N, K) for dtype, M, N, K in gpu.PASSES]
+    rows = [(0, M, N, K) for M, N, K, _ in gpu.MANY_ROWS] + [(0, 50, N, 40) for N in gpu.INFINITE_ROWS]
+    text = "\n".join(" ".join(map(str, c)) for c in held + passes + rows)
+    out = [line.split() for line in subprocess.run([exe], input=text, check=True, capture_output=True, text=True).stdout.splitlines()]
+    forms = {tuple(map(int, l[1:])) for l in out if l[0] == "form"}
+    calls = [tuple(map(int, l[1:])) for l in out if l[0] == "call"]
+    assert len(calls) == len(held) + len(passes) + len(rows) and len(forms) == 12 + 10
+    assert {c[1:6] for c in calls[:len(held)]} == forms and not any(c[0] for c in calls[:len(held)])
+    for (_, M, N, K), c in zip(passes, calls[len(held):]):
+        assert c[0] == 0 and c[4] == 1 and -(-N // 16) > 24 * c[6] and c[7] == 1       # a block is 24 tiles at most
+    assert all(c[0] == 1 for c in calls[len(held) + len(passes):])
+
+
 # ---------------------------------------------------------------- refusals
 def matvec(**kw):
     a = dict(x=FAKE, codes=FAKE + (1 << 30), scales=FAKE + (2 << 30), zeros=None, bias=None, residual=None, M=4, N=64, K=256,
