@@ -455,6 +455,40 @@ def test_logits_topk(coral, dtype, M, V, prompt, output, biases, allowed, shared
     assert int(ws[:512].view(torch.int32).abs().sum()) == 0                        # the control words, as they were
 
 
+PREPARED = (128 + 4096) * 4         # bytes of control words and score words, where the rows' counters lie
+
+
+@pytest.mark.parametrize("M,V,k", [(1, 9000, 3), (64, 30000, 64), (24, 300000, 20), (5, 1000, 10)])
+def test_logits_topk_leaves_its_counters_as_they_were(coral, M, V, k):
+    ws = torch.zeros(max(coral.coral_logits_topk_workspace_bytes(M, V, k), PREPARED), dtype=torch.uint8, device="cuda")
+    z = torch.randn((M, V), device="cuda", generator=torch.Generator("cuda").manual_seed(M))
+    first = coral.coral_logits_topk(z, k, workspace=ws)
+    for _ in range(3):
+        again = coral.coral_logits_topk(z, k, workspace=ws)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+        assert int(ws[:PREPARED].view(torch.int32).abs().sum()) == 0
+
+
+def test_logits_topk_and_a_head_with_a_shared_gate_in_one_workspace(coral):
+    """The head's score words are the rows' counters: zero whenever one call takes them from the other."""
+    M, H, V, G, k = 1, 4096, 64000, 256, 10
+    gen = torch.Generator("cuda").manual_seed(3)
+    hidden, gate, head = (torch.randn(s, device="cuda", generator=gen).bfloat16() * 0.02 for s in ((M, H), (G, H), (V, H)))
+    gi = coral.GroupIndex(np.arange(G + 1) * (V // G), np.arange(V, dtype=np.int32))
+    z = torch.randn((64, V), device="cuda", generator=gen)
+    ws = torch.empty(max(coral.coral_lmhead_workspace_bytes(M, H, V, G, 4, k, coral.CORAL_BF16),
+                         coral.coral_logits_topk_workspace_bytes(64, V, k)), dtype=torch.uint8, device="cuda")
+    coral.coral_lmhead_workspace_init(ws)
+    want = [t.clone() for t in coral.coral_lmhead_grouped(hidden, gate, None, head, gi, 4, k)]
+    want_ids, want_logp = coral.coral_logits_topk(z, k)
+    scores = ws[512:PREPARED].view(torch.int32)
+    for _ in range(4):
+        got = coral.coral_lmhead_grouped(hidden, gate, None, head, gi, 4, k, workspace=ws)
+        assert int(scores.abs().sum()) == 0 and all(torch.equal(a, b) for a, b in zip(got, want))
+        ids, logp = coral.coral_logits_topk(z, k, workspace=ws)
+        assert int(scores.abs().sum()) == 0 and torch.equal(ids, want_ids) and torch.equal(logp, want_logp)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,V,k", [(1, 700, 64), (3, 5001, 20), (16, 20000, 64)])
 def test_logits_topk_ties_go_to_the_lower_id(coral, dtype, M, V, k):

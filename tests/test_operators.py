@@ -167,6 +167,23 @@ def test_topk_workspace_bytes():
         assert topk(M=64, V=V, k=k, ws_bytes=sizes[-1] - 1, ids=FAKE + (20 << 30), logp=FAKE + (21 << 30), ws=(FAKE + (30 << 30)) & ~255) == WORKSPACE
 
 
+def test_row_counters_lie_in_the_score_words(tmp_path):
+    """One counter a row, each in 256 bytes of its own, in the words that the heads' shared gate leaves zero between
+    calls and coral_lmhead_workspace_init clears; the published lists behind them."""
+    import subprocess
+    (tmp_path / "c.cpp").write_text('#include <cstdio>\n#include "control_words.h"\nint main() { using namespace coral_ctrl;\n'
+                                    'std::printf("%d %d %d %d %d %d\\n", kWords, kGateScores, kGateScoreWords, kPreparedWords, kRowArrival, kRowArrivalStride); }\n')
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2502_16880_amd", "csrc"), str(tmp_path / "c.cpp"), "-o", str(tmp_path / "c")], check=True)
+    out = subprocess.run([str(tmp_path / "c")], check=True, capture_output=True, text=True).stdout
+    words, scores, n_scores, prepared, first, stride = map(int, out.split())
+    counters = [first + m * stride for m in range(64)]
+    assert stride * 4 >= 256 and scores == words and prepared == scores + n_scores
+    assert all(scores <= c < scores + n_scores for c in counters)
+    import test_gpu_operators as gpu
+    assert gpu.PREPARED == 4 * prepared and (gpu.PREPARED - 4 * words) == 4 * n_scores
+    assert coral.coral_logits_topk_workspace_bytes(1, 1, 1) > 4 * prepared
+
+
 def test_binding_refuses_host_tensors_and_wrong_types():
     x, codes, scales = torch.zeros(2, 64), torch.zeros(3, 32, dtype=torch.uint8), torch.zeros(3, 1)
     with pytest.raises(ValueError, match="device memory"):
