@@ -683,6 +683,33 @@ def test_logits_of_the_widest_rows(coral):
     assert torch.equal(got, z)
 
 
+# More published candidates than the workgroup's merge takes at once: one wave merges the lists.
+@pytest.mark.parametrize("V,k", [(262145, 64), (300000, 64), (1000000, 64), (1000000, 20), (999993, 17)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_topk_many_lists(coral, dtype, V, k):
+    M = 6
+    gen = torch.Generator("cuda").manual_seed(V + k)
+    z = torch.randn((M, V), device="cuda", generator=gen) * 3
+    z[1] = torch.randint(-8, 9, (V,), device="cuda", generator=gen) * 0.5          # equal values
+    z[2, V // 2:V // 2 + 100] += 50                                                 # the best in one slice
+    z[3] = -float("inf")
+    z[3, 5::V // 9] = torch.arange(len(range(5, V, V // 9)), device="cuda") * 0.25  # fewer candidates than k
+    z[4] = 2.0
+    z[5] = torch.linspace(0, 40, V, device="cuda")                                  # the best last
+    z = z.to(TORCH[dtype])
+    ids, logp = coral.coral_logits_topk(z, k)
+    z64 = z.double()
+    val, at = torch.sort(z64, dim=1, descending=True, stable=True)
+    val, at = val[:, :k], at[:, :k].int()
+    real = val > -float("inf")
+    assert torch.equal(ids, torch.where(real, at, torch.full_like(at, -1)))
+    want = val - torch.logsumexp(z64, dim=1, keepdim=True)
+    assert torch.equal(logp == -float("inf"), ~real)
+    # (as in check_topk, without rules)
+    tol = 2.0 ** -24 * (440 + 2 * want[real].abs() + 2 * val[real].abs())
+    assert bool(((logp.double() - want)[real].abs() <= tol).all())
+
+
 def test_logits_calls_on_streams_and_in_graphs(coral):
     M, V, k = 4, 30000, 12
     r = Rules(M, V, 200, 100, 20, 0.5)
