@@ -348,8 +348,10 @@ coral_status coral_lmhead_dense(const void *hidden, const void *lm_W, int M, int
  *   y        [device] out [M,N] of out_dt; overlaps no input, but may be the residual itself where
  *            out_dt is dt
  * Limits: 1 <= M <= 64; K a multiple of 8, at most CORAL_W4_MAX_K; group 32, 64 or a multiple of 128
- * (the last one may be cut short by K).  Values of x must be finite: the results of a token with
- * another value are unspecified, the other tokens' are not.  Needs no workspace.
+ * (the last one may be cut short by K).  Values of x must be finite, and with integer codes
+ * (47 + zero) sum |x| over any 128 columns must stay in fp32's range (|x| up to 8e33 does whatever the
+ * zero points): the results of a token with other values are unspecified, the other tokens' are not.
+ * Of fp32 values what lies below 2^-133 is dropped.  Needs no workspace.
  */
 typedef enum {
     CORAL_W4_INT = 0,

@@ -5,7 +5,8 @@
 // that a lane holds the sums of one weight row and the row's scales and zero points are one value a
 // lane.  Codes become 16-bit operands exactly: an integer code n is put into the mantissa of 16.0
 // (16 + n, two operations for two codes) and the sum of (16 + zero) x is taken off per group in fp32,
-// or is where the accumulator starts; an e2m1 code has an instruction.  Scales multiply the group's
+// or is where the accumulator starts; an e2m1 code has an instruction.  (So sums of (16 + code) |x| and of
+// (16 + zero) |x|, 31 and 271 at most, have to stay in fp32's range.)  Scales multiply the group's
 // fp32 sum, never a 16-bit weight.  fp32 activations are split into three bf16 values whose sum they
 // are, and every product is taken three times: the sums are fp32 sums of exact products in all types.
 #pragma once
@@ -88,7 +89,7 @@ __device__ __forceinline__ uint4 w4_order(uint4 v) {
 }
 
 // Part c of eight fp32 values, x = hi + mid + lo exactly in bf16: the significand's 24 bits are cut off in
-// eights.
+// eights.  (Below 2^-133, the smallest step of a bf16, there is nothing: that affects |x| < 2^-110 only.)
 __device__ __forceinline__ uint4 w4_part(uint4 x, uint4 y, int c) {
     const unsigned f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
     unsigned b[8];

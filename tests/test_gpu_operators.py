@@ -287,6 +287,64 @@ def test_matvec_w4_zero_scales_and_extreme_values(coral):
         c.check(c.run(coral))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N,group", [(3, 70, 32), (20, 70, 128), (50, 96017, 64)])
+def test_matvec_w4_zero_points_of_all_bytes(coral, dtype, M, N, group):
+    c = Product(dtype, M, N, 520, group, seed=13)
+    c.zeros_host = np.random.default_rng(14).integers(0, 256, c.zeros_host.shape, dtype=np.uint8)
+    c.zeros = torch.from_numpy(c.zeros_host).cuda()
+    c.check(c.run(coral), rows=np.unique(np.r_[0:40, N - 30:N]))
+
+
+@pytest.mark.parametrize("zeros", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N", [(3, 70), (20, 70), (50, 96017)])
+def test_matvec_w4_largest_activations(coral, dtype, M, N, zeros):
+    """(47 + zero) sum |x| over 128 columns just inside fp32: nothing overflows on the way.  (All activations are
+    equal: the worst case of the sums' roundings applies, not what random signs leave of it.)"""
+    c = Product(dtype, M, N, 256, 128, zeros=zeros, seed=15)
+    if zeros:
+        c.zeros_host[:] = 255
+        c.zeros.fill_(255)
+    c.x, c.x64 = stored(np.full((M, 256), 0.99 * np.finfo(np.float32).max / 128 / (47 + (255 if zeros else 8))), dtype)
+    c.scales, c.scales64 = stored(np.full(c.scales64.shape, 2.0 ** -10), dtype)
+    y = c.run(coral)
+    assert bool(torch.isfinite(y).all())
+    args = (c.x64, c.codes_host[:50], c.scales64[:50], c.zeros_host[:50] if zeros else None, 128)
+    off = np.abs(y[:, :50].double().cpu().numpy() - plain.matvec_w4(*args))
+    assert (off <= plain.matvec_w4_bound(*args)).all()
+
+
+@pytest.mark.parametrize("kind,zeros", [("int", False), ("int", True), ("e2m1", False)])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N", [(2, 70), (9, 70), (50, 96017)])
+def test_matvec_w4_subnormal_activations(coral, dtype, kind, zeros, M, N):
+    """Values below the type's smallest normal number count as they are; of fp32 ones what lies below 2^-133, the
+    smallest step of their bf16 parts, is dropped: less than that a value, times its weight."""
+    c = Product(dtype, M, N, 256, 64, kind, zeros, seed=16)
+    rng = np.random.default_rng(17)
+    x = rng.integers(-60, 61, (M, 256)) * 2.0 ** -24 if dtype == "f16" else rng.standard_normal((M, 256)) * (1e-36 if dtype == "f32" else 1e-38)
+    c.x, c.x64 = stored(x, dtype)
+    c.scales, c.scales64 = stored(np.full(c.scales64.shape, 2.0 ** 10), dtype)
+    y = c.run(coral)[:, :50].double().cpu().numpy()
+    args = (c.codes_host[:50], c.scales64[:50], c.zeros_host[:50] if zeros else None, 64, kind)
+    bound = plain.matvec_w4_bound(c.x64, *args)
+    if dtype == "f32":
+        bound += 2.0 ** -133 * np.abs(plain.w4_weights(*args)).sum(axis=1)
+    off = np.abs(y - plain.matvec_w4(c.x64, *args))
+    assert (off <= bound).all() and (dtype == "f32" or (off == 0).all())
+
+
+def test_matvec_w4_just_above_what_three_bf16_values_hold(coral):
+    """fp32 activations whose lowest bit is 2^-133, a whole number of the parts' smallest steps: nothing is dropped."""
+    c = Product("f32", 3, 70, 256, 64, seed=18)
+    n = np.random.default_rng(19).integers(-2 ** 23, 2 ** 23, (3, 256))
+    c.x, c.x64 = stored(n * 2.0 ** -133, "f32")
+    assert np.array_equal(c.x64, n * 2.0 ** -133)
+    c.scales, c.scales64 = stored(np.full(c.scales64.shape, 2.0 ** 10), "f32")
+    c.check(c.run(coral))
+
+
 def test_matvec_w4_beyond_4_gib_of_codes(coral):
     """Rows whose codes lie past 2^32 bytes."""
     N, K = 150000, 58368
