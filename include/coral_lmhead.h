@@ -420,7 +420,8 @@ coral_status coral_logits_adjust(const void *logits, const coral_logit_rules *ru
  * candidate hold (-1, -inf).  With a value of +inf the row's log-probabilities are unspecified.
  *   workspace [device] at least coral_logits_topk_workspace_bytes(M, V, k) bytes, 256-byte aligned,
  *             prepared once by coral_lmhead_workspace_init with at least that many bytes (or filled
- *             with zeros); one of the heads' serves too, for calls that do not overlap.  Outputs overlap neither it nor an input.
+ *             with zeros); one of the heads' serves too, for calls that do not overlap.  Outputs
+ *             overlap neither it nor an input.
  * Limits: 1 <= M <= 64, 1 <= k <= 64, k <= V <= CORAL_LOGITS_MAX_V.
  */
 size_t coral_logits_topk_workspace_bytes(int M, int V, int k);
