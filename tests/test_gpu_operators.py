@@ -376,6 +376,24 @@ def test_matvec_w4_beyond_4_gib_of_scales(coral):
     assert bool((y == 0.5 * len(range(0, K, 4096))).all()), torch.nonzero(y != 0.5 * 255)[:4].tolist()
 
 
+def shifted(t, n=1):
+    """The same values, n elements behind a 256-byte boundary."""
+    whole = torch.empty(t.numel() + n, dtype=t.dtype, device=t.device)        # (the allocator gives such boundaries)
+    whole[n:] = t.reshape(-1)
+    return whole[n:].view(t.shape)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("M,N,K,group", [(3, 83, 1000, 32), (9, 83, 2568, 128), (20, 83, 5000, 64), (50, 96017, 136, 32)])
+def test_matvec_w4_operands_aligned_to_their_type_only(coral, dtype, M, N, K, group):
+    """Scales, zero points, bias, residual and results one element behind a boundary (x and codes are on 16 bytes)."""
+    c = Product(dtype, M, N, K, group, bias=True, residual=True, seed=20)
+    want = c.run(coral, "silu", out_dtype=TORCH[dtype])
+    c.scales, c.zeros, c.bias, c.residual = (shifted(t) for t in (c.scales, c.zeros, c.bias, c.residual))
+    assert torch.equal(c.run(coral, "silu", out=shifted(torch.zeros_like(want))), want)
+    assert torch.equal(c.run(coral, "silu", residual=c.residual, out=c.residual), want)
+
+
 def test_matvec_w4_on_another_stream_and_in_a_graph(coral):
     c = Product("bf16", 4, 200, 1024, 128, seed=6)
     want = c.run(coral)
@@ -586,6 +604,35 @@ def test_masked_nan_and_infinities_do_not_matter(coral):
         got = coral.coral_logits_topk(dirty, 20, mask=mask)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         assert torch.equal(coral.coral_logits_adjust(dirty, mask=mask), y)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_infinite_logits_are_the_first_candidates(coral, dtype):
+    """(What their rows' log-probabilities are is left open.)"""
+    z = torch.randn((3, 9001), device="cuda", generator=torch.Generator("cuda").manual_seed(1)).to(TORCH[dtype])
+    z[0, 8999] = z[2, 17] = z[2, 5000] = float("inf")
+    ids, _ = coral.coral_logits_topk(z, 20)
+    assert torch.equal(ids, torch.sort(z, dim=1, descending=True, stable=True).indices[:, :20].int())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 9, 64])
+def test_many_rows_of_few_tokens(coral, dtype, V):
+    r = Rules(64, V, 3, 2, 2, 0.7)
+    z, z64 = stored(np.random.default_rng(V).standard_normal((64, V)), dtype)
+    for k in sorted({1, (V + 1) // 2, V}):
+        check_topk(*coral.coral_logits_topk(z, k, **r.device()), z64, r, k)
+    check_adjusted(coral.coral_logits_adjust(z, **r.device()), z64, r)
+
+
+def test_rules_aligned_to_their_type_only(coral):
+    r = Rules(9, 5003, 70, 31, 7, 0.5)
+    d = r.device()
+    moved = {n: None if t is None else torch.cat([t.reshape(-1)[:1], t.reshape(-1)])[1:].view(t.shape) for n, t in d.items()}
+    z = torch.randn((9, 5003), device="cuda")
+    assert torch.equal(coral.coral_logits_adjust(z, **moved), coral.coral_logits_adjust(z, **d))
+    a, b = coral.coral_logits_topk(z, 12, **moved), coral.coral_logits_topk(z, 12, **d)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
 def test_rows_that_nothing_is_left_of(coral):
