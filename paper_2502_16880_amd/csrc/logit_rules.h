@@ -14,10 +14,11 @@
 // Measured: written back, 64 rows of 151665 bf16 values with prompts of 8000, outputs of 1000, 100 biases and
 // masks: 20 us (39 MB of logits: 8 us); without rules 9.7 us.  One row of 128256 fp32: 6 us, most of it
 // the launch and two trips to memory.  The k best: 64 rows of 152064 fp32, every rule, k = 64: 33 us, without
-// rules 21 us, k = 10 17 us (the reading alone: 6 us); one row, k = 10: 8.6 us.  What bounds the large ones
-// is the instructions of a value (words of LDS read, rules, comparisons, 2^x), the small ones the chain of
+// rules 22 us, k = 10 17 us (the reading alone: 6 us); one row, k = 10: 9.0 us.  What bounds the large ones
+// is the instructions of a value (words of LDS read, rules, comparisons, 2^x) and that 64 rows are 2432 workgroups for
+// 2048 places (62 registers, 19 KB of LDS): the chain of one is run twice.  The small ones are the chain of
 // the steps, from the launch to the last workgroup's merge.  24 rows over one prompt of 60000 tokens: 20 us,
-// of which 9 are the prompt's reading by each of 13 slices.
+// of which 7 are the prompt's reading by each of 13 slices.
 // A slice of 8192 values, two batches a wave, instead of 4096 took 24 us for 21 and 42 for 41; one streamed by
 // eight waves in tiles, with notes of 16 bits in LDS, 29 and 48.
 #pragma once

@@ -142,11 +142,12 @@ __device__ __forceinline__ void w4_store(const W4Params& p, int m, int n, float 
 // by row by the whole workgroup one tile ahead and kept in LDS as fp32.  The waves' sums meet in LDS
 // once a tile.  More tokens than T tiles hold are other workgroups' (the grid's second dimension).
 //
-// Measured (copy 4.9 TB/s, reading alone 6.5 TB/s): bf16, one token, 128256 x 4096, groups of 128: 50 us, 5.4
-// TB/s, bound by memory; e2m1 in groups of 32: 50 us, 5.9 TB/s.  fp16, 16 tokens, 152064 x 3584, groups of 64
-// with zero points: 65 to 73 us, 4.1 TB/s: a product of 32 columns takes a dozen vector instructions beside
+// Measured (copy 4.9 TB/s, reading alone 6.5 TB/s): bf16, one token, 128256 x 4096, groups of 128: 45 us, 6.0
+// TB/s, bound by memory (48 to 53 where calls follow each other in a graph without a pause); e2m1 in groups of 32: 50 to 52 us
+// there, 5.7 TB/s.  fp16, 16 tokens, 152064 x 3584, groups of 64
+// with zero points: 63 us, 4.9 TB/s (69 to 73): a product of 32 columns takes a dozen vector instructions beside
 // it (codes to operands, zero point, scale), which are about as long as the reading.  fp32, one token, 128256 x
-// 4096: 55 us; 7 tokens, 50257 x 2568, groups of 32: 33 us, 2.6 TB/s: three products for one, and one workgroup
+// 4096: 51 us (54 to 57); 7 tokens, 50257 x 2568, groups of 32: 33 us, 2.6 TB/s: three products for one, and one workgroup
 // a compute unit for its registers.  4096 x 4096, one token: 6.1 us, of which the launch is 2.5 and one trip to memory 2.
 //
 // Lane 16 q + r takes the 16 bytes of row r that hold columns 32 q to 32 q + 31 of a unit, and product
@@ -492,8 +493,8 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
 // exchanged through a slice of LDS of the wave's own, as are the scales.  With slots finer than a unit a
 // stage's loads are spread over its products (all at once they keep the waves waiting: 64 tokens, e2m1, groups
 // of 32, 126 against 118 us); with one slot the registers do not allow it.
-// Measured: bf16, 64 tokens, 128256 x 4096: 109 us with integers in groups of 128, 119 us with e2m1 in groups
-// of 32, 620 and 565 TFLOP/s.  The products alone take 33 us.  Of a stage's 11800 cycles 5100 are products, 3000
+// Measured: bf16, 64 tokens, 128256 x 4096: 105 us with integers in groups of 128, 112 to 120 us with e2m1 in groups
+// of 32, 640 and 560 TFLOP/s.  The products alone take 33 us.  Of a stage's 11800 cycles 5100 are products, 3000
 // the issue of its loads, 1200 the barrier, the rest reads of LDS and vector instructions that the two waves
 // of a SIMD, which its registers allow, do not hide from each other.
 template <int DT, int KIND, int SLOTS>
