@@ -12,6 +12,7 @@ typedef __amdgpu_buffer_rsrc_t Buffer;
 // The bytes from `first` on of an operand of `bytes`, or none: of more than kBufferEnd those before it, so that
 // an offset from kBufferEnd on lies behind every view's end.
 constexpr unsigned kBufferEnd = 0xffffffe0u;
+constexpr unsigned kBufferBehind = 0xfffffffcu;  // such an offset, to be or'ed to any (the instructions hold a small negative number)
 __device__ __forceinline__ Buffer buffer_view(const void* base, size_t first, size_t bytes, bool any = true) {
     const size_t left = any && first < bytes ? bytes - first : 0;
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(base)) + first, 0,

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kW4Block, w4_held_regs(DT == kF32 && !SPREAD, T, NB
     auto s_at = [&](unsigned tid, int pass, int i, unsigned size) CORAL_INLINE {
         const unsigned slot = pass * (kW4Held * NB * SLOTS) + tid % 32 + 32 * i;
         const unsigned at = tid / 32 * p.n_groups + (FINE ? slot : w4_group_of(p, slot));
-        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferEnd;
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferBehind;
         return at * size | behind;
     };
     constexpr unsigned W = DT == kF32 ? 4u : 2u;
@@ -541,7 +541,7 @@ __global__ __launch_bounds__(kW4Block, 2) void k_w4_rows(W4Params p) {
         const int e = i * kWave + fresh_lane();
         const unsigned slot = stage * STAGE_SLOTS + e % STAGE_SLOTS, g = FINE ? slot : w4_group_of(p, slot);
         const unsigned at = (unsigned)(e / STAGE_SLOTS) * (unsigned)p.n_groups + g;
-        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferEnd;         // (as in k_w4_held)
+        const unsigned behind = slot * (kW4UnitCols / SLOTS) < (unsigned)p.K ? 0u : kBufferBehind;         // (as in k_w4_held)
         s_raw[i] = buffer_read2(view, at * 2u | behind);
         if constexpr (ZERO) z_raw[i] = buffer_read1(z_view, at | behind);
     };
