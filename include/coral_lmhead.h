@@ -431,6 +431,153 @@ coral_status coral_logits_topk(const void *logits, const coral_logit_rules *rule
                                void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * A drafter's attention: queries and keys on their way into it, a cache of keys and values held in 4
+ * bits, attention over that cache (the nodes of a draft tree, single tokens of many sequences) and over
+ * whole prompts.  What these calls share:
+ *   - A head has head_dim = 64, 128 or 256 values.  q_heads is a multiple of kv_heads: query head h
+ *     reads the keys and values of head h / (q_heads / kv_heads).  At most 1024 heads of a kind.
+ *   - Rows of heads [T, heads, head_dim] may be columns of a wider matrix (a projection's output that
+ *     holds queries, keys and values): a stride is the distance of two tokens in elements, at least
+ *     heads * head_dim, and a multiple of 16 bytes, as the base is.
+ *   - T may be 0: such a call checks its other sizes, and does nothing.
+ *   - An output shares memory with no input, but where it says so.
+ */
+
+/*
+ * Norms of queries and keys for each head, and the rotation by their positions, in one pass:
+ *   y = x / sqrt(mean_d x[d]^2 + eps) * weight[d]              (where a weight is given)
+ *   (y[a], y[b]) = (y[a] cos - y[b] sin, y[b] cos + y[a] sin)  for the pair i = 0 .. rot_dim/2 - 1,
+ *       angle = positions[t] * inv_freq[i] (by a product in 64 bits: far positions keep their angle);
+ *       (a, b) = (i, i + rot_dim/2), or (2 i, 2 i + 1) where interleaved; values from rot_dim on stay
+ * in fp32, rounded once to the storage type.  With a cache the keys so made and the values are also
+ * appended to it, with the bits that coral_kv4_append gives for k_out and v.
+ *   q, k         [device] [T,q_heads,head_dim], [T,kv_heads,head_dim] storage type dt; one of them may
+ *                have no heads (and be NULL)
+ *   rope         [host]
+ *   q_out, k_out [device] out, as q and k; each may be its own input (same base and stride).  k_out may
+ *                be NULL with a cache
+ *   cache        [host] or NULL; v [device] [T,kv_heads,head_dim] and slots [device] [T] go with it
+ * rot_dim 0 leaves out the rotation.  eps >= 0.  Needs no workspace.
+ */
+typedef struct {
+    const void *q_weight;               /* [device] [head_dim] storage type, or NULL for no norm of queries */
+    const void *k_weight;               /* the same for keys; both 16-byte aligned */
+    const int32_t *positions;           /* [device] [T] */
+    const float *inv_freq;              /* [device] [rot_dim/2] radians for one position */
+    float eps;
+    int32_t rot_dim;                    /* even, 0..head_dim */
+    int32_t interleaved;
+} coral_rope;
+
+/*
+ * Keys and values held in 4 bits: values of e2m1 (as CORAL_W4_E2M1) times a power of two for every 32
+ * neighbouring values of a head, in pages of page_size tokens.  Token `slot` is place
+ * slot % page_size of page slot / page_size.  The struct is host memory.
+ *   codes  [device] [pages][kv_heads][page_size][head_dim/2] bytes, value 2j in the low half of byte j
+ *   scales [device] [pages][kv_heads][page_size][head_dim/32] bytes: the unit is 2^(byte - 127); bytes
+ *          above 252 count as 252
+ * page_size: a power of two from 16 to 4096; pages * page_size below 2^31; all four 16-byte aligned and
+ * apart from each other.
+ */
+typedef struct {
+    uint8_t *k_codes;
+    uint8_t *k_scales;
+    uint8_t *v_codes;
+    uint8_t *v_scales;
+    int32_t pages;
+    int32_t page_size;
+    int32_t kv_heads;
+    int32_t head_dim;
+} coral_kv4_cache;
+
+/*
+ * T tokens' keys and values into the cache.  The unit of 32 values is the power of two that puts the
+ * largest of them above 3.5 and at most at 7 units (at least 2^-126; at most 2^125, 2^13 for fp16: what
+ * is larger, infinities too, is held as 6 units); each value is then rounded to the nearest, ties to the
+ * even code.  A NaN is held as some finite value.  What coral_kv4_read gives is appended without loss.
+ *   k, v  [device] [T,kv_heads,head_dim] storage type dt
+ *   slots [device] [T] int32; a slot outside the cache is passed over (-1 for padding).  Of tokens with
+ *         the same slot in one call any may be held, in any mixture
+ * Needs no workspace.
+ */
+coral_status coral_kv4_append(const coral_kv4_cache *cache, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, const int32_t *slots, int T,
+                              coral_dtype dt, void *hip_stream);
+
+/*
+ * T tokens' keys and values out of the cache, as the values that are held, rounded to dt: a cached
+ * prefix for coral_attention_prompt, or the accepted nodes of a draft tree on their way to other slots.
+ *   slots        [device] [T]; rows of slots outside the cache are left as they were
+ *   k_out, v_out [device] out [T,kv_heads,head_dim] of dt, dense, 16-byte aligned
+ */
+coral_status coral_kv4_read(const coral_kv4_cache *cache, const int32_t *slots, int T,
+                            coral_dtype dt, void *k_out, void *v_out, void *hip_stream);
+
+coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                const coral_rope *rope, int T, int q_heads, int kv_heads,
+                                int head_dim, coral_dtype dt, void *q_out, int64_t q_out_stride,
+                                void *k_out, int64_t k_out_stride, const coral_kv4_cache *cache,
+                                const void *v, int64_t v_stride, const int32_t *slots,
+                                void *hip_stream);
+
+/*
+ * Attention over the 4-bit cache: the newest rows of S sequences, each over its own sequence's tokens.
+ *   out[t,h] = sum_j p_j v_j,  p = softmax over the tokens j that row t sees of scale * q[t,h] . k_j
+ * Rows q_offsets[s] .. q_offsets[s+1] are those of sequence s, n of them; token j of a sequence is place
+ * j % page_size of page page_table[s, j / page_size].  Row i of the n sees
+ *   without tree: tokens 0 .. lengths[s] - n + i     (its own, appended before the call, and all older)
+ *   with tree:    tokens 0 .. history[s] - 1, and token history[s] + b, where bit b of tree[t] is set, for
+ *                 b < 64: a draft tree's nodes see their ancestors and themselves
+ * and never a token from lengths[s] on.  A row that sees nothing is zero.  Products are exact but for the
+ * weights p, which keep 8 bits of a bf16 call (16 where a sequence has at most 16 rows of queries for a
+ * head of keys) and 16 or 24 of an fp16 or fp32 one; sums and statistics are fp32.
+ *   q          [device] [T,q_heads,head_dim] storage type dt
+ *   page_table [device] [S,max_pages] int32; tokens of a page that is none of the cache's are not seen
+ *   lengths    [device] [S] int32: tokens in the cache, the new ones among them; cut to 0 .. max_pages *
+ *              page_size
+ *   q_offsets  [device] [S+1] int32, ascending, cut to 0 .. T; rows of no sequence are left as they were,
+ *              and so are those of a sequence behind its first max_rows
+ *   history    [device] [S] int32 and tree [device] [T] words: both or neither
+ *   max_rows   1..64: the most rows of a sequence
+ *   max_length what the lengths may come to: the work is cut by it; longer sequences have right results too
+ *   out        [device] out [T,q_heads,head_dim] of dt, dense, 16-byte aligned
+ *   workspace  [device] at least coral_attention_kv4_workspace_bytes(...) bytes, 256-byte aligned; needs no
+ *              preparation, holds nothing between calls; two calls in flight at once must not share it
+ * Limits: 1 <= S <= 65535.  q must be finite: a row with other values has unspecified results, others not.
+ */
+size_t coral_attention_kv4_workspace_bytes(int S, int max_rows, int max_length, int q_heads,
+                                           int kv_heads, int head_dim, coral_dtype dt);
+
+coral_status coral_attention_kv4(const void *q, int64_t q_stride, const coral_kv4_cache *cache,
+                                 const int32_t *page_table, int max_pages, const int32_t *lengths,
+                                 const int32_t *q_offsets, const int32_t *history,
+                                 const uint64_t *tree, int T, int S, int max_rows, int max_length,
+                                 int q_heads, float scale, coral_dtype dt, void *out,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Causal attention over whole prompts of different lengths, packed one behind the other.
+ *   out[t,h] = sum_j p_j v_j,  p = softmax over j of scale * q[t,h] . k_j
+ * Sequence s has rows q_offsets[s] .. q_offsets[s+1] of q, n of them, and keys k_offsets[s] ..
+ * k_offsets[s+1], m of them; its row i sees keys 0 .. m - n + i (with m = n: itself and all before; with
+ * m > n: a prompt that goes on behind keys that are there; with m < n: the first n - m rows see nothing).
+ * A row that sees nothing is zero.  Scores, statistics and sums are fp32; the weights p are rounded to the
+ * storage type.
+ *   q    [device] [T,q_heads,head_dim], k and v [device] [keys,kv_heads,head_dim], storage type dt;
+ *        keys and values may be 0 tokens (and NULL); their strides at most 2^24 bytes
+ *   q_offsets, k_offsets [device] [S+1] int32, ascending, cut to 0 .. T and 0 .. keys; k_offsets NULL: the
+ *        same as q_offsets (keys = T).  Rows of no sequence are left as they were
+ *   out  [device] out [T,q_heads,head_dim] of dt, dense, 16-byte aligned
+ * Limits: S >= 1.  A key, a value or a query that is not finite makes the results of the rows that see it
+ * unspecified, of no other row.  Needs no workspace.
+ */
+coral_status coral_attention_prompt(const void *q, int64_t q_stride, const void *k,
+                                    int64_t k_stride, const void *v, int64_t v_stride,
+                                    const int32_t *q_offsets, const int32_t *k_offsets, int T,
+                                    int keys, int S, int q_heads, int kv_heads, int head_dim,
+                                    float scale, coral_dtype dt, void *out, void *hip_stream);
+
+/*
  * Measurement variants: identical to coral_lmhead_grouped / coral_lmhead_grouped_logprob /
  * coral_lmhead_dense (same operation of section 3.3, same arguments, same results), and in addition
  * bind two caller-created HIP events (hipEvent_t passed as void*, created with

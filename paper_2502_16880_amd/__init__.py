@@ -9,8 +9,9 @@ the import of this package fails.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import numpy as np
 import torch
@@ -35,6 +36,18 @@ class _GroupIndexStruct(ctypes.Structure):
                 ("group_offsets_host", ctypes.c_void_p),
                 ("group_offsets", ctypes.c_void_p),
                 ("group_rows", ctypes.c_void_p)]
+
+
+class _RopeStruct(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("inv_freq", ctypes.c_void_p), ("eps", ctypes.c_float), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32)]
+
+
+class _Kv4CacheStruct(ctypes.Structure):
+    _fields_ = [("k_codes", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_codes", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class _LogitRulesStruct(ctypes.Structure):
@@ -107,6 +120,21 @@ def _load():
     L.coral_logits_topk.restype = c.c_int
     L.coral_logits_topk.argtypes = [c.c_void_p, c.POINTER(_LogitRulesStruct)] + [c.c_int] * 4 + \
                                    [c.c_void_p] * 3 + [c.c_size_t, c.c_void_p]
+    p, i, i64 = c.c_void_p, c.c_int, c.c_int64
+    L.coral_qk_norm_rope.restype = c.c_int
+    L.coral_qk_norm_rope.argtypes = [p, i64, p, i64, c.POINTER(_RopeStruct), i, i, i, i, i, p, i64, p, i64,
+                                     c.POINTER(_Kv4CacheStruct), p, i64, p, p]
+    L.coral_kv4_append.restype = c.c_int
+    L.coral_kv4_append.argtypes = [c.POINTER(_Kv4CacheStruct), p, i64, p, i64, p, i, i, p]
+    L.coral_kv4_read.restype = c.c_int
+    L.coral_kv4_read.argtypes = [c.POINTER(_Kv4CacheStruct), p, i, i, p, p, p]
+    L.coral_attention_kv4_workspace_bytes.restype = c.c_size_t
+    L.coral_attention_kv4_workspace_bytes.argtypes = [i] * 7
+    L.coral_attention_kv4.restype = c.c_int
+    L.coral_attention_kv4.argtypes = [p, i64, c.POINTER(_Kv4CacheStruct), p, i, p, p, p, p, i, i, i, i, i, c.c_float, i, p, p,
+                                      c.c_size_t, p]
+    L.coral_attention_prompt.restype = c.c_int
+    L.coral_attention_prompt.argtypes = [p, i64, p, i64, p, i64, p, p, i, i, i, i, i, i, c.c_float, i, p, p]
     return L
 
 
@@ -666,3 +694,236 @@ def coral_logits_topk(logits: torch.Tensor, k: int, history: Optional[torch.Tens
              _same_device_ptr(topk_ids, "topk_ids", dev, torch.int32, (M, k)),
              _same_device_ptr(topk_logprob, "topk_logprob", dev, torch.float32, (M, k)), ws, workspace.numel())
     return topk_ids, topk_logprob
+
+
+# ---------------------------------------------------------------- a drafter's attention
+class KV4Cache(NamedTuple):
+    """Keys and values held in 4 bits (coral_kv4_cache of the C ABI), all uint8 and contiguous: codes
+    [pages, kv_heads, page_size, head_dim/2], scales [pages, kv_heads, page_size, head_dim/32].  The
+    calls take any tuple of these four."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def alloc_kv4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, device="cuda") -> KV4Cache:
+    """A cache of zeros."""
+    return KV4Cache(*(torch.zeros((pages, kv_heads, page_size, n), dtype=torch.uint8, device=device)
+                      for n in (head_dim // 2, head_dim // 32) * 2))
+
+
+def _kv4_cache(cache, device):
+    """(struct, pages, page_size, kv_heads, head_dim) of four checked tensors."""
+    k_codes, k_scales, v_codes, v_scales = cache
+    if k_codes.dim() != 4:
+        raise ValueError("the cache's codes must be [pages, kv_heads, page_size, head_dim/2]")
+    pages, kv_heads, page_size, half = k_codes.shape
+    if max(k_codes.shape) > _INT_MAX // 2:
+        raise ValueError("sizes must fit 32 bits")
+    u8, codes, scales = torch.uint8, (pages, kv_heads, page_size, half), (pages, kv_heads, page_size, half // 16)
+    struct = _Kv4CacheStruct(_same_device_ptr(k_codes, "k_codes", device, u8, codes),
+                             _same_device_ptr(k_scales, "k_scales", device, u8, scales),
+                             _same_device_ptr(v_codes, "v_codes", device, u8, codes),
+                             _same_device_ptr(v_scales, "v_scales", device, u8, scales), pages, page_size, kv_heads, half * 2)
+    return struct, pages, page_size, kv_heads, half * 2
+
+
+def _heads_ptr(t: torch.Tensor, name: str, device, dtype) -> Tuple[int, int]:
+    """(pointer, elements from token to token) of [T, heads, head_dim] with dense heads."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must live on {device}, got {t.device}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim], got {list(t.shape)}")
+    T, heads, D = t.shape
+    if max(t.shape) > _INT_MAX:
+        raise ValueError("sizes must fit 32 bits")
+    row, head, one = t.stride()
+    if t.numel() and ((D > 1 and one != 1) or (heads > 1 and head != D)):
+        raise ValueError(f"{name} must have its heads one behind the other (only the tokens may be further apart)")
+    return t.data_ptr(), row if T > 1 and heads and D else heads * D
+
+
+def _on_device(t: torch.Tensor, name: str):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live in device memory")
+    return t.device
+
+
+def coral_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                       inv_freq: Optional[torch.Tensor] = None, q_weight: Optional[torch.Tensor] = None,
+                       k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, interleaved: bool = False,
+                       q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, cache=None,
+                       v: Optional[torch.Tensor] = None, slots: Optional[torch.Tensor] = None, stream=None
+                       ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """coral_qk_norm_rope of the C ABI: (q, k) with each head's norm (weights [head_dim]; None: no norm) and
+    rotated by positions [T] int32 times inv_freq [rot_dim/2] float32 (both None: no rotation).
+
+    q [T,q_heads,head_dim] and k [T,kv_heads,head_dim] may be columns of a wider matrix, and one of them
+    None; q_out and k_out may be q and k themselves.  With cache (see KV4Cache), v [T,kv_heads,head_dim]
+    and slots [T] int32 the keys and values are appended to it too; k_out=False then leaves out the keys'
+    own output (None comes back)."""
+    first = q if q is not None else k
+    if first is None:
+        raise ValueError("q or k is needed")
+    dt, dev, dtype = _dtype_code(first), _on_device(first, "q" if q is not None else "k"), first.dtype
+    T, D = first.shape[0], first.shape[-1]
+    q_ptr, q_row = (None, 0) if q is None else _heads_ptr(q, "q", dev, dtype)
+    k_ptr, k_row = (None, 0) if k is None else _heads_ptr(k, "k", dev, dtype)
+    q_heads, kv_heads = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    if q is not None and k is not None and (k.shape[0] != T or k.shape[2] != D):
+        raise ValueError("q and k must have the same tokens and head_dim")
+    if (positions is None) != (inv_freq is None):
+        raise ValueError("positions and inv_freq go together")
+    rot = 0
+    if inv_freq is not None:
+        rot = 2 * inv_freq.numel()
+    rope = _RopeStruct(_same_device_ptr(q_weight, "q_weight", dev, dtype, (D,)),
+                       _same_device_ptr(k_weight, "k_weight", dev, dtype, (D,)),
+                       _same_device_ptr(positions, "positions", dev, torch.int32, (T,)),
+                       _same_device_ptr(inv_freq, "inv_freq", dev, torch.float32, None), float(eps), min(rot, _INT_MAX),
+                       1 if interleaved else 0)
+    struct, v_ptr, v_row, slot_ptr = None, None, 0, None
+    if cache is not None:
+        if k is None or v is None or slots is None:
+            raise ValueError("a cache goes with k, v and slots")
+        struct = _kv4_cache(cache, dev)[0]
+        v_ptr, v_row = _heads_ptr(v, "v", dev, dtype)
+        if v.shape != k.shape:
+            raise ValueError("v must have the shape of k")
+        slot_ptr = _same_device_ptr(slots, "slots", dev, torch.int32, (T,))
+    elif v is not None or slots is not None or k_out is False:
+        raise ValueError("v, slots and k_out=False go with a cache")
+    if q is None:
+        q_out = None
+    elif q_out is None:
+        q_out = _new(q.shape, dtype, dev, stream)
+    if k is None or k_out is False:
+        k_out = None
+    elif k_out is None:
+        k_out = _new(k.shape, dtype, dev, stream)
+    qo_ptr, qo_row = (None, 0) if q_out is None else _heads_ptr(q_out, "q_out", dev, dtype)
+    ko_ptr, ko_row = (None, 0) if k_out is None else _heads_ptr(k_out, "k_out", dev, dtype)
+    if (q_out is not None and q_out.shape != q.shape) or (k_out is not None and k_out.shape != k.shape):
+        raise ValueError("q_out and k_out must have the shapes of q and k")
+    _enqueue(_L.coral_qk_norm_rope, dev, stream, q_ptr, q_row, k_ptr, k_row, ctypes.byref(rope), T, q_heads, kv_heads, D, dt,
+             qo_ptr, qo_row, ko_ptr, ko_row, None if struct is None else ctypes.byref(struct), v_ptr, v_row, slot_ptr)
+    return q_out, k_out
+
+
+def coral_kv4_append(cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """coral_kv4_append of the C ABI: tokens' keys and values [T,kv_heads,head_dim] into the places slots [T]
+    int32 of the cache (page * page_size + place in the page; outside the cache: passed over)."""
+    dt, dev = _dtype_code(k), _on_device(k, "k")
+    struct, _, _, kv_heads, D = _kv4_cache(cache, dev)
+    k_ptr, k_row = _heads_ptr(k, "k", dev, k.dtype)
+    v_ptr, v_row = _heads_ptr(v, "v", dev, k.dtype)
+    if k.shape[1:] != (kv_heads, D) or v.shape != k.shape:
+        raise ValueError(f"k and v must be [T, {kv_heads}, {D}] as the cache is")
+    T = k.shape[0]
+    _enqueue(_L.coral_kv4_append, dev, stream, ctypes.byref(struct), k_ptr, k_row, v_ptr, v_row,
+             _same_device_ptr(slots, "slots", dev, torch.int32, (T,)), T, dt)
+
+
+def coral_kv4_read(cache, slots: torch.Tensor, dtype: torch.dtype, k_out: Optional[torch.Tensor] = None,
+                   v_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """coral_kv4_read of the C ABI: (k, v), each [T,kv_heads,head_dim] of dtype, as the cache holds them in the
+    places slots [T] int32.  Rows of slots outside the cache are left as k_out and v_out were."""
+    dev = _on_device(slots, "slots")
+    struct, _, _, kv_heads, D = _kv4_cache(cache, dev)
+    slot_ptr = _same_device_ptr(slots, "slots", dev, torch.int32, None)
+    T = slots.numel()
+    if T > _INT_MAX:
+        raise ValueError("sizes must fit 32 bits")
+    if k_out is None:
+        k_out = _new((T, kv_heads, D), dtype, dev, stream)
+    if v_out is None:
+        v_out = _new((T, kv_heads, D), dtype, dev, stream)
+    dt = _dtype_code(k_out)
+    _enqueue(_L.coral_kv4_read, dev, stream, ctypes.byref(struct), slot_ptr, T, dt,
+             _same_device_ptr(k_out, "k_out", dev, dtype, (T, kv_heads, D)),
+             _same_device_ptr(v_out, "v_out", dev, dtype, (T, kv_heads, D)))
+    return k_out, v_out
+
+
+KV4_MAX_ROWS = 64                    # rows of a sequence in one call of attention over the cache
+
+
+def coral_attention_kv4_workspace_bytes(S: int, max_rows: int, max_length: int, q_heads: int, kv_heads: int, head_dim: int,
+                                        dt: int) -> int:
+    if not 0 <= min(S, max_rows, max_length, q_heads, kv_heads, head_dim) <= max(S, max_rows, max_length, q_heads, kv_heads, head_dim) <= _INT_MAX:
+        return 0
+    return int(_L.coral_attention_kv4_workspace_bytes(S, max_rows, max_length, q_heads, kv_heads, head_dim, dt))
+
+
+def _scale_of(scale: Optional[float], head_dim: int) -> float:
+    return 1.0 / math.sqrt(head_dim) if scale is None else float(scale)
+
+
+def coral_attention_kv4(q: torch.Tensor, cache, page_table: torch.Tensor, lengths: torch.Tensor, q_offsets: torch.Tensor,
+                        max_rows: int, max_length: Optional[int] = None, history: Optional[torch.Tensor] = None,
+                        tree: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                        out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """coral_attention_kv4 of the C ABI: attention of q [T,q_heads,head_dim] over the 4-bit cache, [T,q_heads,head_dim].
+
+    Sequence s has rows q_offsets[s] .. q_offsets[s+1] (int32 [S+1]; at most max_rows, 64), lengths[s] cached tokens
+    (int32 [S], the rows' own among them) in pages page_table[s] (int32 [S,max_pages]).  Without tree a row sees itself
+    and all older tokens; with history (int32 [S]) and tree (int64 [T]) the tokens before history[s], and of the 64 from
+    there on those whose bit is set.  max_length: what the lengths may come to (None: what the page table holds).
+    scale: None for 1/sqrt(head_dim).  workspace: plain scratch of coral_attention_kv4_workspace_bytes, not shared by
+    calls that may overlap; None allocates one."""
+    dt, dev = _dtype_code(q), _on_device(q, "q")
+    struct, _, page_size, kv_heads, D = _kv4_cache(cache, dev)
+    q_ptr, q_row = _heads_ptr(q, "q", dev, q.dtype)
+    T, q_heads = q.shape[:2]
+    if q.shape[2] != D:
+        raise ValueError(f"q must be [T, q_heads, {D}] as the cache is")
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [S, max_pages]")
+    S, max_pages = page_table.shape
+    i32, max_rows = torch.int32, int(max_rows)
+    max_length = min(max_pages * page_size, _INT_MAX) if max_length is None else int(max_length)
+    if max(S, max_pages, abs(max_rows), abs(max_length)) > _INT_MAX:
+        raise ValueError("sizes must fit 32 bits")
+    args = (_same_device_ptr(page_table, "page_table", dev, i32, (S, max_pages)), max_pages,
+            _same_device_ptr(lengths, "lengths", dev, i32, (S,)), _same_device_ptr(q_offsets, "q_offsets", dev, i32, (S + 1,)),
+            _same_device_ptr(history, "history", dev, i32, (S,)), _same_device_ptr(tree, "tree", dev, torch.int64, (T,)))
+    if out is None:
+        out = _new((T, q_heads, D), q.dtype, dev, stream)
+    if workspace is None:
+        workspace = _new((coral_attention_kv4_workspace_bytes(S, max_rows, max_length, q_heads, kv_heads, D, dt),), torch.uint8, dev, stream)
+    _enqueue(_L.coral_attention_kv4, dev, stream, q_ptr, q_row, ctypes.byref(struct), *args, T, S, max_rows, max_length, q_heads,
+             _scale_of(scale, D), dt, _same_device_ptr(out, "out", dev, q.dtype, (T, q_heads, D)),
+             _same_device_ptr(workspace, "workspace", dev, torch.uint8, None), workspace.numel())
+    return out
+
+
+def coral_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                           k_offsets: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                           out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """coral_attention_prompt of the C ABI: causal attention over packed sequences, [T,q_heads,head_dim].
+
+    q [T,q_heads,head_dim]; k and v [keys,kv_heads,head_dim]; sequence s has rows q_offsets[s] .. q_offsets[s+1] (int32
+    [S+1]) and keys k_offsets[s] .. k_offsets[s+1] (None: the same), its last row sees its last key.  scale: None for
+    1/sqrt(head_dim)."""
+    dt, dev = _dtype_code(q), _on_device(q, "q")
+    q_ptr, q_row = _heads_ptr(q, "q", dev, q.dtype)
+    k_ptr, k_row = _heads_ptr(k, "k", dev, q.dtype)
+    v_ptr, v_row = _heads_ptr(v, "v", dev, q.dtype)
+    T, q_heads, D = q.shape
+    keys, kv_heads = k.shape[:2]
+    if k.shape[2] != D or v.shape != k.shape:
+        raise ValueError("k and v must have one shape, and q's head_dim")
+    S = q_offsets.numel() - 1
+    if S > _INT_MAX:
+        raise ValueError("sizes must fit 32 bits")
+    args = (_same_device_ptr(q_offsets, "q_offsets", dev, torch.int32, (S + 1,)),
+            _same_device_ptr(k_offsets, "k_offsets", dev, torch.int32, (S + 1,)))
+    if out is None:
+        out = _new((T, q_heads, D), q.dtype, dev, stream)
+    _enqueue(_L.coral_attention_prompt, dev, stream, q_ptr, q_row, k_ptr, k_row, v_ptr, v_row, *args, T, keys, S, q_heads,
+             kv_heads, D, _scale_of(scale, D), dt, _same_device_ptr(out, "out", dev, q.dtype, (T, q_heads, D)))
+    return out

@@ -1,0 +1,86 @@
+// Entry point of attention over the 4-bit cache (kernels: kv4_attention.h).
+#include "kv4_attention.h"
+
+#include <math.h>
+
+#include <initializer_list>
+
+#include "kv4_kernels.h"
+
+namespace {
+
+constexpr int kMostSequences = 65535;
+
+// Sizes that the plan is made of; false where one is out of range.
+coral_status check_kv4_sizes(int T, int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim, coral_dtype dt) {
+    if (!storage_known(dt) || T < 0 || S < 1 || max_rows < 1 || max_length < 0 || q_heads < 1 || kv_heads < 1 || head_dim < 1) return CORAL_ERR_SHAPE;
+    if (q_heads % kv_heads) return CORAL_ERR_SHAPE;
+    if (!head_dim_known(head_dim) || q_heads > kMostHeads || S > kMostSequences || max_rows > kKv4MostRows) return CORAL_ERR_UNSUPPORTED;
+    return CORAL_OK;
+}
+int query_terms(coral_dtype dt) { return dt == CORAL_BF16 ? 1 : dt == CORAL_F16 ? 2 : 3; }
+
+}  // namespace
+
+extern "C" size_t coral_attention_kv4_workspace_bytes(int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim,
+                                                      coral_dtype dt) {
+    if (check_kv4_sizes(0, S, max_rows, max_length, q_heads, kv_heads, head_dim, dt) != CORAL_OK) return 0;
+    const size_t n = kv4_workspace(kv4_plan(S, max_rows, max_length, q_heads, kv_heads, head_dim, query_terms(dt)), S, kv_heads, head_dim);
+    return n < 256 ? 256 : (n + 255) / 256 * 256;
+}
+
+extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, const coral_kv4_cache* cache, const int32_t* page_table,
+                                            int max_pages, const int32_t* lengths, const int32_t* q_offsets, const int32_t* history,
+                                            const uint64_t* tree, int T, int S, int max_rows, int max_length, int q_heads, float scale,
+                                            coral_dtype dt, void* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+    Kv4AttnParams p = {};
+    coral_status st = check_kv4(cache, &p.cache);
+    if (st != CORAL_OK) return st;
+    const int kv_heads = cache->kv_heads, head_dim = cache->head_dim;
+    if ((st = check_kv4_sizes(T, S, max_rows, max_length, q_heads, kv_heads, head_dim, dt)) != CORAL_OK) return st;
+    if (max_pages < 0 || !isfinite(scale)) return CORAL_ERR_SHAPE;
+    if ((tree == nullptr) != (history == nullptr)) return CORAL_ERR_NULL;
+    if (T == 0) return CORAL_OK;
+    Rows in_q, out_rows, parts[4];
+    if ((st = check_rows(q, q_stride, q_heads, head_dim, dt, T, &in_q)) != CORAL_OK) return st;
+    if ((st = check_rows(out, (int64_t)q_heads * head_dim, q_heads, head_dim, dt, T, &out_rows)) != CORAL_OK) return st;
+    if ((max_pages > 0 && !page_table) || !lengths || !q_offsets) return CORAL_ERR_NULL;
+    if (((uintptr_t)page_table | (uintptr_t)lengths | (uintptr_t)q_offsets | (uintptr_t)history) & 3u) return CORAL_ERR_UNSUPPORTED;
+    if ((uintptr_t)tree & 7u) return CORAL_ERR_UNSUPPORTED;
+    const Kv4Plan plan = kv4_plan(S, max_rows, max_length, q_heads, kv_heads, head_dim, query_terms(dt));
+    if ((int64_t)kv_heads * plan.row_blocks > 65535) return CORAL_ERR_UNSUPPORTED;
+    const size_t need = kv4_workspace(plan, S, kv_heads, head_dim);
+    if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return CORAL_ERR_WORKSPACE;
+    kv4_parts(cache, parts);
+    auto whole = [](const void* base, int64_t bytes) { return Rows{base, bytes, bytes, 1}; };
+    const Rows inputs[10] = {in_q, parts[0], parts[1], parts[2], parts[3], whole(page_table, (int64_t)S * max_pages * 4), whole(lengths, S * 4ll),
+                             whole(q_offsets, (S + 1) * 4ll), whole(history, S * 4ll), whole(tree, T * 8ll)};
+    const Rows scratch = whole(need ? workspace : nullptr, (int64_t)need);
+    for (const Rows& r : inputs)
+        if (rows_overlap(out_rows, r) || rows_overlap(scratch, r)) return CORAL_ERR_UNSUPPORTED;
+    if (rows_overlap(out_rows, scratch)) return CORAL_ERR_UNSUPPORTED;
+    p.q = static_cast<const char*>(q);
+    p.out = static_cast<char*>(out);
+    p.q_stride = in_q.stride;
+    p.out_stride = out_rows.stride;
+    p.page_table = page_table; p.lengths = lengths; p.q_offsets = q_offsets; p.history = history; p.tree = tree;
+    p.max_pages = max_pages; p.T = T; p.max_rows = max_rows; p.group = q_heads / kv_heads; p.kv_heads = kv_heads; p.q_heads = q_heads;
+    p.row_blocks = plan.row_blocks; p.splits = plan.splits;
+    p.scale_log2 = scale * kLog2e;
+    if (need) {
+        const size_t rows = (size_t)S * kv_heads * plan.row_blocks * plan.splits * 16 * plan.tiles;
+        p.part = static_cast<float*>(workspace);
+        p.part_stats = reinterpret_cast<float2*>(p.part + rows * head_dim);
+    }
+    const void* fn = dt == CORAL_F32 ? coral_kv4_kernel_f32(head_dim, plan.tiles) : dt == CORAL_BF16 ? coral_kv4_kernel_bf16(head_dim, plan.tiles)
+                                                                                                    : coral_kv4_kernel_f16(head_dim, plan.tiles);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    hipLaunchKernelGGL(reinterpret_cast<kv4_attn_fn>(const_cast<void*>(fn)), dim3(plan.splits, kv_heads * plan.row_blocks, S), dim3(kKv4Threads), 0, stream, p);
+    if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
+    if (plan.splits > 1) {
+        const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim) : coral_kv4_join_f16(head_dim);
+        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(q_heads, max_rows, S), dim3(kKv4Threads), 0, stream, p, plan.tiles);
+        if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
+    }
+    return CORAL_OK;
+}

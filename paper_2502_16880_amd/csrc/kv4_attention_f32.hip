@@ -1,0 +1,10 @@
+// Kernels of attention over the 4-bit cache for f32 queries.
+#include "kv4_attention.h"
+#include "kv4_kernels.h"
+
+const void* coral_kv4_kernel_f32(int head_dim, int tiles) {
+    return reinterpret_cast<const void*>(head_dim == 64 ? kv4_kernel<kF32, 64>(tiles) : head_dim == 128 ? kv4_kernel<kF32, 128>(tiles) : kv4_kernel<kF32, 256>(tiles));
+}
+const void* coral_kv4_join_f32(int head_dim) {
+    return reinterpret_cast<const void*>(head_dim == 64 ? k_kv4_join<kF32, 64> : head_dim == 128 ? k_kv4_join<kF32, 128> : k_kv4_join<kF32, 256>);
+}

@@ -1,0 +1,394 @@
+// Causal attention over whole prompts, packed one behind the other.
+//
+//   out[t,h] = sum_j p_j v_j,  p = softmax_j(scale * q[t,h] . k_j)  over j <= m - n + i for row i of a sequence
+//   of n rows and m keys
+//
+// A workgroup takes 128 rows (fp32: 64) of one sequence and head and passes over the keys once, 64 at a time
+// (D = 256: 32), with the running largest score and sum of each row; a wave's rows, their sums and
+// weights never leave its registers.  Scores are taken as K Q^T, so that keys lie along a lane's registers
+// and rows along the lanes: that is how the second product, V^T P^T, wants its weights, and a row's maximum
+// is one exchange between halves of the wave.  Keys and values go through LDS once for all waves, in 16-byte
+// pieces whose place in a row is exchanged by the row's number, so that neither the reading of keys (16 rows, one
+// piece each) nor the transposing one of values (four rows, four pieces each) meets a bank twice.
+#pragma once
+#include "attention_common.h"
+
+namespace {
+
+constexpr int kPromptThreads = 256;
+constexpr int kPromptWaves = kPromptThreads / kWave;
+constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
+constexpr int kXcds = 8;
+
+typedef __attribute__((ext_vector_type(16))) float f32x16_t;
+typedef __attribute__((ext_vector_type(4))) short s16x4_t;
+
+struct PromptParams {
+    const char *q, *k, *v;
+    char* out;
+    int64_t q_stride, k_stride, v_stride, out_stride;        // bytes from token to token
+    const int32_t *q_offsets, *k_offsets;
+    int T, keys, S, q_heads, group, tiles;                   // tiles: of rows, at most, over all sequences
+    float scale_log2;                                        // above zero; the sign is taken by q
+    unsigned q_sign;                                         // bit to flip in every value of q
+};
+
+// Which rows a workgroup takes: sequences' tiles are counted in order.
+struct PromptTile {
+    int row0, rows, first, k0, keys;                         // the sequence's rows and keys, and the tile's first row in it
+    bool any;
+};
+template <int ROWS>
+__device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int tile, int lane) {
+    PromptTile r;
+    r.any = false;
+    r.row0 = r.rows = r.first = r.k0 = r.keys = 0;
+    int before = 0;
+    for (int s0 = 0; s0 < p.S; s0 += kWave) {
+        const int s = s0 + lane;
+        int n = 0, a = 0;
+        if (s < p.S) {
+            a = p.q_offsets[s];
+            const int b = p.q_offsets[s + 1];
+            a = a < 0 ? 0 : a > p.T ? p.T : a;
+            n = (b > p.T ? p.T : b) - a;
+            n = n < 0 ? 0 : n;
+        }
+        const int count = (n + ROWS - 1) / ROWS, upto = before + wave_scan_inclusive(count);
+        const uint64_t found = __builtin_amdgcn_ballot_w64(tile < upto);
+        if (found) {
+            const int src = __builtin_ctzll(found);
+            r.row0 = __builtin_amdgcn_readlane(a, src);
+            r.rows = __builtin_amdgcn_readlane(n, src);
+            const int at = tile - (__builtin_amdgcn_readlane(upto, src) - __builtin_amdgcn_readlane(count, src));
+            r.first = ((r.rows + ROWS - 1) / ROWS - 1 - at) * ROWS;      // the last rows, which see most, first
+            r.any = r.first >= 0;
+            const int seq = s0 + src;
+            if (p.k_offsets) {
+                const int ka = p.k_offsets[seq], kb = p.k_offsets[seq + 1];
+                r.k0 = ka < 0 ? 0 : ka > p.keys ? p.keys : ka;
+                r.keys = (kb > p.keys ? p.keys : kb) - r.k0;
+                r.keys = r.keys < 0 ? 0 : r.keys;
+            } else {
+                r.k0 = r.row0;
+                r.keys = r.rows;
+            }
+            return r;
+        }
+        before = __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    return r;
+}
+
+// Workgroups are dealt to the eight dies in turn; each die takes neighbouring (head, tile) pairs, so that the
+// keys of one head are read through one L2.
+__device__ __forceinline__ int prompt_unit(int x, int units) {
+    const int per = (units + kXcds - 1) / kXcds, u = x % kXcds * per + x / kXcds;
+    return x / kXcds < per && u < units ? u : -1;
+}
+
+// Place of 16-byte piece c of row r in LDS (bytes), rows of `pieces` pieces.
+template <int PIECES>
+__device__ __forceinline__ int prompt_place(int r, int c) {
+    const int f = PIECES == 8 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+    return (r * PIECES + (c ^ f)) * 16;
+}
+
+template <int DT>
+__device__ __forceinline__ f32x16_t mfma_32(uint4 a, uint4 b, f32x16_t acc) {
+    if (DT == kF16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+}
+__device__ __forceinline__ uint2 prompt_transposed(const char* at) {
+    const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(at));
+    return __builtin_bit_cast(uint2, r);
+}
+
+// Two 16-bit values, those that are infinite or NaN made zero; `odd` tells whether there were any.
+template <int DT>
+__device__ __forceinline__ unsigned only_finite2(unsigned w, bool& odd) {
+    const unsigned e = DT == kF16 ? 0x7c00u : 0x7f80u;
+    const bool lo = (w & e) == e, hi = (w >> 16 & e) == e;
+    odd |= lo | hi;
+    return (lo ? 0u : w & 0xffffu) | (hi ? 0u : w & 0xffff0000u);
+}
+__device__ __forceinline__ unsigned only_finite(unsigned w, bool& odd) {
+    const bool bad = (w & 0x7f800000u) == 0x7f800000u;
+    odd |= bad;
+    return bad ? 0u : w;
+}
+// Keys 0 .. most of a tile, one bit each.
+__device__ __forceinline__ unsigned long long keys_to(int most) { return most < 0 ? 0ull : most > 62 ? ~0ull : (2ull << most) - 1ull; }
+
+// 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
+// (2^-12) each with random signs, which come to about the result's own rounding.
+template <int DT, int D>
+__global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(PromptParams p) {
+    constexpr int BN = D == 256 ? 32 : 64, ROWS = 128, PIECES = D / 8, LOADS = BN * PIECES / kPromptThreads;
+    constexpr int QC = D / 16, KT = BN / 32, DT32 = D / 32, kTile = BN * D * 2;
+    __shared__ __align__(256) char lds[2][2][kTile];             // [buffer][keys, values]
+    __shared__ unsigned long long odd[4];                        // of a tile that rows see a part of: keys whose values are not finite
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int col = lane & 31, h = lane >> 5;
+    const int unit = prompt_unit(blockIdx.x, p.q_heads * p.tiles);
+    if (unit < 0) return;
+    const int head = unit / p.tiles;
+    const PromptTile t = prompt_tile<ROWS>(p, unit % p.tiles, lane);
+    if (!t.any) return;
+    const int reach = t.keys - t.rows;                           // row i sees keys up to reach + i
+    const int last = t.first + ROWS < t.rows ? t.first + ROWS : t.rows;
+    const int n_keys = reach + last < 0 ? 0 : reach + last;      // keys that some row of the tile sees
+    const int n_tiles = (n_keys + BN - 1) / BN;
+    const int my_first = t.first + wave * 32, row = my_first + col;
+
+    uint4 q[QC];
+    {
+        const char* from = p.q + (int64_t)(t.row0 + row) * p.q_stride + (int64_t)head * (D * 2) + h * 16;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            q[c] = make_uint4(0, 0, 0, 0);
+            if (row < t.rows) q[c] = load_vec(reinterpret_cast<const uint4*>(from + c * 32));
+            q[c].x ^= p.q_sign; q[c].y ^= p.q_sign; q[c].z ^= p.q_sign; q[c].w ^= p.q_sign;
+        }
+    }
+    const int64_t kv_head = head / p.group;
+    const char* k_base = p.k + (int64_t)t.k0 * p.k_stride + kv_head * (D * 2);
+    const char* v_base = p.v + (int64_t)t.k0 * p.v_stride + kv_head * (D * 2);
+    const size_t k_bytes = t.keys ? (size_t)(t.keys - 1) * p.k_stride + D * 2 : 0, v_bytes = t.keys ? (size_t)(t.keys - 1) * p.v_stride + D * 2 : 0;
+    uint4 next_k[LOADS], next_v[LOADS];
+    auto fetch = [&](int tile) CORAL_INLINE {
+        const Buffer kb = buffer_view(k_base, (size_t)tile * BN * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)tile * BN * p.v_stride, v_bytes);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
+            next_k[i] = buffer_read16(kb, (unsigned)(r * (int)p.k_stride + c * 16));
+            next_v[i] = buffer_read16(vb, (unsigned)(r * (int)p.v_stride + c * 16));
+        }
+    };
+    // From this tile on some rows see a part of a tile.  A product of 0 and infinity must not reach the rows that do not
+    // see the value: it is made zero, and the rows that see it become NaN by the key's bit.
+    const int first_cut = (reach + t.first + 1 < 0 ? 0 : reach + t.first + 1) / BN;
+    auto put = [&](int tile) CORAL_INLINE {
+        char* to = lds[tile & 1][0];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * kPromptThreads + threadIdx.x, place = prompt_place<PIECES>(at / PIECES, at % PIECES);
+            if (tile >= first_cut) {
+                bool bad = false;
+                next_v[i].x = only_finite2<DT>(next_v[i].x, bad);
+                next_v[i].y = only_finite2<DT>(next_v[i].y, bad);
+                next_v[i].z = only_finite2<DT>(next_v[i].z, bad);
+                next_v[i].w = only_finite2<DT>(next_v[i].w, bad);
+                if (bad) atomicOr(&odd[tile & 3], 1ull << (at / PIECES));
+            }
+            store_vec(reinterpret_cast<uint4*>(to + place), next_k[i]);
+            store_vec(reinterpret_cast<uint4*>(to + kTile + place), next_v[i]);
+        }
+    };
+    f32x16_t sum[DT32];
+#pragma unroll
+    for (int d = 0; d < DT32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[d][i] = 0.f;
+    float ref = -INFINITY, total = 0.f;
+    if (threadIdx.x < 4) odd[threadIdx.x] = 0;
+    __syncthreads();
+    if (n_tiles > 0) {
+        fetch(0);
+        put(0);
+    }
+    __syncthreads();
+    for (int j = 0; j < n_tiles; ++j) {
+        const char *keys = lds[j & 1][0], *values = lds[j & 1][1];
+        if (j + 1 < n_tiles) fetch(j + 1);
+        if (threadIdx.x == 0) odd[(j + 2) & 3] = 0;              // tile j - 2's; put(j + 2) comes behind the barrier
+        const int k0 = j * BN;
+        if (k0 <= reach + my_first + 31 && my_first < t.rows) {  // some row of the wave sees some key of the tile (uniform)
+            f32x16_t s[KT];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
+#pragma unroll
+                for (int c = 0; c < QC; ++c)
+                    s[kt] = mfma_32<DT>(load_vec(reinterpret_cast<const uint4*>(keys + prompt_place<PIECES>(kt * 32 + col, 2 * c + h))), q[c], s[kt]);
+            }
+            const bool cut = k0 + BN - 1 > reach + my_first;
+            if (cut) {
+                const int most = reach + row - k0;               // newest key of the tile that the row sees
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (kt * 32 + 8 * (i / 4) + 4 * h + i % 4 > most) s[kt][i] = -INFINITY;
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
+            top = lane_xor_max<32>(top) * p.scale_log2;
+            const bool move = top > ref + kPromptMoveAt || (ref == -INFINITY && top > -INFINITY);
+            if (__builtin_amdgcn_ballot_w64(move)) {
+                const float to = move ? top : ref, by = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to), keep = move ? by : 1.f;
+                ref = to;
+                total *= keep;
+#pragma unroll
+                for (int d = 0; d < DT32; ++d) sum[d] *= keep;
+            }
+            const float base = ref == -INFINITY ? 0.f : ref;
+            uint4 w[BN / 16];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                float e[16], part = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[kt][i], p.scale_log2, -base));
+                    part += e[i];
+                }
+                total += part;
+                w[2 * kt] = make_uint4(narrow2<DT>(e[0], e[1]), narrow2<DT>(e[2], e[3]), narrow2<DT>(e[4], e[5]), narrow2<DT>(e[6], e[7]));
+                w[2 * kt + 1] = make_uint4(narrow2<DT>(e[8], e[9]), narrow2<DT>(e[10], e[11]), narrow2<DT>(e[12], e[13]), narrow2<DT>(e[14], e[15]));
+            }
+            // the values' operand: column 32 d + lane % 32, keys 16 c + 4 h + 0..3 and 16 c + 8 + 4 h + 0..3
+            const int quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2, in = (lane & 1) * 8, r = 4 * h + (lane & 15) / 4;
+            auto operand = [&](int d, int c) CORAL_INLINE {
+                const uint2 lo = prompt_transposed(values + prompt_place<PIECES>(16 * c + r, 4 * d + quad) + in);
+                const uint2 hi = prompt_transposed(values + prompt_place<PIECES>(16 * c + 8 + r, 4 * d + quad) + in);
+                return make_uint4(lo.x, lo.y, hi.x, hi.y);
+            };
+            if (j >= first_cut && (odd[j & 3] & keys_to(reach + row - k0))) total = NAN;
+#pragma unroll
+            for (int d = 0; d < DT32; ++d)
+#pragma unroll
+                for (int c = 0; c < BN / 16; ++c) sum[d] = mfma_32<DT>(operand(d, c), w[c], sum[d]);
+        }
+        if (j + 1 < n_tiles) put(j + 1);
+        __syncthreads();
+    }
+    total = lane_xor_sum<32>(total);
+    if (row >= t.rows) return;
+    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;          // a row that sees nothing: zeros
+    char* to = p.out + (int64_t)(t.row0 + row) * p.out_stride + (int64_t)head * (D * 2) + h * 8;
+#pragma unroll
+    for (int d = 0; d < DT32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<uint2*>(to + (d * 32 + 2 * i) * 2) =
+                make_uint2(narrow2<DT>(sum[d][i] * inv, sum[d][i + 1] * inv), narrow2<DT>(sum[d][i + 2] * inv, sum[d][i + 3] * inv));
+}
+
+// fp32 on the matrix cores' fp32 products (a sixteenth of the 16-bit rate): 16 rows a wave, 32 keys at a time, no
+// rounding of the weights.  One value a lane and product: lane (key or column, g) has the g-th of four.
+template <int D>
+__global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
+    constexpr int BN = 32, ROWS = 64, PIECES = D / 4, LOADS = BN * PIECES / kPromptThreads, QC = D / 16, DTILES = D / 16, kRow = D + 4;
+    __shared__ __align__(16) float k_lds[BN][kRow], v_lds[BN][kRow];
+    __shared__ unsigned long long odd[2];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int col = lane & 15, g = lane >> 4;
+    const int unit = prompt_unit(blockIdx.x, p.q_heads * p.tiles);
+    if (unit < 0) return;
+    const int head = unit / p.tiles;
+    const PromptTile t = prompt_tile<ROWS>(p, unit % p.tiles, lane);
+    if (!t.any) return;
+    const int reach = t.keys - t.rows, last = t.first + ROWS < t.rows ? t.first + ROWS : t.rows;
+    const int n_keys = reach + last < 0 ? 0 : reach + last, n_tiles = (n_keys + BN - 1) / BN;
+    const int my_first = t.first + wave * 16, row = my_first + col;
+    uint4 q[QC];
+    {
+        const char* from = p.q + (int64_t)(t.row0 + row) * p.q_stride + (int64_t)head * (D * 4) + g * 16;
+#pragma unroll
+        for (int c = 0; c < QC; ++c) {
+            q[c] = make_uint4(0, 0, 0, 0);
+            if (row < t.rows) q[c] = load_vec(reinterpret_cast<const uint4*>(from + c * 64));
+            q[c].x ^= p.q_sign; q[c].y ^= p.q_sign; q[c].z ^= p.q_sign; q[c].w ^= p.q_sign;
+        }
+    }
+    const int64_t kv_head = head / p.group;
+    const char* k_base = p.k + (int64_t)t.k0 * p.k_stride + kv_head * (D * 4);
+    const char* v_base = p.v + (int64_t)t.k0 * p.v_stride + kv_head * (D * 4);
+    const size_t k_bytes = t.keys ? (size_t)(t.keys - 1) * p.k_stride + D * 4 : 0, v_bytes = t.keys ? (size_t)(t.keys - 1) * p.v_stride + D * 4 : 0;
+    f32x4_t sum[DTILES];
+#pragma unroll
+    for (int d = 0; d < DTILES; ++d) sum[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float ref = -INFINITY, total = 0.f;
+    const int first_cut = (reach + t.first + 1 < 0 ? 0 : reach + t.first + 1) / BN;       // as in k_prompt
+    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+    for (int j = 0; j < n_tiles; ++j) {
+        const int k0 = j * BN;
+        const Buffer kb = buffer_view(k_base, (size_t)k0 * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)k0 * p.v_stride, v_bytes);
+        uint4 nk[LOADS], nv[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
+            nk[i] = buffer_read16(kb, (unsigned)(r * (int)p.k_stride + c * 16));
+            nv[i] = buffer_read16(vb, (unsigned)(r * (int)p.v_stride + c * 16));
+        }
+        __syncthreads();                                         // the tile before has been read
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
+            if (j >= first_cut) {
+                bool bad = false;
+                nv[i].x = only_finite(nv[i].x, bad);
+                nv[i].y = only_finite(nv[i].y, bad);
+                nv[i].z = only_finite(nv[i].z, bad);
+                nv[i].w = only_finite(nv[i].w, bad);
+                if (bad) atomicOr(&odd[j & 1], 1ull << r);
+            }
+            store_vec(reinterpret_cast<uint4*>(&k_lds[r][c * 4]), nk[i]);
+            store_vec(reinterpret_cast<uint4*>(&v_lds[r][c * 4]), nv[i]);
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) odd[(j + 1) & 1] = 0;              // read before the barrier above, written behind the next one
+        if (k0 > reach + my_first + 15 || my_first >= t.rows) continue;      // uniform over the wave
+        f32x4_t s[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < QC; ++c)
+                s[i] = mfma_tile<kF32>(load_vec(reinterpret_cast<const uint4*>(&k_lds[i * 16 + col][c * 16 + 4 * g])), q[c], s[i]);
+        }
+        const bool cut = k0 + BN - 1 > reach + my_first;
+        const int most = reach + row - k0;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = s[i / 4][i % 4] * p.scale_log2;
+            if (cut && (i / 4) * 16 + 4 * g + i % 4 > most) x[i] = -INFINITY;
+        }
+        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+        top = lane_xor_max<16>(lane_xor_max<32>(top));
+        const bool move = top > ref + kPromptMoveAt || (ref == -INFINITY && top > -INFINITY);
+        if (__builtin_amdgcn_ballot_w64(move)) {
+            const float to = move ? top : ref, by = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to), keep = move ? by : 1.f;
+            ref = to;
+            total *= keep;
+#pragma unroll
+            for (int d = 0; d < DTILES; ++d) sum[d] *= keep;
+        }
+        const float base = ref == -INFINITY ? 0.f : ref;
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(x[i] - base);
+            total += w[i];
+        }
+        if (j >= first_cut && (odd[j & 1] & keys_to(most))) total = NAN;
+#pragma unroll
+        for (int d = 0; d < DTILES; ++d)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                sum[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v_lds[(i / 4) * 16 + 4 * g + i % 4][d * 16 + col], w[i], sum[d], 0, 0, 0);
+    }
+    total = lane_xor_sum<16>(lane_xor_sum<32>(total));
+    if (row >= t.rows) return;
+    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
+    char* to = p.out + (int64_t)(t.row0 + row) * p.out_stride + (int64_t)head * (D * 4) + g * 16;
+#pragma unroll
+    for (int d = 0; d < DTILES; ++d) *reinterpret_cast<f32x4_t*>(to + d * 64) = sum[d] * inv;
+}
+
+}  // namespace
