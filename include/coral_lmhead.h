@@ -541,8 +541,9 @@ coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, 
  *   max_rows   1..64: the most rows of a sequence
  *   max_length what the lengths may come to: the work is cut by it; longer sequences have right results too
  *   out        [device] out [T,q_heads,head_dim] of dt, dense, 16-byte aligned
- *   workspace  [device] at least coral_attention_kv4_workspace_bytes(...) bytes, 256-byte aligned; needs no
- *              preparation, holds nothing between calls; two calls in flight at once must not share it
+ *   workspace  [device] at least coral_attention_kv4_workspace_bytes(...) bytes, 256-byte aligned, prepared once by
+ *              coral_lmhead_workspace_init with at least that many bytes (or filled with zeros); one of the
+ *              heads' serves too, for calls that do not overlap
  * Limits: 1 <= S <= 65535.  q must be finite: a row with other values has unspecified results, others not.
  */
 size_t coral_attention_kv4_workspace_bytes(int S, int max_rows, int max_length, int q_heads,

@@ -873,8 +873,8 @@ def coral_attention_kv4(q: torch.Tensor, cache, page_table: torch.Tensor, length
     (int32 [S], the rows' own among them) in pages page_table[s] (int32 [S,max_pages]).  Without tree a row sees itself
     and all older tokens; with history (int32 [S]) and tree (int64 [T]) the tokens before history[s], and of the 64 from
     there on those whose bit is set.  max_length: what the lengths may come to (None: what the page table holds).
-    scale: None for 1/sqrt(head_dim).  workspace: plain scratch of coral_attention_kv4_workspace_bytes, not shared by
-    calls that may overlap; None allocates one."""
+    scale: None for 1/sqrt(head_dim).  workspace: coral_attention_kv4_workspace_bytes, prepared by
+    coral_lmhead_workspace_init or zeros, and not shared by calls that may overlap; None allocates one."""
     dt, dev = _dtype_code(q), _on_device(q, "q")
     struct, _, page_size, kv_heads, D = _kv4_cache(cache, dev)
     q_ptr, q_row = _heads_ptr(q, "q", dev, q.dtype)
@@ -894,7 +894,9 @@ def coral_attention_kv4(q: torch.Tensor, cache, page_table: torch.Tensor, length
     if out is None:
         out = _new((T, q_heads, D), q.dtype, dev, stream)
     if workspace is None:
-        workspace = _new((coral_attention_kv4_workspace_bytes(S, max_rows, max_length, q_heads, kv_heads, D, dt),), torch.uint8, dev, stream)
+        n = coral_attention_kv4_workspace_bytes(S, max_rows, max_length, q_heads, kv_heads, D, dt)
+        workspace = _new((max(n, 512),), torch.uint8, dev, stream)
+        _enqueue(_L.coral_lmhead_workspace_init, dev, stream, workspace.data_ptr(), workspace.numel())
     _enqueue(_L.coral_attention_kv4, dev, stream, q_ptr, q_row, ctypes.byref(struct), *args, T, S, max_rows, max_length, q_heads,
              _scale_of(scale, D), dt, _same_device_ptr(out, "out", dev, q.dtype, (T, q_heads, D)),
              _same_device_ptr(workspace, "workspace", dev, torch.uint8, None), workspace.numel())

@@ -14,11 +14,13 @@
 // fp16 queries are two bf16 values and fp32 ones three (exactly); so are the weights p.
 #pragma once
 #include "attention_common.h"
+#include "control_words.h"
 #include "kv4_plan.h"
 
 namespace {
 
 constexpr int kKv4Threads = 256;
+constexpr int kKv4ArrivalStride = 4;
 constexpr int kKv4Waves = kKv4Threads / kWave;
 constexpr int kKv4WaveStep = kKv4Step / kKv4Waves;          // 32 tokens
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -31,44 +33,137 @@ struct Kv4AttnParams {
     Kv4 cache;
     const int32_t *page_table, *lengths, *q_offsets, *history;
     const uint64_t* tree;
-    float* part;                        // [item][split][row][D] sums, then [item][split][row] (largest, sum) pairs
+    float* part;                        // [workgroup][2][row][D] sums, then [workgroup][2][row] (largest, sum) pairs
     float2* part_stats;
-    int max_pages, T, max_rows, group, kv_heads, row_blocks, splits, q_heads;
+    unsigned* arrived;                  // [workgroup] counters, kKv4ArrivalStride words apart, zero between calls
+    int max_pages, T, S, max_rows, group, kv_heads, workgroups;
+    bool apart, join_inside;
     float scale_log2;                   // scores are kept in powers of two
 };
 
-// What the arguments say about a sequence, cut to the arrays.
+// What the arguments say about a sequence, cut to the arrays, and what it takes: its items (a block of ROWS rows for
+// one head of keys) times their steps of 128 tokens and what an item takes before and behind its steps (pages,
+// queries, sums: 3.5 us against 2 for a step among others; without it a share of short sequences took 82 us where
+// others took 47).  One sequence a lane.
+constexpr unsigned kKv4ItemSteps = 3;
 struct Kv4Seq {
-    int row0, rows, length, seen_by_all, history;
-    bool tree;
+    int row0, rows, length, history;
+    unsigned steps;
+    unsigned long long cost;
 };
+template <int ROWS>
 __device__ __forceinline__ Kv4Seq kv4_sequence(const Kv4AttnParams& p, int s) {
-    Kv4Seq q;
+    Kv4Seq q = {};
+    if (s >= p.S) return q;
     const int a = p.q_offsets[s], b = p.q_offsets[s + 1];
+    int length = p.lengths[s];
+    const int h = p.tree ? p.history[s] : 0;
     q.row0 = a < 0 ? 0 : a > p.T ? p.T : a;
     const int end = b > p.T ? p.T : b;
     q.rows = end - q.row0 < p.max_rows ? end - q.row0 : p.max_rows;
+    q.rows = q.rows < 0 ? 0 : q.rows;
     const int64_t room = (int64_t)p.max_pages << p.cache.page_shift;
-    int length = p.lengths[s];
     length = length < 0 ? 0 : length > room ? (int)room : length;
-    q.tree = p.tree != nullptr;
-    if (q.tree) {
-        const int h = p.history[s];
-        q.history = h < 0 ? 0 : h > length ? length : h;
-        q.length = length - q.history > 64 ? q.history + 64 : length;
-        q.seen_by_all = q.history;
-    } else {
-        q.history = 0;
-        q.length = length;
-        q.seen_by_all = length - (q.rows - 1);                  // row i of n sees tokens up to length - n + i
-    }
+    q.history = h < 0 ? 0 : h > length ? length : h;
+    q.length = p.tree && length - q.history > 64 ? q.history + 64 : length;
+    q.steps = q.length > kKv4Step ? ((unsigned)q.length + kKv4Step - 1) / kKv4Step : 1;       // (rows that see nothing are written too)
+    q.cost = (unsigned long long)((q.rows * p.group + ROWS - 1) / ROWS) * p.kv_heads * (q.steps + kKv4ItemSteps);
     return q;
 }
-// Tokens of one split: a multiple of the workgroup's step.
-__device__ __forceinline__ int kv4_chunk(int length, int splits) {
-    const int steps = (length + kKv4Step - 1) / kKv4Step;
-    return (steps + splits - 1) / splits * kKv4Step;
+// Sum over the lanes up to each: sums of 64 numbers below 2^46 in two halves.
+__device__ __forceinline__ unsigned long long wave_scan_u46(unsigned long long x) {
+    const unsigned lo = (unsigned)wave_scan_inclusive((int)(x & 0xfffffu)), hi = (unsigned)wave_scan_inclusive((int)(x >> 20));
+    return ((unsigned long long)hi << 20) + lo;
 }
+__device__ __forceinline__ unsigned long long readlane64(unsigned long long x, int lane) {
+    return (unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// n / d for n < 2^20, where inv is 1 / d to a unit in its last place: n + 1/2 is at least 1 / (2 d) from a multiple of d
+// away, and n inv at most 2^20 / d * 2^-22.4 off.
+__device__ __forceinline__ unsigned quotient20(unsigned n, float inv) { return (unsigned)(((float)n + 0.5f) * inv); }
+__device__ __forceinline__ float reciprocal(unsigned d) { return __builtin_amdgcn_rcpf((float)d); }
+__device__ __forceinline__ unsigned long long divide64(unsigned long long n, unsigned d) {
+    return n >> 32 ? n / d : n >> 20 ? (unsigned)n / d : quotient20((unsigned)n, reciprocal(d));
+}
+
+// An item (a block of a sequence's rows for one head of keys), and a place in it: step j is place
+// kKv4ItemSteps + j.
+struct Kv4Item {
+    int seq, row0, rows, length, history, head, first_row;
+    unsigned place, steps;
+    __device__ __forceinline__ unsigned step_at(unsigned at) const {
+        return at < kKv4ItemSteps ? 0 : at - kKv4ItemSteps < steps ? at - kKv4ItemSteps : steps;
+    }
+};
+// All sequences' items lie one behind the other; 64 sequences at a time are looked at, one a lane.
+template <int ROWS>
+struct Kv4Line {
+    Kv4Seq lanes;
+    unsigned long long upto, before;     // of these sequences; of all before them
+    int s0;
+    unsigned long long each;             // places of a share, and how many shares of all have one more, spread evenly
+    unsigned more, shares;               // (shares at most 768)
+    float inv_shares;
+
+    __device__ __forceinline__ void load(const Kv4AttnParams& p, int from, int lane) {
+        s0 = from;
+        lanes = kv4_sequence<ROWS>(p, from + lane);
+        upto = wave_scan_u46(lanes.cost);
+    }
+    __device__ __forceinline__ void open(const Kv4AttnParams& p, int lane) {
+        unsigned long long total = 0;
+        for (int s = p.S > kWave ? kWave : p.S; s < p.S; s += kWave) {
+            load(p, s, lane);
+            total += readlane64(upto, kWave - 1);
+        }
+        load(p, 0, lane);
+        before = 0;
+        deal(p, total + readlane64(upto, kWave - 1));
+    }
+    __device__ __forceinline__ void deal(const Kv4AttnParams& p, unsigned long long total) {
+        shares = total < (unsigned)p.workgroups ? (unsigned)total : (unsigned)p.workgroups;       // each has a place at least
+        inv_shares = reciprocal(shares ? shares : 1);
+        each = shares ? divide64(total, shares) : 0;
+        more = shares ? (unsigned)(total - each * shares) : 0;
+    }
+    // which share has a place
+    __device__ __forceinline__ unsigned share_of(unsigned long long place) const {
+        unsigned w = (unsigned)((float)place * __builtin_amdgcn_rcpf((float)each + (float)more * inv_shares));     // nearly
+        w = w < shares ? w : shares - 1;
+        while (begin(w) > place) --w;
+        while (w + 1 < shares && begin(w + 1) <= place) ++w;
+        return w;
+    }
+    // where share w begins
+    __device__ __forceinline__ unsigned long long begin(unsigned w) const { return each * w + quotient20(more * w, inv_shares); }
+    // what lies at a place below the total; places do not go back
+    __device__ __forceinline__ Kv4Item find(const Kv4AttnParams& p, unsigned long long place, int lane) {
+        for (;;) {
+            const uint64_t found = __builtin_amdgcn_ballot_w64(place - before < upto);
+            if (found) {
+                const int src = __builtin_ctzll(found);
+                return at(p, src, place - before - (readlane64(upto, src) - readlane64(lanes.cost, src)));
+            }
+            before += readlane64(upto, kWave - 1);
+            load(p, s0 + kWave, lane);
+        }
+    }
+    __device__ __forceinline__ Kv4Item at(const Kv4AttnParams& p, int src, unsigned long long in) const {
+        Kv4Item t;
+        t.seq = s0 + src;
+        t.row0 = __builtin_amdgcn_readlane(lanes.row0, src);
+        t.rows = __builtin_amdgcn_readlane(lanes.rows, src);
+        t.length = __builtin_amdgcn_readlane(lanes.length, src);
+        t.history = __builtin_amdgcn_readlane(lanes.history, src);
+        t.steps = (unsigned)__builtin_amdgcn_readlane((int)lanes.steps, src);
+        const unsigned size = t.steps + kKv4ItemSteps, item = (unsigned)divide64(in, size), blocks = (unsigned)(t.rows * p.group + ROWS - 1) / ROWS;
+        t.place = (unsigned)(in - (unsigned long long)item * size);
+        t.head = (int)divide64(item, blocks);
+        t.first_row = (int)(item - t.head * blocks) * ROWS;
+        return t;
+    }
+};
 
 // N bf16 values whose sum is x (8 bits more each).
 template <int N>
@@ -142,32 +237,204 @@ constexpr int kKv4LdsRow = D + 16;                           // values from toke
 template <int D>
 constexpr int kKv4SumRow = D + 4;                            // floats from row to row when the waves' sums meet
 
-// One workgroup: NT tiles of 16 rows of one sequence and one head of keys, one split of its tokens; its four
-// waves take steps of 32 tokens in turn and add up at the end.
+// What a workgroup has to know of an item behind its steps: which rows, in how many shares' parts it lies, in which of
+// them its first step, and whether that share begins inside it.
+struct Kv4Kept {
+    int row0, head, first_row, n_rows, s0;
+    unsigned w0, parts;
+    bool opens;
+    unsigned more, shares;
+    unsigned long long before, place, share_end, each;
+};
+__device__ __forceinline__ Kv4Kept kv4_kept(const Kv4Kept& from) {
+    auto one = [](int x) CORAL_INLINE { return __builtin_amdgcn_readfirstlane(x); };
+    auto two = [&](unsigned long long x) CORAL_INLINE { return (unsigned long long)(unsigned)one((int)(x >> 32)) << 32 | (unsigned)one((int)x); };
+    return {one(from.row0), one(from.head), one(from.first_row), one(from.n_rows), one(from.s0), (unsigned)one((int)from.w0), (unsigned)one((int)from.parts),
+            one(from.opens) != 0, (unsigned)one((int)from.more), (unsigned)one((int)from.shares), two(from.before), two(from.place), two(from.share_end),
+            two(from.each)};
+}
+
+// Two floats to and from memory that other dies read, past the L2.
+__device__ __forceinline__ void publish2(float* to, float a, float b) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(to), (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 published2(const float* from) {
+    const unsigned long long w = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)w), __uint_as_float((unsigned)(w >> 32)));
+}
+
+// D / 16 values of a row, divided by the sum of its weights; a row that sees nothing is zero.
+template <int DT, int D>
+__device__ __forceinline__ void kv4_write(const Kv4AttnParams& p, const Kv4Kept& item, int r, float inv_group, int d0, const float (&o)[D / 16], float all) {
+    constexpr int kBytes = DT == kF32 ? 4 : 2;
+    const float inv = all > 0.f ? 1.f / all : all == 0.f ? 0.f : all;
+    const int i = (int)quotient20(r, inv_group);
+    char* to = p.out + (int64_t)(item.row0 + i) * p.out_stride + (int64_t)(item.head * p.group + r - i * p.group) * (D * kBytes) + d0 * kBytes;
+#pragma unroll
+    for (int j = 0; j < D / 16; j += 4) {
+        if (DT == kF32) *reinterpret_cast<f32x4_t*>(to + j * 4) = f32x4_t{o[j] * inv, o[j + 1] * inv, o[j + 2] * inv, o[j + 3] * inv};
+        else *reinterpret_cast<uint2*>(to + j * 2) = make_uint2(narrow2<DT>(o[j] * inv, o[j + 1] * inv), narrow2<DT>(o[j + 2] * inv, o[j + 3] * inv));
+    }
+}
+
+// A wave joins the parts of a row, D / 64 values a lane: the parts' statistics first, one a lane, then eight parts' sums
+// at a time.
+template <int DT, int D, class RowOf>
+__device__ __forceinline__ void kv4_join_row(const Kv4AttnParams& p, const Kv4Kept& item, int r, float inv_group, int lane, RowOf row_of) {
+    constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2;
+    const unsigned parts = item.parts;
+    float ref = -INFINITY, all = 0.f, o[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) o[n] = 0.f;
+    for (unsigned j0 = 0; j0 < parts; j0 += kWave) {
+        float2 stat = make_float2(-INFINITY, 0.f);
+        if (j0 + lane < parts) stat = published2(&p.part_stats[row_of(j0 + lane)].x);
+        float top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(stat.x, [](float a, float b) { return fmaxf(a, b); })));
+        top = fmaxf(top, ref);
+        const float keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top), by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
+        ref = top;
+        all = fmaf(all, keep, by * stat.y);
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[n] *= keep;
+        const unsigned left = parts - j0 < kWave ? parts - j0 : kWave;
+        for (unsigned i = 0; i < left; i += 8) {
+            float x[8][N];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float* from = p.part + row_of(j0 + (i + u < left ? i + u : left - 1)) * D + lane * N;
+                if (N == 1) x[u][0] = __uint_as_float(__hip_atomic_load(reinterpret_cast<const unsigned*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+#pragma unroll
+                for (int n = 0; n + 1 < N; n += 2) {
+                    const float2 w = published2(from + n);
+                    x[u][n] = w.x;
+                    x[u][n + 1] = w.y;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float f = i + u < left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), (int)(i + u) & (kWave - 1))) : 0.f;
+#pragma unroll
+                for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, x[u][n], o[n]);
+            }
+        }
+    }
+    all = wave_sum(all);
+    const float inv = all > 0.f ? 1.f / all : all == 0.f ? 0.f : all;
+    const int i = (int)quotient20(r, inv_group);
+    char* to = p.out + (int64_t)(item.row0 + i) * p.out_stride + (int64_t)(item.head * p.group + r - i * p.group) * (D * kBytes) + lane * (N * kBytes);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        if (DT == kF32) reinterpret_cast<float*>(to)[n] = o[n] * inv;
+        else reinterpret_cast<unsigned short*>(to)[n] = narrow16<DT>(o[n] * inv);
+    }
+}
+
+typedef const __attribute__((address_space(4))) Kv4AttnParams* Kv4ArgsPtr;
+
+// Four waves take the steps of an item in turn, 32 tokens each of a step, and add up at the end.  A workgroup's share of
+// all steps is a run of them that may cross items: the first and the last may be parts of an item, which the item's last
+// workgroup puts together, or, where parts and rows are many, k_kv4_join.
 template <int DT, int D, int NT, int TP>
-__global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) {
+__global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 : DT == kF16 ? 2 : 3))) void k_kv4_attention(Kv4AttnParams) {
+    // The arguments are read where they are used: held in scalar registers all the way they would be spilled.
+    const Kv4ArgsPtr args = (Kv4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+    const Kv4AttnParams& p = *(const Kv4AttnParams*)args;
     constexpr int TQ = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, C = D / 32, DTILES = D / 16, kBytes = DT == kF32 ? 4 : 2;
     constexpr int kWaveValues = kKv4WaveStep * kKv4LdsRow<D>;
     static_assert(kWaveValues * 2 >= 16 * kKv4SumRow<D> * 4, "a wave's sums fit where its values were");
     __shared__ __align__(16) unsigned short staged[kKv4Waves][kWaveValues];
     __shared__ float wave_top[kKv4Waves][NT * 16], wave_sum_[kKv4Waves][NT * 16];
+    __shared__ Kv4Kept kept;
+    __shared__ bool is_last;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x, head = blockIdx.y / p.row_blocks, block = blockIdx.y % p.row_blocks;
-    const Kv4Seq seq = kv4_sequence(p, blockIdx.z);
-    const int n_rows = seq.rows * p.group, first_row = block * NT * 16;
-    if (first_row >= n_rows) return;
-    const int chunk = kv4_chunk(seq.length, p.splits);
-    const int used = seq.length > 0 ? (seq.length + chunk - 1) / chunk : 1;
-    if (split >= used) return;
-    const int begin = split * chunk, end = begin + chunk < seq.length ? begin + chunk : seq.length;
+    unsigned long long place, share_end;
+    Kv4Line<NT * 16> line;
+    if (p.apart) {
+        line.load(p, (int)blockIdx.y, lane);
+        line.before = line.each = line.more = line.shares = 0;
+        const unsigned size = (unsigned)__builtin_amdgcn_readlane((int)line.lanes.steps, 0) + kKv4ItemSteps;
+        place = (unsigned long long)blockIdx.x * size;
+        if (place >= readlane64(line.lanes.cost, 0)) return;
+        share_end = place + size;
+    } else {
+        line.open(p, lane);
+        if (blockIdx.x >= line.shares) return;
+        place = line.begin(blockIdx.x);
+        share_end = line.begin(blockIdx.x + 1);
+    }
+    for (int slot = 0;; slot = 1) {                              // where the sums of a part of an item go: the share's first or its last
+    Kv4ArgsPtr args_here = args;
+    asm volatile("" : "+s"(args_here));
+    const Kv4AttnParams& p = *(const Kv4AttnParams*)args_here;
+    const Kv4 cache = p.cache;                                   // what the steps use
+    const float scale_log2 = p.scale_log2;
+    const int page_mask = (1 << cache.page_shift) - 1;
+    const Kv4Item work = line.find(p, place, lane);
+    const unsigned size = work.steps + kKv4ItemSteps, rest = share_end - place < size - work.place ? (unsigned)(share_end - place) : size - work.place;
+    const unsigned first_step = work.step_at(work.place), n_steps = work.step_at(work.place + rest) - first_step;
+    if (n_steps == 0) break;                                     // the share ends before the item's first step
+    const int head = work.head, first_row = work.first_row, n_rows = work.rows * p.group, length = work.length, history = work.history;
+    const unsigned begin = first_step * kKv4Step, stop = begin + n_steps * kKv4Step, end = stop < (unsigned)length ? stop : (unsigned)length;
+    const int seen_by_all = p.tree ? history : length - (work.rows - 1);       // row i of n sees tokens up to length - n + i
 
-    // the query's operands
+    // Pages of the wave's next 32 steps, two tiles of 16 tokens each: one a lane.
+    const int32_t* table = p.page_table + (int64_t)work.seq * p.max_pages;
+    auto pages_from = [&](int step) CORAL_INLINE {
+        const unsigned token = begin + (unsigned)(step + lane / 2) * kKv4Step + wave * kKv4WaveStep + (lane & 1) * 16;
+        return token < end ? table[token >> cache.page_shift] : -1;
+    };
+    int pages = pages_from(0);
+    Kv4Tile<D> k[2][2], v[2][2];
+    unsigned now[2];
+    bool held[2][2];
+    // tiles of a step; a page that is none is read from the cache's first and not seen
+    auto fetch = [&](int set, int step) CORAL_INLINE {
+        now[set] = begin + (unsigned)step * kKv4Step + wave * kKv4WaveStep;
+        if (now[set] >= end) return;                             // (uniform)
+        if (step && (step & 31) == 0) pages = pages_from(step);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + i);
+            held[set][i] = page >= 0 && page < cache.pages;
+            const int64_t row = (((int64_t)(held[set][i] ? page : 0) * cache.kv_heads + head) << cache.page_shift) + (((int)now[set] + i * 16) & page_mask);
+            kv4_load<D>(k[set][i], cache.k_codes + row * (D / 2), cache.k_scales + row * (D / 32), col, g);
+            kv4_load<D>(v[set][i], cache.v_codes + row * (D / 2), cache.v_scales + row * (D / 32), col, g);
+        }
+    };
+    fetch(0, 0);
+    fetch(1, 1);
+    // what is wanted behind the steps goes through LDS: scalar registers are short
+    if (threadIdx.x == 0) {
+        kept.row0 = work.row0;
+        kept.head = head;
+        kept.first_row = first_row;
+        kept.n_rows = n_rows;
+        kept.s0 = line.s0;
+        kept.before = line.before;
+        kept.place = place + rest;
+        kept.share_end = share_end;
+        kept.each = line.each;
+        kept.more = line.more;
+        kept.shares = line.shares;
+        kept.parts = 1;
+        if (n_steps != work.steps) {
+            const unsigned long long start = place - work.place;
+            const unsigned w0 = line.share_of(start + kKv4ItemSteps);
+            kept.parts = line.share_of(start + size - 1) - w0 + 1;
+            kept.w0 = w0;
+            kept.opens = line.begin(w0) >= start;
+        }
+    }
+
+    // the query's operands (rows are below 2^16)
+    const float inv_group = reciprocal(p.group);
     uint4 q[NT][TQ][C];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = first_row + n * 16 + col, i = r / p.group;
-        const char* from = p.q + (int64_t)(seq.row0 + i) * p.q_stride + (int64_t)(head * p.group + r % p.group) * (D * kBytes);
+        const int r = first_row + n * 16 + col, i = (int)quotient20(r, inv_group);
+        const char* from = p.q + (int64_t)(work.row0 + i) * p.q_stride + (int64_t)(head * p.group + r - i * p.group) * (D * kBytes);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (r < n_rows) {
@@ -196,9 +463,9 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
     uint64_t sees[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int r = first_row + n * 16 + col, i = (r < n_rows ? r : n_rows - 1) / p.group;
-        sees_to[n] = seq.tree ? seq.history : seq.length - seq.rows + i + 1;
-        sees[n] = seq.tree ? p.tree[seq.row0 + i] : 0;
+        const int r = first_row + n * 16 + col, i = (int)quotient20(r < n_rows ? r : n_rows - 1, inv_group);
+        sees_to[n] = p.tree ? history : length - work.rows + i + 1;
+        sees[n] = p.tree ? p.tree[work.row0 + i] : 0;
     }
 
     f32x4_t sum[NT][DTILES];
@@ -211,33 +478,7 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
         for (int d = 0; d < DTILES; ++d) sum[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     unsigned short* values = staged[wave];
-    const int32_t* table = p.page_table + (int64_t)blockIdx.z * p.max_pages;
-    const int page_mask = (1 << p.cache.page_shift) - 1;
-    // the pages of the wave's next 32 steps, two tiles of 16 tokens each: one a lane
-    int pages = 0, step = 0;
-    auto fetch_pages = [&]() CORAL_INLINE {
-        const int token = begin + ((step + lane / 2) * kKv4Waves + wave) * kKv4WaveStep + (lane & 1) * 16;
-        pages = token < end ? table[token >> p.cache.page_shift] : -1;
-    };
-    Kv4Tile<D> k[2], v[2];
-    bool held[2];
-    // tiles of a step; a page that is none (or behind the end) is read from the cache's first and not seen
-    auto fetch = [&](int at) CORAL_INLINE {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int page = __builtin_amdgcn_readlane(pages, 2 * (step & 31) + i);
-            held[i] = page >= 0 && page < p.cache.pages;
-            const int64_t row = (((int64_t)(held[i] ? page : 0) * p.kv_heads + head) << p.cache.page_shift) + ((at + i * 16) & page_mask);
-            kv4_load<D>(k[i], p.cache.k_codes + row * (D / 2), p.cache.k_scales + row * (D / 32), col, g);
-            kv4_load<D>(v[i], p.cache.v_codes + row * (D / 2), p.cache.v_scales + row * (D / 32), col, g);
-        }
-    };
-    int at = begin + wave * kKv4WaveStep;
-    if (at < end) {
-        fetch_pages();
-        fetch(at);
-    }
-    while (at < end) {
+    auto process = [&](int set, int step) CORAL_INLINE {
         // scores: tokens along the registers (4 g + i of each tile), rows along the lanes
         f32x4_t score[NT][2];
 #pragma unroll
@@ -246,7 +487,7 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
             for (int n = 0; n < NT; ++n) score[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const uint4 a = kv4_operand(k[i].code[c], kv4_unit(k[i].scale[c / 4]));
+                const uint4 a = kv4_operand(k[set][i].code[c], kv4_unit(k[set][i].scale[c / 4]));
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -260,47 +501,49 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 store_vec(reinterpret_cast<uint4*>(values + (i * 16 + col) * kKv4LdsRow<D> + kv4_column<D>(c, g)),
-                          kv4_operand(v[i].code[c], kv4_unit(v[i].scale[c / 4])));
-        const bool all_seen = at + kKv4WaveStep <= seq.seen_by_all && at + kKv4WaveStep <= end && held[0] && held[1];
-        const bool held0 = held[0], held1 = held[1];
-        const int now = at;
-        at += kKv4Step;
-        ++step;
-        if (at < end) {
-            if ((step & 31) == 0) fetch_pages();
-            fetch(at);
-        }
+                          kv4_operand(v[set][i].code[c], kv4_unit(v[set][i].scale[c / 4])));
+        const int at = (int)now[set];
+        const bool held0 = held[set][0], held1 = held[set][1];
+        const bool all_seen = at + kKv4WaveStep <= seen_by_all && held0 && held1;
+        fetch(set, step + 2);
         uint4 weight[NT][TP];
+        float s[NT][8], to[NT];
+        bool any = false;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float s[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] = score[n][j / 4][j % 4] * p.scale_log2;
+            for (int j = 0; j < 8; ++j) s[n][j] = score[n][j / 4][j % 4] * scale_log2;
             if (!all_seen) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int token = now + (j / 4) * 16 + 4 * g + j % 4, bit = token - seq.history;
+                    const int token = at + (j / 4) * 16 + 4 * g + j % 4, bit = token - history;
                     const bool in = token < sees_to[n] || (bit >= 0 && bit < 64 && (sees[n] >> (bit & 63) & 1));
-                    s[j] = in && token < seq.length && (j < 4 ? held0 : held1) ? s[j] : -INFINITY;
+                    s[n][j] = in && token < length && (j < 4 ? held0 : held1) ? s[n][j] : -INFINITY;
                 }
             }
-            float top = fmaxf(fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3])), fmaxf(fmaxf(s[4], s[5]), fmaxf(s[6], s[7])));
+            float top = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
             top = lane_xor_max<16>(lane_xor_max<32>(top));
             const bool move = top > ref[n] + kMoveAt || (ref[n] == -INFINITY && top > -INFINITY);
-            if (__builtin_amdgcn_ballot_w64(move)) {
-                const float to = move ? top : ref[n];
-                const float by = ref[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[n] - to);
-                const float keep = move ? by : 1.f;
-                ref[n] = to;
+            to[n] = move ? top : ref[n];
+            any |= move;
+        }
+        if (__builtin_amdgcn_ballot_w64(any)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float keep = to[n] == ref[n] ? 1.f : ref[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[n] - to[n]);
+                ref[n] = to[n];
                 total[n] *= keep;
 #pragma unroll
                 for (int d = 0; d < DTILES; ++d) sum[n][d] *= keep;
             }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
             const float base = ref[n] == -INFINITY ? 0.f : ref[n];
             float w[8], part[8][TP];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                w[j] = __builtin_amdgcn_exp2f(s[j] - base);
+                w[j] = __builtin_amdgcn_exp2f(s[n][j] - base);
                 split_bf16<TP>(w[j], part[j]);
             }
             total[n] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
@@ -322,9 +565,18 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
                 for (int t = 0; t < TP; ++t) sum[n][d] = mfma_bf16(a, weight[n][t], sum[n][d]);
         }
         __builtin_amdgcn_wave_barrier();
+    };
+    for (int step = 0; now[0] < end; step += 2) {
+        process(0, step);
+        if (now[1] >= end) break;
+        process(1, step + 1);
     }
 
     // the waves' sums relative to the largest reference, in the order of the waves
+    Kv4ArgsPtr args_again = args;
+    asm volatile("" : "+s"(args_again));
+    {
+    const Kv4AttnParams& p = *(const Kv4AttnParams*)args_again;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float all = lane_xor_sum<16>(lane_xor_sum<32>(total[n]));
@@ -334,11 +586,13 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
         }
     }
     const int row = threadIdx.x / 16, d0 = (threadIdx.x & 15) * (D / 16);
-    const int64_t item = ((int64_t)blockIdx.z * p.kv_heads + head) * p.row_blocks + block;
+    __syncthreads();
+    const Kv4Kept end_of = kv4_kept(kept);
+    const float inv_group_ = reciprocal(p.group);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         float* mine = reinterpret_cast<float*>(staged[wave]);
-        __syncthreads();
+        if (n) __syncthreads();
 #pragma unroll
         for (int d = 0; d < DTILES; ++d)
             *reinterpret_cast<f32x4_t*>(mine + col * kKv4SumRow<D> + d * 16 + 4 * g) = sum[n][d];
@@ -352,8 +606,8 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
             by[w] = t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t - top);
             all = fmaf(by[w], wave_sum_[w][n * 16 + row], all);
         }
-        const int r = first_row + n * 16 + row;
-        if (r >= n_rows) continue;
+        const int r = end_of.first_row + n * 16 + row;
+        if (r >= end_of.n_rows) continue;
         float o[D / 16];
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) o[j] = 0.f;
@@ -363,70 +617,100 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_attention(Kv4AttnParams p) 
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[j] = by[w] == 0.f ? o[j] : fmaf(by[w], from[j], o[j]);
         }
-        if (used > 1) {
-            const int64_t at_row = (item * p.splits + split) * (NT * 16) + n * 16 + row;
+        if (end_of.parts > 1) {
+            const int64_t at_row = ((int64_t)blockIdx.x * 2 + slot) * (NT * 16) + n * 16 + row;
 #pragma unroll
-            for (int j = 0; j < D / 16; j += 4)
-                *reinterpret_cast<f32x4_t*>(p.part + at_row * D + d0 + j) = f32x4_t{o[j], o[j + 1], o[j + 2], o[j + 3]};
-            if (d0 == 0) p.part_stats[at_row] = make_float2(top, all);
+            for (int j = 0; j < D / 16; j += 2) publish2(p.part + at_row * D + d0 + j, o[j], o[j + 1]);
+            if (d0 == 0) publish2(&p.part_stats[at_row].x, top, all);
         } else {
-            const float inv = all > 0.f ? 1.f / all : all == 0.f ? 0.f : all;      // a row that sees nothing: zeros
-            char* to = p.out + (int64_t)(seq.row0 + r / p.group) * p.out_stride + (int64_t)(head * p.group + r % p.group) * (D * kBytes) + d0 * kBytes;
-#pragma unroll
-            for (int j = 0; j < D / 16; j += 4) {
-                if (DT == kF32) {
-                    *reinterpret_cast<f32x4_t*>(to + j * 4) = f32x4_t{o[j] * inv, o[j + 1] * inv, o[j + 2] * inv, o[j + 3] * inv};
-                } else {
-                    *reinterpret_cast<uint2*>(to + j * 2) = make_uint2(narrow2<DT>(o[j] * inv, o[j + 1] * inv), narrow2<DT>(o[j + 2] * inv, o[j + 3] * inv));
-                }
+            kv4_write<DT, D>(p, end_of, r, inv_group_, d0, o, all);
+        }
+    }
+    if (end_of.parts > 1 && p.join_inside) {
+        // The item's last workgroup joins its parts.  They are counted in the word of the share that has its first step.
+        __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's stores are out
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            unsigned* word = p.arrived + end_of.w0 * kKv4ArrivalStride;
+            const unsigned old = __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            is_last = old + 1 == end_of.parts;
+            if (is_last) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (is_last) {                                           // uniform
+            for (int r = wave; r < NT * 16 && end_of.first_row + r < end_of.n_rows; r += kKv4Waves) {
+                auto row_of = [&](unsigned j) CORAL_INLINE { return ((int64_t)(end_of.w0 + j) * 2 + (j == 0 && !end_of.opens ? 1 : 0)) * (NT * 16) + r; };
+                kv4_join_row<DT, D>(p, end_of, end_of.first_row + r, inv_group_, lane, row_of);
             }
         }
     }
+    place = end_of.place;
+    share_end = end_of.share_end;
+    if (place >= share_end) return;
+    __syncthreads();                                             // the sums have been read: the next item's values may come
+    line.load(p, end_of.s0, lane);
+    line.before = end_of.before;
+    line.each = end_of.each;
+    line.more = end_of.more;
+    line.shares = end_of.shares;
+    line.inv_shares = reciprocal(line.shares ? line.shares : 1);
+    }
+    }
 }
 
-// Joins the splits of a row: one workgroup a row, its waves take splits in turn.
-template <int DT, int D>
-__global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p, int tiles) {
-    constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2;
+// Joins the parts of an item that several workgroups have taken: one workgroup a row, its waves take parts in turn.
+template <int DT, int D, int NT>
+__global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
+    constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2, kRows = NT * 16;
     __shared__ float sums[kKv4Waves][D];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int q_head = blockIdx.x, i = blockIdx.y;
-    const Kv4Seq seq = kv4_sequence(p, blockIdx.z);
-    if (i >= seq.rows || seq.length <= 0) return;
-    const int chunk = kv4_chunk(seq.length, p.splits), used = (seq.length + chunk - 1) / chunk;
-    if (used < 2) return;                                     // written already
-    const int head = q_head / p.group, r = i * p.group + q_head % p.group, rows = tiles * 16;
-    const int64_t item = ((int64_t)blockIdx.z * p.kv_heads + head) * p.row_blocks + r / rows;
-    const int64_t first = item * p.splits * rows + r % rows;  // the row in split s: first + s * rows
-    // each wave looks at all splits' statistics, at most four a lane
+    const int q_head = blockIdx.x, t = blockIdx.y;
+    Kv4Line<kRows> line;
+    unsigned long long total = 0, start = 0;
+    unsigned steps = 0;
+    int r = 0;
+    for (int s = 0; s < p.S; s += kWave) {
+        line.load(p, s, lane);
+        const uint64_t found = __builtin_amdgcn_ballot_w64(t >= line.lanes.row0 && t < line.lanes.row0 + line.lanes.rows);
+        if (found) {
+            const int src = __builtin_ctzll(found);
+            const Kv4Item first = line.at(p, src, 0);
+            steps = first.steps;
+            r = (t - first.row0) * p.group + q_head % p.group;
+            const unsigned blocks = (unsigned)(first.rows * p.group + kRows - 1) / kRows;
+            start = total + readlane64(line.upto, src) - readlane64(line.lanes.cost, src) + (unsigned long long)(q_head / p.group * blocks + r / kRows) * (steps + kKv4ItemSteps);
+        }
+        total += readlane64(line.upto, kWave - 1);
+    }
+    if (!steps) return;                                          // a row of no sequence
+    line.deal(p, total);
+    const unsigned long long end = start + kKv4ItemSteps + steps;
+    const unsigned w0 = line.share_of(start + kKv4ItemSteps), last = line.share_of(end - 1);
+    if (w0 == last) return;                                      // one workgroup's, which has written it
+    // part j: share w0 + j; the first lies behind what else its share holds, unless it begins with the item
+    const int64_t first = ((int64_t)w0 * 2 + (line.begin(w0) >= start ? 0 : 1)) * kRows + r % kRows, others = (int64_t)(w0 + 1) * 2 * kRows + r % kRows;
+    const int parts = (int)(last - w0) + 1;
+    auto row_of = [&](int j) CORAL_INLINE { return j == 0 ? first : others + (int64_t)(j - 1) * 2 * kRows; };
     float top = -INFINITY;
-    float2 stat[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int s = j * kWave + lane;
-        stat[j] = s < used ? p.part_stats[first + (int64_t)s * rows] : make_float2(-INFINITY, 0.f);
-        top = fmaxf(top, stat[j].x);
-    }
+    for (int j = lane; j < parts; j += kWave) top = fmaxf(top, p.part_stats[row_of(j)].x);
     top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(top, [](float a, float b) { return fmaxf(a, b); })));
-    float all = 0.f, by[4];
+    float all = 0.f, o[N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        by[j] = stat[j].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[j].x - top);
-        all = fmaf(by[j], stat[j].y, all);
-    }
-    all = wave_sum(all);
-    float o[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) o[j] = 0.f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int n = 0; n < N; ++n) o[n] = 0.f;
+    for (int j0 = 0; j0 < parts; j0 += kWave) {
+        float2 stat = make_float2(-INFINITY, 0.f);
+        if (j0 + lane < parts) stat = p.part_stats[row_of(j0 + lane)];
+        const float by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
+        all = fmaf(by, stat.y, all);
 #pragma unroll 4
-        for (int s = j * kWave + wave; s < (j + 1) * kWave && s < used; s += kKv4Waves) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by[j]), s & (kWave - 1)));
-            const float* from = p.part + (first + (int64_t)s * rows) * D + lane * N;
+        for (int j = j0 + wave; j < j0 + kWave && j < parts; j += kKv4Waves) {
+            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j - j0));
+            const float* from = p.part + row_of(j) * D + lane * N;
 #pragma unroll
             for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, from[n], o[n]);
         }
+    }
+    all = wave_sum(all);
 #pragma unroll
     for (int n = 0; n < N; ++n) sums[wave][lane * N + n] = o[n];
     __syncthreads();
@@ -434,22 +718,26 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p, int t
     const int d = threadIdx.x;
     const float v = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
     const float y = all > 0.f ? v / all : all == 0.f ? 0.f : all;
-    char* to = p.out + (int64_t)(seq.row0 + i) * p.out_stride + ((int64_t)q_head * D + d) * kBytes;
+    char* to = p.out + (int64_t)t * p.out_stride + ((int64_t)q_head * D + d) * kBytes;
     if (DT == kF32) *reinterpret_cast<float*>(to) = y;
     else *reinterpret_cast<unsigned short*>(to) = narrow16<DT>(y);
 }
 
 using kv4_attn_fn = void (*)(Kv4AttnParams);
-using kv4_join_fn = void (*)(Kv4AttnParams, int);
+using kv4_join_fn = void (*)(Kv4AttnParams);
 // The weights p of bf16 calls are two bf16 values where a wave has one tile (which memory bounds: no cost; the result's
 // only rounding is then its own) and one where it has more (the products bound it: a second term would
 // take a third longer; the roundings of single weights, 2^-9 each, average out to about the result's own).
 template <int DT, int D>
 kv4_attn_fn kv4_kernel(int tiles) {
-    constexpr int terms = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, most = 512 / (D * terms), many = DT == kBF16 ? 1 : terms;
-    if (tiles == 4) return k_kv4_attention<DT, D, most >= 4 ? 4 : 1, most >= 4 ? many : DT == kF32 ? 3 : 2>;
+    constexpr int terms = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, most = kv4_most_tiles(D, terms), many = DT == kBF16 ? 1 : terms;
     if (tiles == 2) return k_kv4_attention<DT, D, most >= 2 ? 2 : 1, most >= 2 ? many : DT == kF32 ? 3 : 2>;
     return k_kv4_attention<DT, D, 1, DT == kF32 ? 3 : 2>;
+}
+template <int DT, int D>
+kv4_join_fn kv4_join(int tiles) {
+    constexpr int most = kv4_most_tiles(D, DT == kBF16 ? 1 : DT == kF16 ? 2 : 3);
+    return tiles == 2 ? k_kv4_join<DT, D, most >= 2 ? 2 : 1> : k_kv4_join<DT, D, 1>;
 }
 
 }  // namespace

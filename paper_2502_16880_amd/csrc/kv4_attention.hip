@@ -25,7 +25,7 @@ int query_terms(coral_dtype dt) { return dt == CORAL_BF16 ? 1 : dt == CORAL_F16 
 extern "C" size_t coral_attention_kv4_workspace_bytes(int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim,
                                                       coral_dtype dt) {
     if (check_kv4_sizes(0, S, max_rows, max_length, q_heads, kv_heads, head_dim, dt) != CORAL_OK) return 0;
-    const size_t n = kv4_workspace(kv4_plan(S, max_rows, max_length, q_heads, kv_heads, head_dim, query_terms(dt)), S, kv_heads, head_dim);
+    const size_t n = kv4_workspace(kv4_plan(S, max_rows, max_length, q_heads, kv_heads, head_dim, query_terms(dt)), head_dim);
     return n < 256 ? 256 : (n + 255) / 256 * 256;
 }
 
@@ -49,7 +49,7 @@ extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, con
     if ((uintptr_t)tree & 7u) return CORAL_ERR_UNSUPPORTED;
     const Kv4Plan plan = kv4_plan(S, max_rows, max_length, q_heads, kv_heads, head_dim, query_terms(dt));
     if ((int64_t)kv_heads * plan.row_blocks > 65535) return CORAL_ERR_UNSUPPORTED;
-    const size_t need = kv4_workspace(plan, S, kv_heads, head_dim);
+    const size_t need = kv4_workspace(plan, head_dim);
     if (need && (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < need)) return CORAL_ERR_WORKSPACE;
     kv4_parts(cache, parts);
     auto whole = [](const void* base, int64_t bytes) { return Rows{base, bytes, bytes, 1}; };
@@ -64,22 +64,27 @@ extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, con
     p.q_stride = in_q.stride;
     p.out_stride = out_rows.stride;
     p.page_table = page_table; p.lengths = lengths; p.q_offsets = q_offsets; p.history = history; p.tree = tree;
-    p.max_pages = max_pages; p.T = T; p.max_rows = max_rows; p.group = q_heads / kv_heads; p.kv_heads = kv_heads; p.q_heads = q_heads;
-    p.row_blocks = plan.row_blocks; p.splits = plan.splits;
+    p.max_pages = max_pages; p.T = T; p.S = S; p.max_rows = max_rows; p.group = q_heads / kv_heads; p.kv_heads = kv_heads;
+    p.workgroups = plan.workgroups; p.apart = plan.apart; p.join_inside = plan.join_inside;
     p.scale_log2 = scale * kLog2e;
     if (need) {
-        const size_t rows = (size_t)S * kv_heads * plan.row_blocks * plan.splits * 16 * plan.tiles;
-        p.part = static_cast<float*>(workspace);
+        const size_t rows = (size_t)plan.workgroups * 2 * 16 * plan.tiles;
+        static_assert(kKv4Control == coral_ctrl::kPreparedWords * sizeof(unsigned) && kKv4Control % 256 == 0, "");
+        static_assert(kKv4Units * 3 * kKv4ArrivalStride <= coral_ctrl::kGateScoreWords, "a counter for each workgroup");
+        p.arrived = static_cast<unsigned*>(workspace) + coral_ctrl::kGateScores;
+        p.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKv4Control);
         p.part_stats = reinterpret_cast<float2*>(p.part + rows * head_dim);
     }
     const void* fn = dt == CORAL_F32 ? coral_kv4_kernel_f32(head_dim, plan.tiles) : dt == CORAL_BF16 ? coral_kv4_kernel_bf16(head_dim, plan.tiles)
                                                                                                     : coral_kv4_kernel_f16(head_dim, plan.tiles);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    hipLaunchKernelGGL(reinterpret_cast<kv4_attn_fn>(const_cast<void*>(fn)), dim3(plan.splits, kv_heads * plan.row_blocks, S), dim3(kKv4Threads), 0, stream, p);
+    const dim3 grid = plan.apart ? dim3(kv_heads * plan.row_blocks, S) : dim3(plan.workgroups);
+    hipLaunchKernelGGL(reinterpret_cast<kv4_attn_fn>(const_cast<void*>(fn)), grid, dim3(kKv4Threads), 0, stream, p);
     if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
-    if (plan.splits > 1) {
-        const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim) : coral_kv4_join_f16(head_dim);
-        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(q_heads, max_rows, S), dim3(kKv4Threads), 0, stream, p, plan.tiles);
+    if (need && !plan.join_inside) {
+        const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim, plan.tiles) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim, plan.tiles)
+                                                                                                        : coral_kv4_join_f16(head_dim, plan.tiles);
+        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(q_heads, T), dim3(kKv4Threads), 0, stream, p);
         if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
     }
     return CORAL_OK;

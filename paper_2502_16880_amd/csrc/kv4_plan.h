@@ -4,37 +4,48 @@
 #include <stdint.h>
 
 struct Kv4Plan {
-    int tiles;         // tiles of 16 rows (a row: one token, one query head) that a workgroup takes
-    int row_blocks;    // workgroups beside each other for one sequence's rows of one head of keys
-    int splits;        // workgroups along a sequence's tokens, at most
+    int tiles;         // tiles of 16 rows (a row: one token, one query head) that a workgroup takes together
+    int row_blocks;    // so many times that, at most, for one sequence's rows of one head of keys
+    int workgroups;    // among which all sequences' steps are shared equally, or
+    bool apart;        // one workgroup for each sequence, head of keys and block of rows
+    bool join_inside;  // an item's last workgroup joins its parts; or a kernel of its own does, many workgroups at once
 };
 
+constexpr size_t kKv4Control = 16896;   // bytes of the workspace's control words and the words behind them
 constexpr int kKv4Step = 128;           // tokens that a workgroup's four waves take together: 32 each
 constexpr int kKv4MostRows = 64;        // rows (tokens) of a sequence in one call
+constexpr int kKv4Units = 256;          // compute units of the card
+constexpr int kKv4Apart = 256;          // sequences beyond which they are not shared out (each workgroup sums them all up)
+constexpr int kKv4JoinRows = 8;         // rows and parts of an item, at most, that one workgroup joins as fast as another
+constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave
 
 // Query operands and sums of a wave's tiles stay in registers: with `terms` bf16 values for a query value
 // (1 for bf16, 2 for fp16, 3 for fp32) this many tiles fit.
-inline int kv4_most_tiles(int head_dim, int terms) {
-    const int n = 512 / (head_dim * terms);
-    return n >= 4 ? 4 : n >= 2 ? 2 : 1;
+constexpr int kv4_most_tiles(int head_dim, int terms) { return head_dim * terms <= 128 ? 2 : 1; }
+// Workgroups that a compute unit holds: waves on a SIMD that registers are kept for (sums and query operands of the
+// tiles, two steps' codes).
+constexpr int kv4_occupancy(int head_dim, int tiles, int terms) {
+    return head_dim * tiles * (terms + 2) <= 384 ? 3 : head_dim < 256 && head_dim * tiles * (terms + 2) <= 768 ? 2 : 1;
 }
 
 inline Kv4Plan kv4_plan(int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim, int terms) {
     Kv4Plan p;
     const int tiles = (max_rows * (q_heads / kv_heads) + 15) / 16, most = kv4_most_tiles(head_dim, terms);
-    p.tiles = 1;
-    while (p.tiles < tiles && p.tiles < most) p.tiles *= 2;
+    p.tiles = tiles < most ? tiles : most;
     p.row_blocks = (tiles + p.tiles - 1) / p.tiles;
-    const int64_t steps = ((int64_t)max_length + kKv4Step - 1) / kKv4Step, items = (int64_t)S * kv_heads * p.row_blocks;
-    int64_t n = (2048 + items - 1) / items;
-    if (n > steps) n = steps;
-    if (n > 256) n = 256;
-    p.splits = n < 1 ? 1 : (int)n;
+    const int64_t steps = max_length > kKv4Step ? ((int64_t)max_length + kKv4Step - 1) / kKv4Step : 1;
+    const int64_t all = (int64_t)S * kv_heads * p.row_blocks * steps, places = kKv4Units * kv4_occupancy(head_dim, p.tiles, terms);
+    p.workgroups = (int)(all < places ? all : places);
+    p.apart = S > kKv4Apart;
+    const int64_t parts = p.workgroups / ((int64_t)S * kv_heads * p.row_blocks) + 2, rows = max_rows * (q_heads / kv_heads);
+    p.join_inside = rows <= kKv4JoinRows && parts <= kKv4JoinParts;
     return p;
 }
 
-// One split's share of a row: head_dim sums, the largest score and the sum of exponentials, in fp32.
-inline size_t kv4_workspace(const Kv4Plan& p, int S, int kv_heads, int head_dim) {
-    if (p.splits < 2) return 0;
-    return (size_t)S * kv_heads * p.row_blocks * p.splits * (16 * p.tiles) * ((size_t)head_dim + 2) * sizeof(float);
+// A workgroup's share begins and ends inside an item (a sequence's block of rows for a head of keys) in two places at
+// most: two blocks of sums of head_dim values, the largest score and the sum of exponentials for each row, in fp32,
+// behind the control words.
+inline size_t kv4_workspace(const Kv4Plan& p, int head_dim) {
+    if (p.apart || p.workgroups < 2) return 0;
+    return kKv4Control + (size_t)p.workgroups * 2 * (16 * p.tiles) * ((size_t)head_dim + 2) * sizeof(float);
 }

@@ -235,7 +235,7 @@ int main() {
     int s, rows, length, q, kv, d, terms;
     while (std::scanf("%d %d %d %d %d %d %d", &s, &rows, &length, &q, &kv, &d, &terms) == 7) {
         const Kv4Plan p = kv4_plan(s, rows, length, q, kv, d, terms);
-        std::printf("%d %d %d %zu\n", p.tiles, p.row_blocks, p.splits, kv4_workspace(p, s, kv, d));
+        std::printf("%d %d %d %d %zu\n", p.tiles, p.row_blocks, p.workgroups, p.apart ? 1 : 0, kv4_workspace(p, d));
     }
 }
 """
@@ -249,10 +249,10 @@ def test_plan_covers_every_row_and_the_workspace_what_it_needs(tmp_path):
              for q, kv in ((8, 8), (32, 8), (28, 4), (1024, 1)) for d in (64, 128, 256) for terms in (1, 2, 3)]
     text = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True, check=True).stdout
     for (s, rows, length, q, kv, d, terms), line in zip(calls, text.splitlines()):
-        tiles, blocks, splits, need = map(int, line.split())
-        assert tiles in (1, 2, 4) and tiles * blocks * 16 >= rows * (q // kv) and (blocks - 1) * tiles * 16 < rows * (q // kv)
-        assert tiles * d * terms <= 512 or tiles == 1
-        assert 1 <= splits <= 256 and (splits - 1) * 128 < max(length, 1)
-        assert need == (s * kv * blocks * splits * tiles * 16 * (d + 2) * 4 if splits > 1 else 0)
+        tiles, blocks, groups, apart, need = map(int, line.split())
+        assert tiles in (1, 2) and tiles * blocks * 16 >= rows * (q // kv) and (blocks - 1) * tiles * 16 < rows * (q // kv)
+        assert tiles == 1 or d * terms <= 128
+        assert 1 <= groups <= 768 and groups <= s * kv * blocks * max(1, -(-length // 128)) and apart == (s > 256)
+        assert need == (16896 + groups * 2 * tiles * 16 * (d + 2) * 4 if groups > 1 and not apart else 0)
         dt = {1: BF16, 2: F16, 3: F32}[terms]
         assert coral.coral_attention_kv4_workspace_bytes(s, rows, length, q, kv, d, dt) >= max(need, 256)

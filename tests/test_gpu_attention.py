@@ -324,8 +324,8 @@ def test_attention_kv4_long(coral, dtype, D, q_heads, kv_heads, rows, page):
     assert torch.equal(c.run(), out)
 
 
-def test_attention_kv4_every_number_of_splits(coral):
-    """The work is cut by max_length: results differ by the order of sums only, whatever the lengths are."""
+def test_attention_kv4_every_number_of_shares(coral):
+    """The work is cut by max_length and shared out: results differ by the order of sums only, whatever the lengths are."""
     c = Cached(coral, "f32", [(1000, 3), (130, 1), (700, 64)], 4, 2, 64, 32)
     for most in (0, 1, 129, 500, 1000, 4000, 100000):
         c.check(c.run(max_length=most))
@@ -337,6 +337,17 @@ def test_attention_kv4_many_sequences_of_any_length(coral, dtype):
     sequences = [(int(n), int(min(n, r))) for n, r in zip(np.exp(rng.uniform(0, 7, 150)).astype(int) + 1, rng.integers(1, 5, 150))]
     c = Cached(coral, dtype, sequences, 6, 2, 64, 32)
     c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_kv4_more_sequences_than_are_shared_out(coral, dtype):
+    rng = np.random.default_rng(9)
+    c = Cached(coral, dtype, [(int(n), 1 + int(n > 2)) for n in rng.integers(1, 200, 1030)], 4, 2, 64, 16, tree=dtype == "f16")
+    c.sequences[700] = (0, 0)
+    out = c.run()
+    c.check(out, only=[0, 1, 500, 699, 701, 1028, 1029])
+    few = Cached(coral, dtype, [(int(n), 1) for n in rng.integers(1, 3000, 250)], 2, 1, 64, 64)      # shared out, four loads of sequences
+    few.check(few.run(), only=[0, 63, 64, 128, 200, 249])
 
 
 def test_attention_kv4_peaked_scores(coral):
@@ -438,7 +449,7 @@ def test_attention_kv4_strided_queries_another_stream_and_graph_replays(coral):
     stream.synchronize()
     assert torch.equal(other, want)
     # one workspace under two graphs, lengths that grow between replays
-    ws = torch.empty(coral.coral_attention_kv4_workspace_bytes(2, 4, 900, 8, 2, 128, coral.CORAL_BF16), dtype=torch.uint8, device="cuda")
+    ws = torch.zeros(coral.coral_attention_kv4_workspace_bytes(2, 4, 900, 8, 2, 128, coral.CORAL_BF16), dtype=torch.uint8, device="cuda")
     lengths, outs, graphs = args[3].clone(), [torch.zeros_like(want) for _ in range(2)], []
     for out in outs:
         graph = torch.cuda.CUDAGraph()
@@ -448,7 +459,7 @@ def test_attention_kv4_strided_queries_another_stream_and_graph_replays(coral):
     for n in (900, 500, 4, 0, 811):
         lengths.copy_(ints([n, 77]))
         eager = coral.coral_attention_kv4(args[0], args[1], args[2], lengths, args[4], 4, max_length=900)
-        ws.fill_(255)
+        assert bool((ws[:16896] == 0).all())                      # the counters are as they were
         for graph, out in zip(graphs, outs):
             out.fill_(3)
             graph.replay()
