@@ -527,6 +527,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _enqueue(fn, device, stream, *args) -> None:
     """Calls the library on the tensors' device and the given stream (None: the device's current one)."""
     if stream is None:
@@ -535,7 +538,7 @@ def _enqueue(fn, device, stream, *args) -> None:
         raise ValueError(f"the stream belongs to {stream.device}, the tensors to {device}")
     else:
         handle = stream.cuda_stream
-    if device.index == torch.cuda.current_device():
+    if device.index == _current_device():
         st = fn(*args, handle)
     else:
         with torch.cuda.device(device):
@@ -714,36 +717,49 @@ def alloc_kv4_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, de
 
 
 def _kv4_cache(cache, device):
-    """(struct, pages, page_size, kv_heads, head_dim) of four checked tensors."""
+    """(struct, page_size, kv_heads, head_dim) of four checked tensors."""
     k_codes, k_scales, v_codes, v_scales = cache
-    if k_codes.dim() != 4:
+    codes = k_codes.shape
+    if len(codes) != 4:
         raise ValueError("the cache's codes must be [pages, kv_heads, page_size, head_dim/2]")
-    pages, kv_heads, page_size, half = k_codes.shape
-    if max(k_codes.shape) > _INT_MAX // 2:
+    pages, kv_heads, page_size, half = codes
+    if max(codes) > _INT_MAX // 2:
         raise ValueError("sizes must fit 32 bits")
-    u8, codes, scales = torch.uint8, (pages, kv_heads, page_size, half), (pages, kv_heads, page_size, half // 16)
+    u8, scales = torch.uint8, (pages, kv_heads, page_size, half // 16)
     struct = _Kv4CacheStruct(_same_device_ptr(k_codes, "k_codes", device, u8, codes),
                              _same_device_ptr(k_scales, "k_scales", device, u8, scales),
                              _same_device_ptr(v_codes, "v_codes", device, u8, codes),
                              _same_device_ptr(v_scales, "v_scales", device, u8, scales), pages, page_size, kv_heads, half * 2)
-    return struct, pages, page_size, kv_heads, half * 2
+    return ctypes.byref(struct), page_size, kv_heads, half * 2
 
 
 def _heads_ptr(t: torch.Tensor, name: str, device, dtype) -> Tuple[int, int]:
     """(pointer, elements from token to token) of [T, heads, head_dim] with dense heads."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} must live on {device}, got {t.device}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [tokens, heads, head_dim], got {list(t.shape)}")
-    T, heads, D = t.shape
-    if max(t.shape) > _INT_MAX:
+    shape = t.shape
+    if len(shape) != 3:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim], got {list(shape)}")
+    T, heads, D = shape
+    if T > _INT_MAX or heads > _INT_MAX or D > _INT_MAX:
         raise ValueError("sizes must fit 32 bits")
     row, head, one = t.stride()
-    if t.numel() and ((D > 1 and one != 1) or (heads > 1 and head != D)):
+    if (one != 1 or head != D) and ((D > 1 and one != 1) or (heads > 1 and head != D)) and T and heads and D:
         raise ValueError(f"{name} must have its heads one behind the other (only the tokens may be further apart)")
     return t.data_ptr(), row if T > 1 and heads and D else heads * D
+
+
+def _heads_out(out, like, name, device, stream) -> Tuple[torch.Tensor, int, int]:
+    """(tensor, pointer, elements from token to token) of an output like `like`: the one given, or a new dense one."""
+    if out is None:
+        shape = like.shape
+        out = like.new_empty(shape) if stream is None else _new(shape, like.dtype, device, stream)
+        return out, out.data_ptr(), shape[1] * shape[2]
+    if out.shape != like.shape:
+        raise ValueError(f"{name} must be {list(like.shape)}, got {list(out.shape)}")
+    return (out, *_heads_ptr(out, name, device, like.dtype))
 
 
 def _on_device(t: torch.Tensor, name: str):
@@ -769,23 +785,25 @@ def coral_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos
     if first is None:
         raise ValueError("q or k is needed")
     dt, dev, dtype = _dtype_code(first), _on_device(first, "q" if q is not None else "k"), first.dtype
-    T, D = first.shape[0], first.shape[-1]
-    q_ptr, q_row = (None, 0) if q is None else _heads_ptr(q, "q", dev, dtype)
-    k_ptr, k_row = (None, 0) if k is None else _heads_ptr(k, "k", dev, dtype)
-    q_heads, kv_heads = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
-    if q is not None and k is not None and (k.shape[0] != T or k.shape[2] != D):
-        raise ValueError("q and k must have the same tokens and head_dim")
+    q_ptr = k_ptr = v_ptr = qo_ptr = ko_ptr = struct = slot_ptr = None
+    q_row = k_row = v_row = qo_row = ko_row = q_heads = kv_heads = 0
+    if q is not None:
+        q_ptr, q_row = _heads_ptr(q, "q", dev, dtype)
+        T, q_heads, D = q.shape
+    if k is not None:
+        k_ptr, k_row = _heads_ptr(k, "k", dev, dtype)
+        k_tokens, kv_heads, k_dim = k.shape
+        if q is None:
+            T, D = k_tokens, k_dim
+        elif k_tokens != T or k_dim != D:
+            raise ValueError("q and k must have the same tokens and head_dim")
     if (positions is None) != (inv_freq is None):
         raise ValueError("positions and inv_freq go together")
-    rot = 0
-    if inv_freq is not None:
-        rot = 2 * inv_freq.numel()
     rope = _RopeStruct(_same_device_ptr(q_weight, "q_weight", dev, dtype, (D,)),
                        _same_device_ptr(k_weight, "k_weight", dev, dtype, (D,)),
                        _same_device_ptr(positions, "positions", dev, torch.int32, (T,)),
-                       _same_device_ptr(inv_freq, "inv_freq", dev, torch.float32, None), float(eps), min(rot, _INT_MAX),
-                       1 if interleaved else 0)
-    struct, v_ptr, v_row, slot_ptr = None, None, 0, None
+                       _same_device_ptr(inv_freq, "inv_freq", dev, torch.float32, None), float(eps),
+                       0 if inv_freq is None else min(2 * inv_freq.numel(), _INT_MAX - 1), 1 if interleaved else 0)
     if cache is not None:
         if k is None or v is None or slots is None:
             raise ValueError("a cache goes with k, v and slots")
@@ -798,18 +816,14 @@ def coral_qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos
         raise ValueError("v, slots and k_out=False go with a cache")
     if q is None:
         q_out = None
-    elif q_out is None:
-        q_out = _new(q.shape, dtype, dev, stream)
+    else:
+        q_out, qo_ptr, qo_row = _heads_out(q_out, q, "q_out", dev, stream)
     if k is None or k_out is False:
         k_out = None
-    elif k_out is None:
-        k_out = _new(k.shape, dtype, dev, stream)
-    qo_ptr, qo_row = (None, 0) if q_out is None else _heads_ptr(q_out, "q_out", dev, dtype)
-    ko_ptr, ko_row = (None, 0) if k_out is None else _heads_ptr(k_out, "k_out", dev, dtype)
-    if (q_out is not None and q_out.shape != q.shape) or (k_out is not None and k_out.shape != k.shape):
-        raise ValueError("q_out and k_out must have the shapes of q and k")
+    else:
+        k_out, ko_ptr, ko_row = _heads_out(k_out, k, "k_out", dev, stream)
     _enqueue(_L.coral_qk_norm_rope, dev, stream, q_ptr, q_row, k_ptr, k_row, ctypes.byref(rope), T, q_heads, kv_heads, D, dt,
-             qo_ptr, qo_row, ko_ptr, ko_row, None if struct is None else ctypes.byref(struct), v_ptr, v_row, slot_ptr)
+             qo_ptr, qo_row, ko_ptr, ko_row, struct, v_ptr, v_row, slot_ptr)
     return q_out, k_out
 
 
@@ -817,13 +831,13 @@ def coral_kv4_append(cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tenso
     """coral_kv4_append of the C ABI: tokens' keys and values [T,kv_heads,head_dim] into the places slots [T]
     int32 of the cache (page * page_size + place in the page; outside the cache: passed over)."""
     dt, dev = _dtype_code(k), _on_device(k, "k")
-    struct, _, _, kv_heads, D = _kv4_cache(cache, dev)
+    struct, _, kv_heads, D = _kv4_cache(cache, dev)
     k_ptr, k_row = _heads_ptr(k, "k", dev, k.dtype)
     v_ptr, v_row = _heads_ptr(v, "v", dev, k.dtype)
-    if k.shape[1:] != (kv_heads, D) or v.shape != k.shape:
+    T, k_heads, k_dim = k.shape
+    if k_heads != kv_heads or k_dim != D or v.shape != k.shape:
         raise ValueError(f"k and v must be [T, {kv_heads}, {D}] as the cache is")
-    T = k.shape[0]
-    _enqueue(_L.coral_kv4_append, dev, stream, ctypes.byref(struct), k_ptr, k_row, v_ptr, v_row,
+    _enqueue(_L.coral_kv4_append, dev, stream, struct, k_ptr, k_row, v_ptr, v_row,
              _same_device_ptr(slots, "slots", dev, torch.int32, (T,)), T, dt)
 
 
@@ -832,19 +846,23 @@ def coral_kv4_read(cache, slots: torch.Tensor, dtype: torch.dtype, k_out: Option
     """coral_kv4_read of the C ABI: (k, v), each [T,kv_heads,head_dim] of dtype, as the cache holds them in the
     places slots [T] int32.  Rows of slots outside the cache are left as k_out and v_out were."""
     dev = _on_device(slots, "slots")
-    struct, _, _, kv_heads, D = _kv4_cache(cache, dev)
+    struct, _, kv_heads, D = _kv4_cache(cache, dev)
     slot_ptr = _same_device_ptr(slots, "slots", dev, torch.int32, None)
     T = slots.numel()
     if T > _INT_MAX:
         raise ValueError("sizes must fit 32 bits")
+    shape = (T, kv_heads, D)
     if k_out is None:
-        k_out = _new((T, kv_heads, D), dtype, dev, stream)
+        k_out = _new(shape, dtype, dev, stream)
+        k_ptr = k_out.data_ptr()
+    else:
+        k_ptr = _same_device_ptr(k_out, "k_out", dev, dtype, shape)
     if v_out is None:
-        v_out = _new((T, kv_heads, D), dtype, dev, stream)
-    dt = _dtype_code(k_out)
-    _enqueue(_L.coral_kv4_read, dev, stream, ctypes.byref(struct), slot_ptr, T, dt,
-             _same_device_ptr(k_out, "k_out", dev, dtype, (T, kv_heads, D)),
-             _same_device_ptr(v_out, "v_out", dev, dtype, (T, kv_heads, D)))
+        v_out = _new(shape, dtype, dev, stream)
+        v_ptr = v_out.data_ptr()
+    else:
+        v_ptr = _same_device_ptr(v_out, "v_out", dev, dtype, shape)
+    _enqueue(_L.coral_kv4_read, dev, stream, struct, slot_ptr, T, _dtype_code(k_out), k_ptr, v_ptr)
     return k_out, v_out
 
 
@@ -875,31 +893,33 @@ def coral_attention_kv4(q: torch.Tensor, cache, page_table: torch.Tensor, length
     there on those whose bit is set.  max_length: what the lengths may come to (None: what the page table holds).
     scale: None for 1/sqrt(head_dim).  workspace: coral_attention_kv4_workspace_bytes, prepared by
     coral_lmhead_workspace_init or zeros, and not shared by calls that may overlap; None allocates one."""
-    dt, dev = _dtype_code(q), _on_device(q, "q")
-    struct, _, page_size, kv_heads, D = _kv4_cache(cache, dev)
-    q_ptr, q_row = _heads_ptr(q, "q", dev, q.dtype)
-    T, q_heads = q.shape[:2]
-    if q.shape[2] != D:
+    dt, dev, dtype = _dtype_code(q), _on_device(q, "q"), q.dtype
+    struct, page_size, kv_heads, D = _kv4_cache(cache, dev)
+    q_ptr, q_row = _heads_ptr(q, "q", dev, dtype)
+    T, q_heads, q_dim = q.shape
+    if q_dim != D:
         raise ValueError(f"q must be [T, q_heads, {D}] as the cache is")
     if page_table.dim() != 2:
         raise ValueError("page_table must be [S, max_pages]")
     S, max_pages = page_table.shape
     i32, max_rows = torch.int32, int(max_rows)
     max_length = min(max_pages * page_size, _INT_MAX) if max_length is None else int(max_length)
-    if max(S, max_pages, abs(max_rows), abs(max_length)) > _INT_MAX:
+    if S > _INT_MAX or max_pages > _INT_MAX or abs(max_rows) > _INT_MAX or abs(max_length) > _INT_MAX:
         raise ValueError("sizes must fit 32 bits")
     args = (_same_device_ptr(page_table, "page_table", dev, i32, (S, max_pages)), max_pages,
             _same_device_ptr(lengths, "lengths", dev, i32, (S,)), _same_device_ptr(q_offsets, "q_offsets", dev, i32, (S + 1,)),
             _same_device_ptr(history, "history", dev, i32, (S,)), _same_device_ptr(tree, "tree", dev, torch.int64, (T,)))
     if out is None:
-        out = _new((T, q_heads, D), q.dtype, dev, stream)
+        out = q.new_empty((T, q_heads, D)) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _same_device_ptr(out, "out", dev, dtype, (T, q_heads, D))
     if workspace is None:
         n = coral_attention_kv4_workspace_bytes(S, max_rows, max_length, q_heads, kv_heads, D, dt)
         workspace = _new((max(n, 512),), torch.uint8, dev, stream)
         _enqueue(_L.coral_lmhead_workspace_init, dev, stream, workspace.data_ptr(), workspace.numel())
-    _enqueue(_L.coral_attention_kv4, dev, stream, q_ptr, q_row, ctypes.byref(struct), *args, T, S, max_rows, max_length, q_heads,
-             _scale_of(scale, D), dt, _same_device_ptr(out, "out", dev, q.dtype, (T, q_heads, D)),
-             _same_device_ptr(workspace, "workspace", dev, torch.uint8, None), workspace.numel())
+    _enqueue(_L.coral_attention_kv4, dev, stream, q_ptr, q_row, struct, *args, T, S, max_rows, max_length, q_heads,
+             _scale_of(scale, D), dt, out_ptr, _same_device_ptr(workspace, "workspace", dev, torch.uint8, None), workspace.numel())
     return out
 
 
@@ -911,21 +931,24 @@ def coral_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_
     q [T,q_heads,head_dim]; k and v [keys,kv_heads,head_dim]; sequence s has rows q_offsets[s] .. q_offsets[s+1] (int32
     [S+1]) and keys k_offsets[s] .. k_offsets[s+1] (None: the same), its last row sees its last key.  scale: None for
     1/sqrt(head_dim)."""
-    dt, dev = _dtype_code(q), _on_device(q, "q")
-    q_ptr, q_row = _heads_ptr(q, "q", dev, q.dtype)
-    k_ptr, k_row = _heads_ptr(k, "k", dev, q.dtype)
-    v_ptr, v_row = _heads_ptr(v, "v", dev, q.dtype)
+    dt, dev, dtype = _dtype_code(q), _on_device(q, "q"), q.dtype
+    q_ptr, q_row = _heads_ptr(q, "q", dev, dtype)
+    k_ptr, k_row = _heads_ptr(k, "k", dev, dtype)
+    v_ptr, v_row = _heads_ptr(v, "v", dev, dtype)
     T, q_heads, D = q.shape
-    keys, kv_heads = k.shape[:2]
-    if k.shape[2] != D or v.shape != k.shape:
+    keys, kv_heads, k_dim = k.shape
+    if k_dim != D or v.shape != k.shape:
         raise ValueError("k and v must have one shape, and q's head_dim")
     S = q_offsets.numel() - 1
     if S > _INT_MAX:
         raise ValueError("sizes must fit 32 bits")
-    args = (_same_device_ptr(q_offsets, "q_offsets", dev, torch.int32, (S + 1,)),
-            _same_device_ptr(k_offsets, "k_offsets", dev, torch.int32, (S + 1,)))
+    offsets_ptr = _same_device_ptr(q_offsets, "q_offsets", dev, torch.int32, (S + 1,))
+    k_offsets_ptr = _same_device_ptr(k_offsets, "k_offsets", dev, torch.int32, (S + 1,))
     if out is None:
-        out = _new((T, q_heads, D), q.dtype, dev, stream)
-    _enqueue(_L.coral_attention_prompt, dev, stream, q_ptr, q_row, k_ptr, k_row, v_ptr, v_row, *args, T, keys, S, q_heads,
-             kv_heads, D, _scale_of(scale, D), dt, _same_device_ptr(out, "out", dev, q.dtype, (T, q_heads, D)))
+        out = q.new_empty((T, q_heads, D)) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
+        out_ptr = out.data_ptr()
+    else:
+        out_ptr = _same_device_ptr(out, "out", dev, dtype, (T, q_heads, D))
+    _enqueue(_L.coral_attention_prompt, dev, stream, q_ptr, q_row, k_ptr, k_row, v_ptr, v_row, offsets_ptr, k_offsets_ptr, T, keys,
+             S, q_heads, kv_heads, D, _scale_of(scale, D), dt, out_ptr)
     return out
