@@ -13,6 +13,8 @@
 #pragma once
 #include "attention_common.h"
 
+#include <type_traits>
+
 namespace {
 
 constexpr int kPromptThreads = 256;
@@ -117,17 +119,32 @@ __device__ __forceinline__ unsigned only_finite(unsigned w, bool& odd) {
     odd |= bad;
     return bad ? 0u : w;
 }
+// acc plus two values.
+template <int DT>
+__device__ __forceinline__ float add_pair(unsigned w, float acc) {
+    if (DT == kF16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, w), __builtin_bit_cast(f16x2_t, 0x3c003c00u), acc, false);
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc, false);
+}
 // Keys 0 .. most of a tile, one bit each.
 __device__ __forceinline__ unsigned long long keys_to(int most) { return most < 0 ? 0ull : most > 62 ? ~0ull : (2ull << most) - 1ull; }
+
+// A wave's 64 pieces of 16 bytes from memory into 1 KB of LDS, past the registers; what lies behind the view's end comes as
+// zero.  Nothing waits for it but dma_arrived.
+__device__ __forceinline__ void dma_piece(Buffer from, unsigned at, unsigned lds_place) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from), "s"(lds_place) : "memory", "m0");
+}
+__device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
 // (2^-12) each with random signs, which come to about the result's own rounding.
 template <int DT, int D>
 __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(PromptParams p) {
     constexpr int BN = D == 256 ? 32 : 64, ROWS = 128, PIECES = D / 8, LOADS = BN * PIECES / kPromptThreads;
-    constexpr int QC = D / 16, KT = BN / 32, DT32 = D / 32, kTile = BN * D * 2;
-    __shared__ __align__(256) char lds[2][2][kTile];             // [buffer][keys, values]
-    __shared__ unsigned long long odd[4];                        // of a tile that rows see a part of: keys whose values are not finite
+    constexpr int QC = D / 16, KT = BN / 32, DT32 = D / 32, KC = BN / 16, kTile = BN * D * 2;
+    __shared__ struct {
+        __align__(256) char tile[2][2][kTile];                   // [buffer][keys, values]
+        unsigned long long odd[4];                               // of a tile that rows see a part of: keys whose values are not finite
+    } lds;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 31, h = lane >> 5;
     const int unit = prompt_unit(blockIdx.x, p.q_heads * p.tiles);
@@ -141,6 +158,28 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
     const int n_tiles = (n_keys + BN - 1) / BN;
     const int my_first = t.first + wave * 32, row = my_first + col;
 
+    const int64_t kv_head = head / p.group;
+    const char* k_base = p.k + (int64_t)t.k0 * p.k_stride + kv_head * (D * 2);
+    const char* v_base = p.v + (int64_t)t.k0 * p.v_stride + kv_head * (D * 2);
+    const size_t k_bytes = t.keys ? (size_t)(t.keys - 1) * p.k_stride + D * 2 : 0, v_bytes = t.keys ? (size_t)(t.keys - 1) * p.v_stride + D * 2 : 0;
+    // piece i * 256 + thread of a tile goes to that place of LDS; which piece of the row that is, is exchanged by the row's number
+    unsigned k_at[LOADS], v_at[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = prompt_place<PIECES>(r, at % PIECES) / 16 % PIECES;
+        k_at[i] = (unsigned)(r * (int)p.k_stride + c * 16);
+        v_at[i] = (unsigned)(r * (int)p.v_stride + c * 16);
+    }
+    const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&lds.tile[0][0][0];
+    auto fetch = [&](int tile) CORAL_INLINE {
+        const Buffer kb = buffer_view(k_base, (size_t)tile * BN * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)tile * BN * p.v_stride, v_bytes);
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds_base + (tile & 1) * 2 * kTile + wave * 1024);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) dma_piece(kb, k_at[i], to + i * 4096);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) dma_piece(vb, v_at[i], to + kTile + i * 4096);
+    };
+    if (n_tiles > 0) fetch(0);
     uint4 q[QC];
     {
         const char* from = p.q + (int64_t)(t.row0 + row) * p.q_stride + (int64_t)head * (D * 2) + h * 16;
@@ -151,71 +190,67 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
             q[c].x ^= p.q_sign; q[c].y ^= p.q_sign; q[c].z ^= p.q_sign; q[c].w ^= p.q_sign;
         }
     }
-    const int64_t kv_head = head / p.group;
-    const char* k_base = p.k + (int64_t)t.k0 * p.k_stride + kv_head * (D * 2);
-    const char* v_base = p.v + (int64_t)t.k0 * p.v_stride + kv_head * (D * 2);
-    const size_t k_bytes = t.keys ? (size_t)(t.keys - 1) * p.k_stride + D * 2 : 0, v_bytes = t.keys ? (size_t)(t.keys - 1) * p.v_stride + D * 2 : 0;
-    uint4 next_k[LOADS], next_v[LOADS];
-    auto fetch = [&](int tile) CORAL_INLINE {
-        const Buffer kb = buffer_view(k_base, (size_t)tile * BN * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)tile * BN * p.v_stride, v_bytes);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
-            next_k[i] = buffer_read16(kb, (unsigned)(r * (int)p.k_stride + c * 16));
-            next_v[i] = buffer_read16(vb, (unsigned)(r * (int)p.v_stride + c * 16));
-        }
-    };
     // From this tile on some rows see a part of a tile.  A product of 0 and infinity must not reach the rows that do not
     // see the value: it is made zero, and the rows that see it become NaN by the key's bit.
     const int first_cut = (reach + t.first + 1 < 0 ? 0 : reach + t.first + 1) / BN;
-    auto put = [&](int tile) CORAL_INLINE {
-        char* to = lds[tile & 1][0];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int at = i * kPromptThreads + threadIdx.x, place = prompt_place<PIECES>(at / PIECES, at % PIECES);
-            if (tile >= first_cut) {
-                bool bad = false;
-                next_v[i].x = only_finite2<DT>(next_v[i].x, bad);
-                next_v[i].y = only_finite2<DT>(next_v[i].y, bad);
-                next_v[i].z = only_finite2<DT>(next_v[i].z, bad);
-                next_v[i].w = only_finite2<DT>(next_v[i].w, bad);
-                if (bad) atomicOr(&odd[tile & 3], 1ull << (at / PIECES));
-            }
-            store_vec(reinterpret_cast<uint4*>(to + place), next_k[i]);
-            store_vec(reinterpret_cast<uint4*>(to + kTile + place), next_v[i]);
-        }
-    };
     f32x16_t sum[DT32];
 #pragma unroll
     for (int d = 0; d < DT32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[d][i] = 0.f;
     float ref = -INFINITY, total = 0.f;
-    if (threadIdx.x < 4) odd[threadIdx.x] = 0;
+    const float scale_log2 = p.scale_log2;
+    // operands' places in a buffer: keys (32 kt + col, piece 2 c + h), values (column 32 d + lane % 32; keys 16 c + 4 h + 0..3 and
+    // 16 c + 8 + 4 h + 0..3: rows r = 4 h + lane % 16 / 4 and r + 8, lanes pointing at four pieces of eight bytes)
+    const int k_place = prompt_place<PIECES>(col, h), r = 4 * h + (lane & 15) / 4, quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2;
+    const int v_place = prompt_place<PIECES>(r, quad) + (lane & 1) * 8, v_place8 = prompt_place<PIECES>(r + 8, quad) + (lane & 1) * 8;
+    if (threadIdx.x < 4) lds.odd[threadIdx.x] = 0;
+    dma_arrived();
     __syncthreads();
-    if (n_tiles > 0) {
-        fetch(0);
-        put(0);
-    }
-    __syncthreads();
-    for (int j = 0; j < n_tiles; ++j) {
-        const char *keys = lds[j & 1][0], *values = lds[j & 1][1];
+    // one tile: CUT where some row may see a part of it only
+    auto step = [&](int j, auto parity, auto may_cut) CORAL_INLINE {
+        constexpr bool CUT = decltype(may_cut)::value;
+        const char *keys = &lds.tile[0][0][0] + parity * (2 * kTile), *values = keys + kTile;
         if (j + 1 < n_tiles) fetch(j + 1);
-        if (threadIdx.x == 0) odd[(j + 2) & 3] = 0;              // tile j - 2's; put(j + 2) comes behind the barrier
         const int k0 = j * BN;
-        if (k0 <= reach + my_first + 31 && my_first < t.rows) {  // some row of the wave sees some key of the tile (uniform)
-            f32x16_t s[KT];
+        if (CUT) {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
+            for (int i = 0; i < LOADS; ++i) {
+                uint4* at = reinterpret_cast<uint4*>(const_cast<char*>(values) + (i * kPromptThreads + threadIdx.x) * 16);
+                const uint4 raw = load_vec(at);
+                bool bad = false;
+                const uint4 fine = make_uint4(only_finite2<DT>(raw.x, bad), only_finite2<DT>(raw.y, bad), only_finite2<DT>(raw.z, bad), only_finite2<DT>(raw.w, bad));
+                if (bad) {
+                    store_vec(at, fine);
+                    atomicOr(&lds.odd[j & 3], 1ull << ((i * kPromptThreads + (int)threadIdx.x) / PIECES));
+                }
+            }
+            if (threadIdx.x == 0) lds.odd[(j + 2) & 3] = 0;      // tile j - 2's
+            __syncthreads();
+        }
+        if (!CUT || (k0 <= reach + my_first + 31 && my_first < t.rows)) {      // some row of the wave sees some key (uniform)
+            f32x16_t s[KT];
+            constexpr int N = KT * QC, AHEAD = 8;                // products, and operands on their way
+            uint4 a[AHEAD];
+            auto key_operand = [&](int i) CORAL_INLINE {
+                return load_vec(reinterpret_cast<const uint4*>(keys + (k_place ^ (i % QC * 32)) + i / QC * (32 * PIECES * 16)));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD && i < N; ++i) a[i] = key_operand(i);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int c = 0; c < QC; ++c)
-                    s[kt] = mfma_32<DT>(load_vec(reinterpret_cast<const uint4*>(keys + prompt_place<PIECES>(kt * 32 + col, 2 * c + h))), q[c], s[kt]);
+            for (int i = 0; i < N; ++i) {
+                s[i / QC] = mfma_32<DT>(a[i % AHEAD], q[i % QC], s[i / QC]);
+                if (i + AHEAD < N) a[i % AHEAD] = key_operand(i + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);               // (left alone, the compiler reads each operand right before its product)
             }
-            const bool cut = k0 + BN - 1 > reach + my_first;
-            if (cut) {
-                const int most = reach + row - k0;               // newest key of the tile that the row sees
+            __builtin_amdgcn_s_setprio(0);
+            const int most = reach + row - k0;                   // newest key of the tile that the row sees
+            if (CUT) {
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -227,7 +262,7 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
-            top = lane_xor_max<32>(top) * p.scale_log2;
+            top = lane_xor_max<32>(top) * scale_log2;
             const bool move = top > ref + kPromptMoveAt || (ref == -INFINITY && top > -INFINITY);
             if (__builtin_amdgcn_ballot_w64(move)) {
                 const float to = move ? top : ref, by = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to), keep = move ? by : 1.f;
@@ -237,35 +272,51 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
                 for (int d = 0; d < DT32; ++d) sum[d] *= keep;
             }
             const float base = ref == -INFINITY ? 0.f : ref;
-            uint4 w[BN / 16];
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                float e[16], part = 0.f;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[kt][i], p.scale_log2, -base));
-                    part += e[i];
-                }
-                total += part;
-                w[2 * kt] = make_uint4(narrow2<DT>(e[0], e[1]), narrow2<DT>(e[2], e[3]), narrow2<DT>(e[4], e[5]), narrow2<DT>(e[6], e[7]));
-                w[2 * kt + 1] = make_uint4(narrow2<DT>(e[8], e[9]), narrow2<DT>(e[10], e[11]), narrow2<DT>(e[12], e[13]), narrow2<DT>(e[14], e[15]));
-            }
-            // the values' operand: column 32 d + lane % 32, keys 16 c + 4 h + 0..3 and 16 c + 8 + 4 h + 0..3
-            const int quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2, in = (lane & 1) * 8, r = 4 * h + (lane & 15) / 4;
-            auto operand = [&](int d, int c) CORAL_INLINE {
-                const uint2 lo = prompt_transposed(values + prompt_place<PIECES>(16 * c + r, 4 * d + quad) + in);
-                const uint2 hi = prompt_transposed(values + prompt_place<PIECES>(16 * c + 8 + r, 4 * d + quad) + in);
+            // values' operand i: columns of tile i % DT32, keys of chunk i / DT32
+            constexpr int M = DT32 * KC, VAHEAD = 4;
+            uint4 b[VAHEAD];
+            auto value_operand = [&](int i) CORAL_INLINE {
+                const uint2 lo = prompt_transposed(values + (v_place ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
+                const uint2 hi = prompt_transposed(values + (v_place8 ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
                 return make_uint4(lo.x, lo.y, hi.x, hi.y);
             };
-            if (j >= first_cut && (odd[j & 3] & keys_to(reach + row - k0))) total = NAN;
 #pragma unroll
-            for (int d = 0; d < DT32; ++d)
+            for (int i = 0; i < VAHEAD && i < M; ++i) b[i] = value_operand(i);
+            // Weights of keys 16 c + 8 (g / 2) + 4 h + 2 (g % 2) and the next, g = 0..3: the products of chunk c wait for these four
+            // only, so the others' vector instructions run beside products.
+            unsigned w[KC][4];
+            auto weigh = [&](int c, int g) CORAL_INLINE {
+                const float x = s[c / 2][8 * (c % 2) + 2 * g], y = s[c / 2][8 * (c % 2) + 2 * g + 1];
+                w[c][g] = narrow2<DT>(__builtin_amdgcn_exp2f(fmaf(x, scale_log2, -base)), __builtin_amdgcn_exp2f(fmaf(y, scale_log2, -base)));
+                total = add_pair<DT>(w[c][g], total);            // of the weights as rounded: half the additions
+            };
 #pragma unroll
-                for (int c = 0; c < BN / 16; ++c) sum[d] = mfma_32<DT>(operand(d, c), w[c], sum[d]);
+            for (int g = 0; g < 4; ++g) weigh(0, g);
+            if (CUT && (lds.odd[j & 3] & keys_to(most))) total = NAN;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                const int c = i / DT32, d = i % DT32;
+                sum[d] = mfma_32<DT>(b[i % VAHEAD], make_uint4(w[c][0], w[c][1], w[c][2], w[c][3]), sum[d]);
+                if (i + VAHEAD < M) b[i % VAHEAD] = value_operand(i + VAHEAD);
+                if (c + 1 < KC) {
+#pragma unroll
+                    for (int g = d * 4 / DT32; g < (d + 1) * 4 / DT32; ++g) weigh(c + 1, g);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        if (j + 1 < n_tiles) put(j + 1);
+        dma_arrived();
         __syncthreads();
+    };
+    int j = 0;
+    const int whole = first_cut < n_tiles ? first_cut : n_tiles;
+    for (; j + 1 < whole; j += 2) {
+        step(j, std::integral_constant<int, 0>(), std::false_type());
+        step(j + 1, std::integral_constant<int, 1>(), std::false_type());
     }
+    for (; j < whole; ++j) step(j, j & 1, std::false_type());
+    for (; j < n_tiles; ++j) step(j, j & 1, std::true_type());
     total = lane_xor_sum<32>(total);
     if (row >= t.rows) return;
     const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;          // a row that sees nothing: zeros
