@@ -40,17 +40,20 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
         rows_overlap(out_rows, {q_offsets, offsets, offsets, 1}) || rows_overlap(out_rows, {k_offsets, offsets, offsets, 1}))
         return CORAL_ERR_UNSUPPORTED;
     const int rows = dt == CORAL_F32 ? 64 : 128;
-    const int64_t tiles = T / rows + (S < T ? S : T), units = tiles * q_heads;       // each sequence has at most one tile that is not full
+    const int64_t tiles = T / rows + (S < T ? S : T);        // each sequence has at most one tile that is not full
+    int parts = 1;
+    while (q_heads * parts % kXcds) parts *= 2;
+    const int64_t units = (tiles + parts - 1) / parts * q_heads * parts;
     if (units > INT32_MAX - 64) return CORAL_ERR_UNSUPPORTED;
     p.q = static_cast<const char*>(q); p.k = static_cast<const char*>(k); p.v = static_cast<const char*>(v);
     p.out = static_cast<char*>(out);
     p.q_stride = in_q.stride; p.k_stride = in_k.stride; p.v_stride = in_v.stride; p.out_stride = out_rows.stride;
     p.q_offsets = q_offsets; p.k_offsets = k_offsets;
-    p.T = T; p.keys = keys; p.S = S; p.q_heads = q_heads; p.group = q_heads / kv_heads; p.tiles = (int)tiles;
+    p.T = T; p.keys = keys; p.S = S; p.q_heads = q_heads; p.group = q_heads / kv_heads; p.tiles = (int)tiles; p.parts = parts;
     // scores are multiplied by a number above zero: the sign goes to q (exactly), and nothing (all weights equal) is little enough
     p.scale_log2 = fmaxf(fabsf(scale) * 1.44269504088896340736f, 1e-37f);
     p.q_sign = signbit(scale) ? (dt == CORAL_F32 ? 0x80000000u : 0x80008000u) : 0u;
-    hipLaunchKernelGGL(prompt_kernel(dt, head_dim), dim3((unsigned)((units + kXcds - 1) / kXcds * kXcds)), dim3(kPromptThreads), 0,
+    hipLaunchKernelGGL(prompt_kernel(dt, head_dim), dim3((unsigned)units), dim3(kPromptThreads), 0,
                        static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }
