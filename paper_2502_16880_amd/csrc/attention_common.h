@@ -2,7 +2,10 @@
 // the cache of 4-bit floats, and the host's checks.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include <stdint.h>
+
+#include <cmath>
 
 #include "buffer_loads.h"
 #include "coral_lmhead.h"
@@ -102,6 +105,11 @@ inline size_t storage_bytes(coral_dtype dt) { return dt == CORAL_F32 ? 4 : 2; }
 inline bool storage_known(coral_dtype dt) { return dt == CORAL_F32 || dt == CORAL_BF16 || dt == CORAL_F16; }
 inline bool head_dim_known(int d) { return d == 64 || d == 128 || d == 256; }
 constexpr int kMostHeads = 1024;
+
+// Scores are multiplied by a number above zero, to powers of two: the sign goes to q (exactly), and a scale of nothing (all
+// weights equal) is little enough.
+inline float score_scale(float scale) { return fmaxf(fabsf(scale) * 1.44269504088896340736f, 1e-37f); }
+inline unsigned score_sign(float scale, coral_dtype dt) { return !std::signbit(scale) ? 0u : dt == CORAL_F32 ? 0x80000000u : 0x80008000u; }
 
 // Rows of `width` bytes, `stride` bytes apart.
 struct Rows {

@@ -23,7 +23,6 @@ constexpr int kKv4Threads = 256;
 constexpr int kKv4ArrivalStride = 4;
 constexpr int kKv4Waves = kKv4Threads / kWave;
 constexpr int kKv4WaveStep = kKv4Step / kKv4Waves;          // 32 tokens
-constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kMoveAt = 8.f;                               // weights stay below 2^8
 
 struct Kv4AttnParams {
@@ -38,7 +37,8 @@ struct Kv4AttnParams {
     unsigned* arrived;                  // [workgroup] counters, kKv4ArrivalStride words apart, zero between calls
     int max_pages, T, S, max_rows, group, kv_heads, workgroups;
     bool apart, join_inside;
-    float scale_log2;                   // scores are kept in powers of two
+    float scale_log2;                   // scores are kept in powers of two; above zero, the sign is taken by q
+    unsigned q_sign;                    // bit to flip in every value of q
 };
 
 // What the arguments say about a sequence, cut to the arrays, and what it takes: its items (a block of ROWS rows for
@@ -200,21 +200,22 @@ __device__ __forceinline__ int kv4_column(int c, int g) {
     return D == 64 ? 16 * g + 8 * c : D == 128 ? 32 * g + 8 * c : 128 * (c >> 2) + 32 * g + 8 * (c & 3);
 }
 template <int D>
-__device__ __forceinline__ void kv4_load(Kv4Tile<D>& t, const unsigned char* codes, const unsigned char* scales, int token, int g) {
+__device__ __forceinline__ void kv4_load(Kv4Tile<D>& t, const unsigned char* codes, const unsigned char* scales, unsigned token, unsigned g) {
+    // (offsets without a sign: the instructions then take the bases from scalar registers)
     if (D == 64) {
-        const uint2 w = *reinterpret_cast<const uint2*>(codes + token * 32 + g * 8);
+        const uint2 w = *reinterpret_cast<const uint2*>(codes + (token * 32u + g * 8u));
         t.code[0] = w.x;
         t.code[1] = w.y;
-        t.scale[0] = scales[token * 2 + g / 2];
+        t.scale[0] = scales[token * 2u + g / 2u];
     } else {
 #pragma unroll
         for (int i = 0; i < D / 128; ++i) {
-            const uint4 w = load_stream(reinterpret_cast<const uint4*>(codes + token * (D / 2) + i * 64 + g * 16));
+            const uint4 w = load_stream(reinterpret_cast<const uint4*>(codes + (token * (D / 2u) + i * 64u + g * 16u)));
             t.code[4 * i % Kv4Tile<D>::kDwords] = w.x;
             t.code[(4 * i + 1) % Kv4Tile<D>::kDwords] = w.y;
             t.code[(4 * i + 2) % Kv4Tile<D>::kDwords] = w.z;
             t.code[(4 * i + 3) % Kv4Tile<D>::kDwords] = w.w;
-            t.scale[i % Kv4Tile<D>::kScales] = scales[token * (D / 32) + i * 4 + g];
+            t.scale[i % Kv4Tile<D>::kScales] = scales[token * (D / 32u) + i * 4u + g];
         }
     }
 }
@@ -226,14 +227,18 @@ __device__ __forceinline__ f32x4_t mfma_bf16(uint4 a, uint4 b, f32x4_t acc) {
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 // Four rows of LDS, 16 columns: lane l of sixteen gets column l of the rows whose pieces the lanes point at
 // (lane l: row l / 4, columns 4 (l % 4) on).
-__device__ __forceinline__ uint2 lds_transposed(const unsigned short* at) {
+__device__ __forceinline__ uint2 lds_transposed(const char* at) {
     const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4_t*)const_cast<unsigned short*>(at));
+        (__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(at));
     return __builtin_bit_cast(uint2, r);
 }
 
+// Where a token's values begin in a wave's part of LDS (bytes): eight banks further from token to token and four more for
+// every second eight of them, so that neither 16 tokens' pieces of 16 bytes nor eight tokens' of 32 meet a bank twice.
 template <int D>
-constexpr int kKv4LdsRow = D + 16;                           // values from token to token: 16 rows in different banks
+__device__ __forceinline__ int kv4_place(int token) { return token * (D * 2 + 32) + (token >> 3 & 1) * 16; }
+template <int D>
+constexpr int kKv4Values = (kKv4WaveStep * (D * 2 + 32) + 16 + 255) / 256 * 256;
 template <int D>
 constexpr int kKv4SumRow = D + 4;                            // floats from row to row when the waves' sums meet
 
@@ -341,9 +346,8 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
     const Kv4ArgsPtr args = (Kv4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
     const Kv4AttnParams& p = *(const Kv4AttnParams*)args;
     constexpr int TQ = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, C = D / 32, DTILES = D / 16, kBytes = DT == kF32 ? 4 : 2;
-    constexpr int kWaveValues = kKv4WaveStep * kKv4LdsRow<D>;
-    static_assert(kWaveValues * 2 >= 16 * kKv4SumRow<D> * 4, "a wave's sums fit where its values were");
-    __shared__ __align__(16) unsigned short staged[kKv4Waves][kWaveValues];
+    static_assert(kKv4Values<D> >= 16 * kKv4SumRow<D> * 4, "a wave's sums of 16 rows fit where its values were");
+    __shared__ __align__(256) char staged[kKv4Waves][kKv4Values<D>];
     __shared__ float wave_top[kKv4Waves][NT * 16], wave_sum_[kKv4Waves][NT * 16];
     __shared__ Kv4Kept kept;
     __shared__ bool is_last;
@@ -440,6 +444,10 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
             if (r < n_rows) {
                 uint4 raw[DT == kF32 ? 2 : 1];
                 load8<DT>(from + kv4_column<D>(c, g) * kBytes, raw);
+#pragma unroll
+                for (int k = 0; k < (DT == kF32 ? 2 : 1); ++k) {
+                    raw[k].x ^= p.q_sign; raw[k].y ^= p.q_sign; raw[k].z ^= p.q_sign; raw[k].w ^= p.q_sign;
+                }
                 if (DT == kBF16) {
                     q[n][0][c] = raw[0];
                 } else {
@@ -477,7 +485,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
 #pragma unroll
         for (int d = 0; d < DTILES; ++d) sum[n][d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    unsigned short* values = staged[wave];
+    char* values = staged[wave];
     auto process = [&](int set, int step) CORAL_INLINE {
         // scores: tokens along the registers (4 g + i of each tile), rows along the lanes
         f32x4_t score[NT][2];
@@ -500,7 +508,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                store_vec(reinterpret_cast<uint4*>(values + (i * 16 + col) * kKv4LdsRow<D> + kv4_column<D>(c, g)),
+                store_vec(reinterpret_cast<uint4*>(values + kv4_place<D>(col) + i * (16 * (D * 2 + 32)) + kv4_column<D>(c, g) * 2),
                           kv4_operand(v[set][i].code[c], kv4_unit(v[set][i].scale[c / 4])));
         const int at = (int)now[set];
         const bool held0 = held[set][0], held1 = held[set][1];
@@ -512,7 +520,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[n][j] = score[n][j / 4][j % 4] * scale_log2;
+            for (int j = 0; j < 8; ++j) s[n][j] = score[n][j / 4][j % 4];
             if (!all_seen) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -522,7 +530,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
                 }
             }
             float top = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
-            top = lane_xor_max<16>(lane_xor_max<32>(top));
+            top = lane_xor_max<16>(lane_xor_max<32>(top)) * scale_log2;
             const bool move = top > ref[n] + kMoveAt || (ref[n] == -INFINITY && top > -INFINITY);
             to[n] = move ? top : ref[n];
             any |= move;
@@ -543,7 +551,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
             float w[8], part[8][TP];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                w[j] = __builtin_amdgcn_exp2f(s[n][j] - base);
+                w[j] = __builtin_amdgcn_exp2f(fmaf(s[n][j], scale_log2, -base));
                 split_bf16<TP>(w[j], part[j]);
             }
             total[n] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
@@ -556,8 +564,8 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int d = 0; d < DTILES; ++d) {
-            const unsigned short* from = values + (4 * g + col / 4) * kKv4LdsRow<D> + d * 16 + (col & 3) * 4;
-            const uint2 lo = lds_transposed(from), hi = lds_transposed(from + 16 * kKv4LdsRow<D>);
+            const char* from = values + kv4_place<D>(4 * g + col / 4) + d * 32 + (col & 3) * 8;
+            const uint2 lo = lds_transposed(from), hi = lds_transposed(from + 16 * (D * 2 + 32));
             const uint4 a = make_uint4(lo.x, lo.y, hi.x, hi.y);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -613,9 +621,13 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
         for (int j = 0; j < D / 16; ++j) o[j] = 0.f;
 #pragma unroll
         for (int w = 0; w < kKv4Waves; ++w) {
-            const float* from = reinterpret_cast<const float*>(staged[w]) + row * kKv4SumRow<D> + d0;
+            const float* from = reinterpret_cast<const float*>(staged[w]);
 #pragma unroll
-            for (int j = 0; j < D / 16; ++j) o[j] = by[w] == 0.f ? o[j] : fmaf(by[w], from[j], o[j]);
+            for (int j = 0; j < D / 16; j += 4) {
+                const f32x4_t x = *reinterpret_cast<const f32x4_t*>(from + row * kKv4SumRow<D> + d0 + j);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[j + i] = by[w] == 0.f ? o[j + i] : fmaf(by[w], x[i], o[j + i]);
+            }
         }
         if (end_of.parts > 1) {
             const int64_t at_row = ((int64_t)blockIdx.x * 2 + slot) * (NT * 16) + n * 16 + row;

@@ -66,7 +66,8 @@ extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, con
     p.page_table = page_table; p.lengths = lengths; p.q_offsets = q_offsets; p.history = history; p.tree = tree;
     p.max_pages = max_pages; p.T = T; p.S = S; p.max_rows = max_rows; p.group = q_heads / kv_heads; p.kv_heads = kv_heads;
     p.workgroups = plan.workgroups; p.apart = plan.apart; p.join_inside = plan.join_inside;
-    p.scale_log2 = scale * kLog2e;
+    p.scale_log2 = score_scale(scale);
+    p.q_sign = score_sign(scale, dt);
     if (need) {
         const size_t rows = (size_t)plan.workgroups * 2 * 16 * plan.tiles;
         static_assert(kKv4Control == coral_ctrl::kPreparedWords * sizeof(unsigned) && kKv4Control % 256 == 0, "");

@@ -25,7 +25,7 @@ constexpr int kv4_most_tiles(int head_dim, int terms) { return head_dim * terms 
 // Workgroups that a compute unit holds: waves on a SIMD that registers are kept for (sums and query operands of the
 // tiles, two steps' codes).
 constexpr int kv4_occupancy(int head_dim, int tiles, int terms) {
-    return head_dim * tiles * (terms + 2) <= 384 ? 3 : head_dim < 256 && head_dim * tiles * (terms + 2) <= 768 ? 2 : 1;
+    return head_dim == 256 ? 1 : tiles == 2 || head_dim * (terms + 2) > 384 ? 2 : 3;
 }
 
 inline Kv4Plan kv4_plan(int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim, int terms) {

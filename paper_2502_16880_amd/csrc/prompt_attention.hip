@@ -50,9 +50,8 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     p.q_stride = in_q.stride; p.k_stride = in_k.stride; p.v_stride = in_v.stride; p.out_stride = out_rows.stride;
     p.q_offsets = q_offsets; p.k_offsets = k_offsets;
     p.T = T; p.keys = keys; p.S = S; p.q_heads = q_heads; p.group = q_heads / kv_heads; p.tiles = (int)tiles; p.parts = parts;
-    // scores are multiplied by a number above zero: the sign goes to q (exactly), and nothing (all weights equal) is little enough
-    p.scale_log2 = fmaxf(fabsf(scale) * 1.44269504088896340736f, 1e-37f);
-    p.q_sign = signbit(scale) ? (dt == CORAL_F32 ? 0x80000000u : 0x80008000u) : 0u;
+    p.scale_log2 = score_scale(scale);
+    p.q_sign = score_sign(scale, dt);
     hipLaunchKernelGGL(prompt_kernel(dt, head_dim), dim3((unsigned)units), dim3(kPromptThreads), 0,
                        static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
