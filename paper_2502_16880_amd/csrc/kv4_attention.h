@@ -676,7 +676,7 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
     constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2, kRows = NT * 16;
     __shared__ float sums[kKv4Waves][D];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int q_head = blockIdx.x, t = blockIdx.y;
+    const int t = blockIdx.x, q_head = blockIdx.y;
     Kv4Line<kRows> line;
     unsigned long long total = 0, start = 0;
     unsigned steps = 0;
@@ -703,23 +703,42 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
     const int64_t first = ((int64_t)w0 * 2 + (line.begin(w0) >= start ? 0 : 1)) * kRows + r % kRows, others = (int64_t)(w0 + 1) * 2 * kRows + r % kRows;
     const int parts = (int)(last - w0) + 1;
     auto row_of = [&](int j) CORAL_INLINE { return j == 0 ? first : others + (int64_t)(j - 1) * 2 * kRows; };
-    float top = -INFINITY;
-    for (int j = lane; j < parts; j += kWave) top = fmaxf(top, p.part_stats[row_of(j)].x);
-    top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(top, [](float a, float b) { return fmaxf(a, b); })));
-    float all = 0.f, o[N];
+    float ref = -INFINITY, all = 0.f, o[N];
 #pragma unroll
     for (int n = 0; n < N; ++n) o[n] = 0.f;
     for (int j0 = 0; j0 < parts; j0 += kWave) {
         float2 stat = make_float2(-INFINITY, 0.f);
         if (j0 + lane < parts) stat = p.part_stats[row_of(j0 + lane)];
-        const float by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
-        all = fmaf(by, stat.y, all);
-#pragma unroll 4
-        for (int j = j0 + wave; j < j0 + kWave && j < parts; j += kKv4Waves) {
-            const float f = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j - j0));
-            const float* from = p.part + row_of(j) * D + lane * N;
+        const int left = parts - j0 < kWave ? parts - j0 : kWave;
+        float x[8][N];
+        auto load = [&](int i) CORAL_INLINE {                    // eight parts of the wave's
 #pragma unroll
-            for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, from[n], o[n]);
+            for (int u = 0; u < 8; ++u) {
+                const int j = i + u * kKv4Waves + wave;
+                const float* from = p.part + row_of(j0 + (j < left ? j : left - 1)) * D + lane * N;
+#pragma unroll
+                for (int n = 0; n < N; ++n) x[u][n] = from[n];
+            }
+        };
+        load(0);
+        float top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(stat.x, [](float a, float b) { return fmaxf(a, b); })));
+        top = fmaxf(top, ref);
+        const float keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top), by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
+        ref = top;
+        all = fmaf(all, keep, by * stat.y);
+#pragma unroll
+        for (int n = 0; n < N; ++n) o[n] *= keep;
+        for (int i = 0;;) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int j = i + u * kKv4Waves + wave;
+                const float f = j < left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j & (kWave - 1))) : 0.f;
+#pragma unroll
+                for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, x[u][n], o[n]);
+            }
+            i += 8 * kKv4Waves;
+            if (i >= left) break;
+            load(i);
         }
     }
     all = wave_sum(all);
