@@ -475,7 +475,7 @@ typedef struct {
  * slot % page_size of page slot / page_size.  The struct is host memory.
  *   codes  [device] [pages][kv_heads][page_size][head_dim/2] bytes, value 2j in the low half of byte j
  *   scales [device] [pages][kv_heads][page_size][head_dim/32] bytes: the unit is 2^(byte - 127); bytes
- *          above 252 count as 252
+ *          above 252 count as 252, in fp16 calls those above 140 as 140 (an append of fp16 has no others)
  * page_size: a power of two from 16 to 4096; pages * page_size below 2^31; all four 16-byte aligned and
  * apart from each other.
  */
@@ -529,8 +529,8 @@ coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, 
  *   with tree:    tokens 0 .. history[s] - 1, and token history[s] + b, where bit b of tree[t] is set, for
  *                 b < 64: a draft tree's nodes see their ancestors and themselves
  * and never a token from lengths[s] on.  A row that sees nothing is zero.  Products are exact but for the
- * weights p, which keep 8 bits of a bf16 call (16 where a sequence has at most 16 rows of queries for a
- * head of keys) and 16 or 24 of an fp16 or fp32 one; sums and statistics are fp32.
+ * weights p, which keep the bits of the storage type, or twice as many where a sequence has at most 16
+ * rows of queries for a head of keys; sums and statistics are fp32.
  *   q          [device] [T,q_heads,head_dim] storage type dt
  *   page_table [device] [S,max_pages] int32; tokens of a page that is none of the cache's are not seen
  *   lengths    [device] [S] int32: tokens in the cache, the new ones among them; cut to 0 .. max_pages *

@@ -73,13 +73,14 @@ def kv4_quantise(x, dtype):
     return code[..., 0::2] | code[..., 1::2] << 4, (e + 127).astype(np.uint8)
 
 
-def kv4_values(codes, scales):
+def kv4_values(codes, scales, dtype="f32"):
+    """What is held, as calls of this type read it."""
     code = unpack(codes.reshape(-1, codes.shape[-1])).reshape(*codes.shape[:-1], -1)
-    unit = np.exp2(np.minimum(scales.astype(np.float64), 252) - 127)
+    unit = np.exp2(np.minimum(scales.astype(np.float64), 127 + LARGEST_UNIT[dtype]) - 127)
     return (E2M1[code].reshape(*scales.shape, 32) * unit[..., None]).reshape(code.shape)
 
 
-def kv4_tokens(codes, scales, page_table, length):
+def kv4_tokens(codes, scales, page_table, length, dtype="f32"):
     """One sequence's tokens [length, kv_heads, D], and which of them lie in a page of the cache."""
     page_size = codes.shape[2]
     if length == 0:
@@ -88,7 +89,7 @@ def kv4_tokens(codes, scales, page_table, length):
     page = np.asarray(page_table)[at // page_size]
     held = (page >= 0) & (page < codes.shape[0])
     page = np.where(held, page, 0)
-    return kv4_values(codes[page, :, at % page_size], scales[page, :, at % page_size]), held
+    return kv4_values(codes[page, :, at % page_size], scales[page, :, at % page_size], dtype), held
 
 
 # ---------------------------------------------------------------- attention

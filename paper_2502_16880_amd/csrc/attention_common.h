@@ -22,6 +22,12 @@ struct Kv4 {
 };
 constexpr unsigned kKv4LargestScale = 252;       // 6 * 2^125 is finite in bf16 and fp32; larger bytes count as this one
 constexpr unsigned kKv4LargestScaleF16 = 140;    // and 6 * 2^13 in fp16
+// A unit as calls of storage type DT read it: no value that they make of it is infinite, whatever the byte.
+template <int DT>
+__device__ __forceinline__ float kv4_unit(unsigned byte) {
+    const unsigned most = DT == kF16 ? kKv4LargestScaleF16 : kKv4LargestScale;
+    return __uint_as_float((byte < most ? byte : most) << 23);
+}
 
 // Eight values of storage type DT as fp32, and back with one rounding to nearest even.
 template <int DT>

@@ -188,8 +188,8 @@ __global__ __launch_bounds__(kHeadThreads) void k_kv4_move(Kv4Params p) {
     uint4 raw[kRaw];
     float x[8];
     if (READ) {
-        const unsigned w = *codes, byte = *scale;
-        const float unit = __uint_as_float((byte < kKv4LargestScale ? byte : kKv4LargestScale) << 23);
+        const unsigned w = *codes;
+        const float unit = kv4_unit<DT>(*scale);
         const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
         const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
         x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1]; x[4] = c[0]; x[5] = c[1]; x[6] = d[0]; x[7] = d[1];

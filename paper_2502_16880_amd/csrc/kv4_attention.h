@@ -2,7 +2,7 @@
 //
 //   out[t,h] = sum_j p_j v_j,  p = softmax_j(scale * q[t,h] . k_j)  over the cached tokens j that row t sees
 //
-// Codes become bf16 operands of the matrix cores exactly (one conversion instruction for two values, the
+// Codes become 16-bit operands of the matrix cores exactly (one conversion instruction for two values, the
 // unit of their 32 included), so scores and sums have exact products and fp32 sums.  A wave takes 32
 // tokens a step: 16 bytes of a token's key a lane, in the order of memory (D = 128: the whole KB of 16 keys
 // in one load); which of the lane's values goes with which column of a product is free as long as the
@@ -11,9 +11,10 @@
 // lane, so converted values pass through the wave's part of LDS and come back transposed
 // (ds_read_b64_tr_b16).  Softmax is taken in one pass: sums are kept relative to a reference of each
 // row that is moved up only when a score passes it by 2^8, so most steps do not touch the sums.
-// fp16 queries are two bf16 values and fp32 ones three (exactly); so are the weights p.
+// Operands of fp16 calls are fp16 (an append of fp16 values has no others), those of fp32 calls three bf16 values for
+// one; so are the weights p.
 #pragma once
-#include "attention_common.h"
+#include "attention_tiles.h"
 #include "control_words.h"
 #include "kv4_plan.h"
 
@@ -165,27 +166,35 @@ struct Kv4Line {
     }
 };
 
-// N bf16 values whose sum is x (8 bits more each).
-template <int N>
-__device__ __forceinline__ void split_bf16(float x, float (&part)[N]) {
+// What products take for calls of storage type DT: fp16 as it is, bf16 as it is, and fp32 as three bf16 values (exactly).
+constexpr int kv4_operand_type(int dt) { return dt == kF16 ? kF16 : kBF16; }
+constexpr int kv4_terms(int dt) { return dt == kF32 ? 3 : 1; }
+// N values of type OT whose sum is x (8 or 11 bits more each).
+template <int OT, int N>
+__device__ __forceinline__ void split_terms(float x, float (&part)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        part[i] = (float)(__bf16)x;
+        part[i] = OT == kF16 ? (float)(_Float16)x : (float)(__bf16)x;
         x -= part[i];
     }
 }
 
-// A dword of codes with its unit as eight bf16 values.
+// A dword of codes with its unit as eight values of type OT.
+template <int OT>
 __device__ __forceinline__ uint4 kv4_operand(unsigned codes, float unit) {
     uint4 r;
-    r.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0));
-    r.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1));
-    r.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2));
-    r.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3));
+    if (OT == kF16) {
+        r.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, unit, 0));
+        r.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, unit, 1));
+        r.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, unit, 2));
+        r.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, unit, 3));
+    } else {
+        r.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0));
+        r.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1));
+        r.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2));
+        r.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3));
+    }
     return r;
-}
-__device__ __forceinline__ float kv4_unit(unsigned byte) {
-    return __uint_as_float((byte < kKv4LargestScale ? byte : kKv4LargestScale) << 23);
 }
 
 // Sixteen tokens' codes of one kind as a lane holds them: dword c of lane (token, g) has the values
@@ -218,19 +227,6 @@ __device__ __forceinline__ void kv4_load(Kv4Tile<D>& t, const unsigned char* cod
             t.scale[i % Kv4Tile<D>::kScales] = scales[token * (D / 32u) + i * 4u + g];
         }
     }
-}
-
-__device__ __forceinline__ f32x4_t mfma_bf16(uint4 a, uint4 b, f32x4_t acc) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
-}
-
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
-// Four rows of LDS, 16 columns: lane l of sixteen gets column l of the rows whose pieces the lanes point at
-// (lane l: row l / 4, columns 4 (l % 4) on).
-__device__ __forceinline__ uint2 lds_transposed(const char* at) {
-    const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(at));
-    return __builtin_bit_cast(uint2, r);
 }
 
 // Where a token's values begin in a wave's part of LDS (bytes): eight banks further from token to token and four more for
@@ -341,11 +337,11 @@ typedef const __attribute__((address_space(4))) Kv4AttnParams* Kv4ArgsPtr;
 // all steps is a run of them that may cross items: the first and the last may be parts of an item, which the item's last
 // workgroup puts together, or, where parts and rows are many, k_kv4_join.
 template <int DT, int D, int NT, int TP>
-__global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 : DT == kF16 ? 2 : 3))) void k_kv4_attention(Kv4AttnParams) {
+__global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT)))) void k_kv4_attention(Kv4AttnParams) {
     // The arguments are read where they are used: held in scalar registers all the way they would be spilled.
     const Kv4ArgsPtr args = (Kv4ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
     const Kv4AttnParams& p = *(const Kv4AttnParams*)args;
-    constexpr int TQ = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, C = D / 32, DTILES = D / 16, kBytes = DT == kF32 ? 4 : 2;
+    constexpr int OT = kv4_operand_type(DT), TQ = kv4_terms(DT), C = D / 32, DTILES = D / 16, kBytes = DT == kF32 ? 4 : 2;
     static_assert(kKv4Values<D> >= 16 * kKv4SumRow<D> * 4, "a wave's sums of 16 rows fit where its values were");
     __shared__ __align__(256) char staged[kKv4Waves][kKv4Values<D>];
     __shared__ float wave_top[kKv4Waves][NT * 16], wave_sum_[kKv4Waves][NT * 16];
@@ -448,17 +444,17 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
                 for (int k = 0; k < (DT == kF32 ? 2 : 1); ++k) {
                     raw[k].x ^= p.q_sign; raw[k].y ^= p.q_sign; raw[k].z ^= p.q_sign; raw[k].w ^= p.q_sign;
                 }
-                if (DT == kBF16) {
+                if (TQ == 1) {
                     q[n][0][c] = raw[0];
                 } else {
                     float x[8], part[8][TQ];
                     widen8<DT>(raw, x);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) split_bf16<TQ>(x[j], part[j]);
+                    for (int j = 0; j < 8; ++j) split_terms<OT>(x[j], part[j]);
 #pragma unroll
                     for (int k = 0; k < TQ; ++k)
-                        q[n][k][c] = make_uint4(narrow2<kBF16>(part[0][k], part[1][k]), narrow2<kBF16>(part[2][k], part[3][k]),
-                                                narrow2<kBF16>(part[4][k], part[5][k]), narrow2<kBF16>(part[6][k], part[7][k]));
+                        q[n][k][c] = make_uint4(narrow2<OT>(part[0][k], part[1][k]), narrow2<OT>(part[2][k], part[3][k]),
+                                                narrow2<OT>(part[4][k], part[5][k]), narrow2<OT>(part[6][k], part[7][k]));
                 }
             } else {
 #pragma unroll
@@ -495,11 +491,11 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
             for (int n = 0; n < NT; ++n) score[n][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const uint4 a = kv4_operand(k[set][i].code[c], kv4_unit(k[set][i].scale[c / 4]));
+                const uint4 a = kv4_operand<OT>(k[set][i].code[c], kv4_unit<DT>(k[set][i].scale[c / 4]));
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int t = 0; t < TQ; ++t) score[n][i] = mfma_bf16(a, q[n][t][c], score[n][i]);
+                    for (int t = 0; t < TQ; ++t) score[n][i] = mfma_tile<OT>(a, q[n][t][c], score[n][i]);
             }
         }
         // values into LDS, token by token
@@ -509,7 +505,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 store_vec(reinterpret_cast<uint4*>(values + kv4_place<D>(col) + i * (16 * (D * 2 + 32)) + kv4_column<D>(c, g) * 2),
-                          kv4_operand(v[set][i].code[c], kv4_unit(v[set][i].scale[c / 4])));
+                          kv4_operand<OT>(v[set][i].code[c], kv4_unit<DT>(v[set][i].scale[c / 4])));
         const int at = (int)now[set];
         const bool held0 = held[set][0], held1 = held[set][1];
         const bool all_seen = at + kKv4WaveStep <= seen_by_all && held0 && held1;
@@ -552,13 +548,13 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 w[j] = __builtin_amdgcn_exp2f(fmaf(s[n][j], scale_log2, -base));
-                split_bf16<TP>(w[j], part[j]);
+                split_terms<OT>(w[j], part[j]);
             }
             total[n] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 #pragma unroll
             for (int t = 0; t < TP; ++t)
-                weight[n][t] = make_uint4(narrow2<kBF16>(part[0][t], part[1][t]), narrow2<kBF16>(part[2][t], part[3][t]),
-                                          narrow2<kBF16>(part[4][t], part[5][t]), narrow2<kBF16>(part[6][t], part[7][t]));
+                weight[n][t] = make_uint4(narrow2<OT>(part[0][t], part[1][t]), narrow2<OT>(part[2][t], part[3][t]),
+                                          narrow2<OT>(part[4][t], part[5][t]), narrow2<OT>(part[6][t], part[7][t]));
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -570,7 +566,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, DT == kBF16 ? 1 
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int t = 0; t < TP; ++t) sum[n][d] = mfma_bf16(a, weight[n][t], sum[n][d]);
+                for (int t = 0; t < TP; ++t) sum[n][d] = mfma_tile<OT>(a, weight[n][t], sum[n][d]);
         }
         __builtin_amdgcn_wave_barrier();
     };
@@ -756,18 +752,18 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
 
 using kv4_attn_fn = void (*)(Kv4AttnParams);
 using kv4_join_fn = void (*)(Kv4AttnParams);
-// The weights p of bf16 calls are two bf16 values where a wave has one tile (which memory bounds: no cost; the result's
-// only rounding is then its own) and one where it has more (the products bound it: a second term would
-// take a third longer; the roundings of single weights, 2^-9 each, average out to about the result's own).
+// The weights p of bf16 and fp16 calls are two values of that type where a wave has one tile (which memory bounds: no cost;
+// the result's only rounding is then its own) and one where it has more (the products bound it: a second would take half
+// as long again; the roundings of single weights, 2^-9 and 2^-12 each, average out to about the result's own).
 template <int DT, int D>
 kv4_attn_fn kv4_kernel(int tiles) {
-    constexpr int terms = DT == kBF16 ? 1 : DT == kF16 ? 2 : 3, most = kv4_most_tiles(D, terms), many = DT == kBF16 ? 1 : terms;
+    constexpr int most = kv4_most_tiles(D, kv4_terms(DT)), many = kv4_terms(DT);
     if (tiles == 2) return k_kv4_attention<DT, D, most >= 2 ? 2 : 1, most >= 2 ? many : DT == kF32 ? 3 : 2>;
     return k_kv4_attention<DT, D, 1, DT == kF32 ? 3 : 2>;
 }
 template <int DT, int D>
 kv4_join_fn kv4_join(int tiles) {
-    constexpr int most = kv4_most_tiles(D, DT == kBF16 ? 1 : DT == kF16 ? 2 : 3);
+    constexpr int most = kv4_most_tiles(D, kv4_terms(DT));
     return tiles == 2 ? k_kv4_join<DT, D, most >= 2 ? 2 : 1> : k_kv4_join<DT, D, 1>;
 }
 

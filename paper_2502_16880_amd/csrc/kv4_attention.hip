@@ -18,7 +18,7 @@ coral_status check_kv4_sizes(int T, int S, int max_rows, int max_length, int q_h
     if (!head_dim_known(head_dim) || q_heads > kMostHeads || S > kMostSequences || max_rows > kKv4MostRows) return CORAL_ERR_UNSUPPORTED;
     return CORAL_OK;
 }
-int query_terms(coral_dtype dt) { return dt == CORAL_BF16 ? 1 : dt == CORAL_F16 ? 2 : 3; }
+int query_terms(coral_dtype dt) { return dt == CORAL_F32 ? 3 : 1; }
 
 }  // namespace
 

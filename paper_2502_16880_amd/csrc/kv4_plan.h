@@ -4,7 +4,7 @@
 #include <stdint.h>
 
 struct Kv4Plan {
-    int tiles;         // tiles of 16 rows (a row: one token, one query head) that a workgroup takes together
+    int tiles;         // tiles of 16 rows (a row: one token, one query head) that a workgroup takes together: 1 or 2
     int row_blocks;    // so many times that, at most, for one sequence's rows of one head of keys
     int workgroups;    // among which all sequences' steps are shared equally, or
     bool apart;        // one workgroup for each sequence, head of keys and block of rows
@@ -19,8 +19,8 @@ constexpr int kKv4Apart = 256;          // sequences beyond which they are not s
 constexpr int kKv4JoinRows = 8;         // rows and parts of an item, at most, that one workgroup joins as fast as another
 constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave
 
-// Query operands and sums of a wave's tiles stay in registers: with `terms` bf16 values for a query value
-// (1 for bf16, 2 for fp16, 3 for fp32) this many tiles fit.
+// Query operands and sums of a wave's tiles stay in registers: with `terms` 16-bit values for a query value
+// (3 for fp32, else 1) this many tiles fit.
 constexpr int kv4_most_tiles(int head_dim, int terms) { return head_dim * terms <= 128 ? 2 : 1; }
 // Workgroups that a compute unit holds: waves on a SIMD that registers are kept for (sums and query operands of the
 // tiles, two steps' codes).

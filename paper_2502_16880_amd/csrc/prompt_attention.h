@@ -11,7 +11,7 @@
 // pieces whose place in a row is exchanged by the row's number, so that neither the reading of keys (16 rows, one
 // piece each) nor the transposing one of values (four rows, four pieces each) meets a bank twice.
 #pragma once
-#include "attention_common.h"
+#include "attention_tiles.h"
 
 #include <type_traits>
 
@@ -21,9 +21,6 @@ constexpr int kPromptThreads = 256;
 constexpr int kPromptWaves = kPromptThreads / kWave;
 constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
 constexpr int kXcds = 8;
-
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
 struct PromptParams {
     const char *q, *k, *v;
@@ -145,23 +142,6 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, 
     return r;
 }
 
-// Place of 16-byte piece c of row r in LDS (bytes), rows of `pieces` pieces.
-template <int PIECES>
-__device__ __forceinline__ int prompt_place(int r, int c) {
-    const int f = PIECES == 8 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
-    return (r * PIECES + (c ^ f)) * 16;
-}
-
-template <int DT>
-__device__ __forceinline__ f32x16_t mfma_32(uint4 a, uint4 b, f32x16_t acc) {
-    if (DT == kF16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), acc, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
-}
-__device__ __forceinline__ uint2 prompt_transposed(const char* at) {
-    const s16x4_t r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4_t*)const_cast<char*>(at));
-    return __builtin_bit_cast(uint2, r);
-}
-
 // Two 16-bit values, those that are infinite or NaN made zero; `odd` tells whether there were any.
 template <int DT>
 __device__ __forceinline__ unsigned only_finite2(unsigned w, bool& odd) {
@@ -174,12 +154,6 @@ __device__ __forceinline__ unsigned only_finite(unsigned w, bool& odd) {
     const bool bad = (w & 0x7f800000u) == 0x7f800000u;
     odd |= bad;
     return bad ? 0u : w;
-}
-// acc plus two values.
-template <int DT>
-__device__ __forceinline__ float add_pair(unsigned w, float acc) {
-    if (DT == kF16) return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, w), __builtin_bit_cast(f16x2_t, 0x3c003c00u), acc, false);
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), acc, false);
 }
 // Keys 0 .. most of a tile, one bit each.
 __device__ __forceinline__ unsigned long long keys_to(int most) { return most < 0 ? 0ull : most > 62 ? ~0ull : (2ull << most) - 1ull; }
@@ -220,7 +194,7 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
     unsigned k_at[LOADS], v_at[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = prompt_place<PIECES>(r, at % PIECES) / 16 % PIECES;
+        const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = tile_place<PIECES>(r, at % PIECES) / 16 % PIECES;
         k_at[i] = (unsigned)(r * (int)p.k_stride + c * 16);
         v_at[i] = (unsigned)(r * (int)p.v_stride + c * 16);
     }
@@ -256,8 +230,8 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
     const float scale_log2 = p.scale_log2;
     // operands' places in a buffer: keys (32 kt + col, piece 2 c + h), values (column 32 d + lane % 32; keys 16 c + 4 h + 0..3 and
     // 16 c + 8 + 4 h + 0..3: rows r = 4 h + lane % 16 / 4 and r + 8, lanes pointing at four pieces of eight bytes)
-    const int k_place = prompt_place<PIECES>(col, h), r = 4 * h + (lane & 15) / 4, quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2;
-    const int v_place = prompt_place<PIECES>(r, quad) + (lane & 1) * 8, v_place8 = prompt_place<PIECES>(r + 8, quad) + (lane & 1) * 8;
+    const int k_place = tile_place<PIECES>(col, h), r = 4 * h + (lane & 15) / 4, quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2;
+    const int v_place = tile_place<PIECES>(r, quad) + (lane & 1) * 8, v_place8 = tile_place<PIECES>(r + 8, quad) + (lane & 1) * 8;
     if (threadIdx.x < 4) lds.odd[threadIdx.x] = 0;
     dma_arrived();
     __syncthreads();
@@ -330,8 +304,8 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
             constexpr int M = DT32 * KC, VAHEAD = 4;
             uint4 b[VAHEAD];
             auto value_operand = [&](int i) CORAL_INLINE {
-                const uint2 lo = prompt_transposed(values + (v_place ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
-                const uint2 hi = prompt_transposed(values + (v_place8 ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
+                const uint2 lo = lds_transposed(values + (v_place ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
+                const uint2 hi = lds_transposed(values + (v_place8 ^ (i % DT32 * 64)) + i / DT32 * (16 * PIECES * 16));
                 return make_uint4(lo.x, lo.y, hi.x, hi.y);
             };
 #pragma unroll

@@ -246,7 +246,7 @@ def test_plan_covers_every_row_and_the_workspace_what_it_needs(tmp_path):
     exe = str(tmp_path / "plan")
     subprocess.run(["g++", "-std=c++17", "-I", os.path.join(ROOT, "paper_2502_16880_amd", "csrc"), str(tmp_path / "plan.cpp"), "-o", exe], check=True)
     calls = [(s, rows, length, q, kv, d, terms) for s in (1, 3, 64, 65535) for rows in (1, 5, 64) for length in (0, 1, 128, 129, 8192, 2 ** 31 - 1)
-             for q, kv in ((8, 8), (32, 8), (28, 4), (1024, 1)) for d in (64, 128, 256) for terms in (1, 2, 3)]
+             for q, kv in ((8, 8), (32, 8), (28, 4), (1024, 1)) for d in (64, 128, 256) for terms in (1, 3)]
     text = subprocess.run([exe], input="\n".join(" ".join(map(str, c)) for c in calls), capture_output=True, text=True, check=True).stdout
     for (s, rows, length, q, kv, d, terms), line in zip(calls, text.splitlines()):
         tiles, blocks, groups, apart, need = map(int, line.split())
@@ -254,5 +254,4 @@ def test_plan_covers_every_row_and_the_workspace_what_it_needs(tmp_path):
         assert tiles == 1 or d * terms <= 128
         assert 1 <= groups <= 768 and groups <= s * kv * blocks * max(1, -(-length // 128)) and apart == (s > 256)
         assert need == (16896 + groups * 2 * tiles * 16 * (d + 2) * 4 if groups > 1 and not apart else 0)
-        dt = {1: BF16, 2: F16, 3: F32}[terms]
-        assert coral.coral_attention_kv4_workspace_bytes(s, rows, length, q, kv, d, dt) >= max(need, 256)
+        assert all(coral.coral_attention_kv4_workspace_bytes(s, rows, length, q, kv, d, dt) >= max(need, 256) for dt in ((BF16, F16) if terms == 1 else (F32,)))

@@ -192,7 +192,7 @@ def test_kv4_append_and_read(coral, dtype, T, kv_heads, D, page):
     coral.coral_kv4_read(cache, ints(slots), TORCH[dtype], k_out, v_out)
     for out, (codes, scales) in ((k_out, sides[0]), (v_out, sides[1])):
         want = np.full((T, kv_heads, D), 77.0)
-        want[good] = plain.kv4_values(codes[at, :, off], scales[at, :, off])
+        want[good] = plain.kv4_values(codes[at, :, off], scales[at, :, off], dtype)
         want = torch.from_numpy(want).to(TORCH[dtype])
         assert torch.equal(out.cpu().nan_to_num(), want.nan_to_num())
     k_kept()
@@ -210,7 +210,7 @@ def test_kv4_read_any_byte(coral, dtype):
     cache, sides = random_cache(coral, rng, 16, 16, 2, 64, scales=(0, 256))
     out = coral.coral_kv4_read(cache, ints(np.arange(256)), TORCH[dtype])
     for got, (codes, scales) in zip(out, sides):
-        want = plain.kv4_values(codes, scales).transpose(0, 2, 1, 3).reshape(256, 2, 64)
+        want = plain.kv4_values(codes, scales, dtype).transpose(0, 2, 1, 3).reshape(256, 2, 64)
         assert torch.equal(got.cpu(), torch.from_numpy(want).to(TORCH[dtype]))
 
 
@@ -293,8 +293,8 @@ class Cached:
         for s, (n, r) in enumerate(self.sequences):
             if only is not None and s not in only:
                 continue
-            k, held = plain.kv4_tokens(*self.sides[0], self.table[s], n)
-            v, _ = plain.kv4_tokens(*self.sides[1], self.table[s], n)
+            k, held = plain.kv4_tokens(*self.sides[0], self.table[s], n, self.dtype)
+            v, _ = plain.kv4_tokens(*self.sides[1], self.table[s], n, self.dtype)
             rows = slice(self.offsets[s], self.offsets[s + 1])
             want = plain.attention(self.q64[rows], k, v, self.seen(s) & held[None], D ** -0.5 if scale is None else scale)
             check_attention(got[rows], want, self.dtype, n, f"sequence {s} of {n} tokens, {r} rows")
