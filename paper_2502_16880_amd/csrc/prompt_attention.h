@@ -60,16 +60,16 @@ __device__ __forceinline__ PromptSeq prompt_sequence(const PromptParams& p, int 
 __device__ __forceinline__ int wave_sum_int(int x) { return __builtin_amdgcn_readlane(wave_scan_inclusive(x), kWave - 1); }
 
 // Workgroups are dealt to the eight dies in turn, and a die takes neighbouring heads, whose keys are then read through one
-// L2: of `parts` as few as make the heads' parts a multiple of eight, a part being every parts-th tile.  One sequence's
-// tiles come head after head, the last rows, which see most, first.  Of several sequences, tiles of all heads come by
-// their levels, the longest first: twelve prompts of 8191 tokens whose tiles came in order took 148 us, the last of them alone.
+// L2: of `parts` as few as make the heads' parts a multiple of eight, a part being every parts-th tile.  Tiles of all of a
+// die's heads come by their levels, the longest first: twelve prompts of 8191 tokens whose tiles came in order took 148 us,
+// the last of them alone, against 118; one of 8192 whose tiles came head after head 527 us against 508, of 2115 64 against 55.
 template <int ROWS>
 __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, int lane) {
     PromptTile r = {};
     const int die = x % kXcds, local = x / kXcds, mine = p.q_heads * p.parts / kXcds;        // heads' parts of a die
     const int per = (p.tiles + p.parts - 1) / p.parts;
-    const int of = p.S == 1 ? local / per : local % mine, at = p.S == 1 ? local - of * per : local / mine;
-    if (of >= mine || at >= per) return r;
+    const int of = local % mine, at = local / mine;
+    if (at >= per) return r;
     const int part = die * mine + of;
     r.head = part / p.parts;
     const int rank = at * p.parts + part % p.parts;
@@ -167,15 +167,21 @@ __device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)
 
 // 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
 // (2^-12) each with random signs, which come to about the result's own rounding.
-template <int DT, int D>
-__global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(PromptParams p) {
-    constexpr int BN = D == 256 ? 32 : 64, ROWS = 128, PIECES = D / 8, LOADS = BN * PIECES / kPromptThreads;
+// RW waves take 32 rows each; with KS = 2 two such groups take every second tile of keys and add up at the end, so that a
+// row's way along its keys is half as long (the entry point takes that where the card has few rows).
+template <int DT, int D, int RW, int KS>
+__global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(PromptParams p) {
+    constexpr int kGroup = RW * kWave;
+    constexpr int BN = D == 256 ? 32 : 64, ROWS = RW * 32, PIECES = D / 8, LOADS = BN * PIECES / kGroup;
     constexpr int QC = D / 16, KT = BN / 32, DT32 = D / 32, KC = BN / 16, kTile = BN * D * 2;
+    static_assert(KS == 1 || KS * 4 * kTile >= ROWS * D * 4, "a group's sums fit where the tiles were");
     __shared__ struct {
-        __align__(256) char tile[2][2][kTile];                   // [buffer][keys, values]
-        unsigned long long odd[4];                               // of a tile that rows see a part of: keys whose values are not finite
+        __align__(256) char tile[KS][2][2][kTile];               // [group][buffer][keys, values]
+        unsigned long long odd[KS][4];                           // of a tile that rows see a part of: keys whose values are not finite
+        float2 stats[KS == 1 ? 1 : ROWS];
     } lds;
-    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x & (kWave - 1), all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int group = KS == 1 ? 0 : all_wave / RW, wave = KS == 1 ? all_wave : all_wave % RW, thread = wave * kWave + lane;
     const int col = lane & 31, h = lane >> 5;
     const PromptTile t = prompt_tile<ROWS>(p, blockIdx.x, lane);
     if (!t.any) return;
@@ -190,24 +196,28 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
     const char* k_base = p.k + (int64_t)t.k0 * p.k_stride + kv_head * (D * 2);
     const char* v_base = p.v + (int64_t)t.k0 * p.v_stride + kv_head * (D * 2);
     const size_t k_bytes = t.keys ? (size_t)(t.keys - 1) * p.k_stride + D * 2 : 0, v_bytes = t.keys ? (size_t)(t.keys - 1) * p.v_stride + D * 2 : 0;
-    // piece i * 256 + thread of a tile goes to that place of LDS; which piece of the row that is, is exchanged by the row's number
+    // the group's piece i * kGroup + thread of a tile goes to that place of LDS; which piece of the row that is, is exchanged by
+    // the row's number
     unsigned k_at[LOADS], v_at[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = tile_place<PIECES>(r, at % PIECES) / 16 % PIECES;
+        const int at = i * kGroup + thread, r = at / PIECES, c = tile_place<PIECES>(r, at % PIECES) / 16 % PIECES;
         k_at[i] = (unsigned)(r * (int)p.k_stride + c * 16);
         v_at[i] = (unsigned)(r * (int)p.v_stride + c * 16);
     }
-    const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&lds.tile[0][0][0];
-    auto fetch = [&](int tile) CORAL_INLINE {
+    char* const tiles = &lds.tile[group][0][0][0];
+    const unsigned lds_base = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)tiles;
+    auto fetch = [&](int j) CORAL_INLINE {                       // the group's j-th tile
+        const int tile = j * KS + group;
+        if (tile >= n_tiles) return;                             // (uniform over the wave)
         const Buffer kb = buffer_view(k_base, (size_t)tile * BN * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)tile * BN * p.v_stride, v_bytes);
-        const unsigned to = __builtin_amdgcn_readfirstlane(lds_base + (tile & 1) * 2 * kTile + wave * 1024);
+        const unsigned to = __builtin_amdgcn_readfirstlane(lds_base + (j & 1) * 2 * kTile + wave * 1024);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) dma_piece(kb, k_at[i], to + i * 4096);
+        for (int i = 0; i < LOADS; ++i) dma_piece(kb, k_at[i], to + i * (kGroup * 16));
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) dma_piece(vb, v_at[i], to + kTile + i * 4096);
+        for (int i = 0; i < LOADS; ++i) dma_piece(vb, v_at[i], to + kTile + i * (kGroup * 16));
     };
-    if (n_tiles > 0) fetch(0);
+    fetch(0);
     uint4 q[QC];
     {
         const char* from = p.q + (int64_t)(t.row0 + row) * p.q_stride + (int64_t)head * (D * 2) + h * 16;
@@ -232,31 +242,34 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
     // 16 c + 8 + 4 h + 0..3: rows r = 4 h + lane % 16 / 4 and r + 8, lanes pointing at four pieces of eight bytes)
     const int k_place = tile_place<PIECES>(col, h), r = 4 * h + (lane & 15) / 4, quad = (lane >> 4 & 1) * 2 + (lane & 3) / 2;
     const int v_place = tile_place<PIECES>(r, quad) + (lane & 1) * 8, v_place8 = tile_place<PIECES>(r + 8, quad) + (lane & 1) * 8;
-    if (threadIdx.x < 4) lds.odd[threadIdx.x] = 0;
+    if (thread < 4) lds.odd[group][thread] = 0;
     dma_arrived();
     __syncthreads();
     // one tile: CUT where some row may see a part of it only
     auto step = [&](int j, auto parity, auto may_cut) CORAL_INLINE {
         constexpr bool CUT = decltype(may_cut)::value;
-        const char *keys = &lds.tile[0][0][0] + parity * (2 * kTile), *values = keys + kTile;
-        if (j + 1 < n_tiles) fetch(j + 1);
-        const int k0 = j * BN;
+        const char *keys = tiles + parity * (2 * kTile), *values = keys + kTile;
+        fetch(j + 1);
+        const int tile = j * KS + group, k0 = tile * BN;
         if (CUT) {
+            if (tile < n_tiles) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                uint4* at = reinterpret_cast<uint4*>(const_cast<char*>(values) + (i * kPromptThreads + threadIdx.x) * 16);
-                const uint4 raw = load_vec(at);
-                bool bad = false;
-                const uint4 fine = make_uint4(only_finite2<DT>(raw.x, bad), only_finite2<DT>(raw.y, bad), only_finite2<DT>(raw.z, bad), only_finite2<DT>(raw.w, bad));
-                if (bad) {
-                    store_vec(at, fine);
-                    atomicOr(&lds.odd[j & 3], 1ull << ((i * kPromptThreads + (int)threadIdx.x) / PIECES));
+                for (int i = 0; i < LOADS; ++i) {
+                    uint4* at = reinterpret_cast<uint4*>(const_cast<char*>(values) + (i * kGroup + thread) * 16);
+                    const uint4 raw = load_vec(at);
+                    bool bad = false;
+                    const uint4 fine = make_uint4(only_finite2<DT>(raw.x, bad), only_finite2<DT>(raw.y, bad), only_finite2<DT>(raw.z, bad), only_finite2<DT>(raw.w, bad));
+                    if (bad) {
+                        store_vec(at, fine);
+                        atomicOr(&lds.odd[group][j & 3], 1ull << ((i * kGroup + thread) / PIECES));
+                    }
                 }
             }
-            if (threadIdx.x == 0) lds.odd[(j + 2) & 3] = 0;      // tile j - 2's
+            if (thread == 0) lds.odd[group][(j + 2) & 3] = 0;    // the group's tile before the last
             __syncthreads();
         }
-        if (!CUT || (k0 <= reach + my_first + 31 && my_first < t.rows)) {      // some row of the wave sees some key (uniform)
+        // some row of the wave sees some key (uniform)
+        if (!CUT || (tile < n_tiles && k0 <= reach + my_first + 31 && my_first < t.rows)) {
             f32x16_t s[KT];
             constexpr int N = KT * QC, AHEAD = 8;                // products, and operands on their way
             uint4 a[AHEAD];
@@ -320,7 +333,7 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
             };
 #pragma unroll
             for (int g = 0; g < 4; ++g) weigh(0, g);
-            if (CUT && (lds.odd[j & 3] & keys_to(most))) total = NAN;
+            if (CUT && (lds.odd[group][j & 3] & keys_to(most))) total = NAN;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < M; ++i) {
@@ -338,14 +351,40 @@ __global__ __launch_bounds__(kPromptThreads, D == 256 ? 1 : 2) void k_prompt(Pro
         __syncthreads();
     };
     int j = 0;
-    const int whole = first_cut < n_tiles ? first_cut : n_tiles;
+    const int whole = (first_cut < n_tiles ? first_cut : n_tiles) / KS, rounds = (n_tiles + KS - 1) / KS;
     for (; j + 1 < whole; j += 2) {
         step(j, std::integral_constant<int, 0>(), std::false_type());
         step(j + 1, std::integral_constant<int, 1>(), std::false_type());
     }
     for (; j < whole; ++j) step(j, j & 1, std::false_type());
-    for (; j < n_tiles; ++j) step(j, j & 1, std::true_type());
-    total = lane_xor_sum<32>(total);
+    for (; j < rounds; ++j) step(j, j & 1, std::true_type());
+    if (KS == 2) {                                               // the second group hands its sums over, lane to lane
+        f32x4_t* to = reinterpret_cast<f32x4_t*>(&lds.tile[0][0][0][0]) + wave * (DT32 * 4 * kWave) + lane;
+        total = lane_xor_sum<32>(total);
+        if (group == 1) {
+#pragma unroll
+            for (int d = 0; d < DT32; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[(d * 4 + i) * kWave] = f32x4_t{sum[d][4 * i], sum[d][4 * i + 1], sum[d][4 * i + 2], sum[d][4 * i + 3]};
+            if (h == 0) lds.stats[wave * 32 + col] = make_float2(ref, total);
+        }
+        __syncthreads();
+        if (group == 1) return;
+        const float2 other = lds.stats[wave * 32 + col];
+        const float top = fmaxf(ref, other.x), mine = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+        const float its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - top);
+        total = total * mine + other.y * its;
+#pragma unroll
+        for (int d = 0; d < DT32; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4_t x = to[(d * 4 + i) * kWave];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[d][4 * i + e] = fmaf(x[e], its, sum[d][4 * i + e] * mine);
+            }
+    } else {
+        total = lane_xor_sum<32>(total);
+    }
     if (row >= t.rows) return;
     const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;          // a row that sees nothing: zeros
     char* to = p.out + (int64_t)(t.row0 + row) * p.out_stride + (int64_t)head * (D * 2) + h * 8;

@@ -5,13 +5,26 @@
 
 namespace {
 
+// Tiles of 128 rows, over all heads, up to which two groups of waves share a workgroup's keys.  One prompt, us with one group and with
+// two: 100 tiles of D = 128 12.8 and 12.6, 256 27.3 and 23.9, 384 39.8 and 34.5, 544 54.6 and 59.3, 1056 148 and 154;  D = 64: 192 30.9
+// and 24.7, 384 57.4 and 42.7, 756 131 and 135;  D = 256 (64 rows by two groups): 136 88 and 57, 256 156 and 112, 504 329 and 385.
+constexpr int64_t kFewUnits = 400;
 constexpr int64_t kMostStride = 1 << 24;         // bytes: a tile's rows are addressed by 32-bit offsets
 
 using prompt_fn = void (*)(PromptParams);
-prompt_fn prompt_kernel(coral_dtype dt, int d) {
-    if (dt == CORAL_F32) return d == 64 ? k_prompt_f32<64> : d == 128 ? k_prompt_f32<128> : k_prompt_f32<256>;
-    if (dt == CORAL_BF16) return d == 64 ? k_prompt<kBF16, 64> : d == 128 ? k_prompt<kBF16, 128> : k_prompt<kBF16, 256>;
-    return d == 64 ? k_prompt<kF16, 64> : d == 128 ? k_prompt<kF16, 128> : k_prompt<kF16, 256>;
+struct PromptForm {
+    prompt_fn fn;
+    int rows, threads;
+};
+template <int DT>
+PromptForm prompt_form(int d, bool few) {
+    if (d == 64) return few ? PromptForm{k_prompt<DT, 64, 4, 2>, 128, 512} : PromptForm{k_prompt<DT, 64, 4, 1>, 128, 256};
+    if (d == 128) return few ? PromptForm{k_prompt<DT, 128, 4, 2>, 128, 512} : PromptForm{k_prompt<DT, 128, 4, 1>, 128, 256};
+    return few ? PromptForm{k_prompt<DT, 256, 2, 2>, 64, 256} : PromptForm{k_prompt<DT, 256, 4, 1>, 128, 256};
+}
+PromptForm prompt_form(coral_dtype dt, int d, bool few) {
+    if (dt == CORAL_F32) return {d == 64 ? k_prompt_f32<64> : d == 128 ? k_prompt_f32<128> : k_prompt_f32<256>, 64, 256};
+    return dt == CORAL_BF16 ? prompt_form<kBF16>(d, few) : prompt_form<kF16>(d, few);
 }
 
 }  // namespace
@@ -39,7 +52,8 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     if (rows_overlap(out_rows, in_q) || rows_overlap(out_rows, in_k) || rows_overlap(out_rows, in_v) ||
         rows_overlap(out_rows, {q_offsets, offsets, offsets, 1}) || rows_overlap(out_rows, {k_offsets, offsets, offsets, 1}))
         return CORAL_ERR_UNSUPPORTED;
-    const int rows = dt == CORAL_F32 ? 64 : 128;
+    const PromptForm form = prompt_form(dt, head_dim, (int64_t)(T / 128 + 1) * q_heads <= kFewUnits);
+    const int rows = form.rows;
     const int64_t tiles = T / rows + (S < T ? S : T);        // each sequence has at most one tile that is not full
     int parts = 1;
     while (q_heads * parts % kXcds) parts *= 2;
@@ -52,7 +66,7 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     p.T = T; p.keys = keys; p.S = S; p.q_heads = q_heads; p.group = q_heads / kv_heads; p.tiles = (int)tiles; p.parts = parts;
     p.scale_log2 = score_scale(scale);
     p.q_sign = score_sign(scale, dt);
-    hipLaunchKernelGGL(prompt_kernel(dt, head_dim), dim3((unsigned)units), dim3(kPromptThreads), 0,
+    hipLaunchKernelGGL(form.fn, dim3((unsigned)units), dim3(form.threads), 0,
                        static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }

@@ -522,6 +522,17 @@ def test_attention_prompt_long(coral, dtype, D, q_heads, kv_heads, lengths):
     assert torch.equal(c.run(), out)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("D,q_heads,kv_heads,lengths", [(64, 160, 16, [(400, 400), (130, 200), (3, 3)]), (128, 160, 32, [(257, 257), (300, 330)]), (256, 96, 8, [(600, 600), (129, 129)])])
+def test_attention_prompt_many_heads(coral, dtype, D, q_heads, kv_heads, lengths):
+    c = Prompt(coral, dtype, lengths, q_heads, kv_heads, D)
+    out, kept = guarded(c.q.shape, TORCH[dtype])
+    c.run(out=out)
+    c.check(out, rows=20)
+    kept()
+    assert torch.equal(c.run(), out)
+
+
 def test_attention_prompt_many_sequences(coral):
     rng = np.random.default_rng(8)
     n = rng.integers(0, 40, 300)
@@ -557,10 +568,11 @@ def test_attention_prompt_rows_of_no_sequence_and_offsets_outside(coral):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("heads", [4, 256])
 @pytest.mark.parametrize("D", [64, 128, 256])
-def test_attention_prompt_values_that_are_not_finite_reach_only_rows_that_see_them(coral, dtype, D):
+def test_attention_prompt_values_that_are_not_finite_reach_only_rows_that_see_them(coral, dtype, D, heads):
     lengths = [(150, 150), (70, 100), (40, 40)]
-    c = Prompt(coral, dtype, lengths, 4, 2, D)
+    c = Prompt(coral, dtype, lengths, heads, 2, D)
     want = c.run()
     spoiled = [(0, 64), (0, 100), (0, 149), (1, 99), (2, 0)]       # (sequence, key)
     clean = torch.ones(260, dtype=torch.bool)
@@ -571,16 +583,16 @@ def test_attention_prompt_values_that_are_not_finite_reach_only_rows_that_see_th
         clean[int(c.offsets[s]) + max(0, key - (m - n)):int(c.offsets[s + 1])] = False
     got = c.run()
     assert torch.equal(got[clean.cuda()], want[clean.cuda()])
-    assert torch.equal(got[:, 2:], want[:, 2:])                    # heads of the other keys
+    assert torch.equal(got[:, heads // 2:], want[:, heads // 2:])  # heads of the other keys
     c.q[5, 3, 0] = math.nan
     again = c.run()
     rest = clean.clone()
     rest[5] = False
     assert torch.equal(again[rest.cuda()], want[rest.cuda()])
-    v_only = Prompt(coral, dtype, lengths, 4, 2, D)                # a value alone makes its later rows not finite
+    v_only = Prompt(coral, dtype, lengths, heads, 2, D)            # a value alone makes its later rows not finite
     v_only.v[64, 1, 7] = math.inf
     got = v_only.run()
-    assert not bool(torch.isfinite(got[64:150, 2:, 7]).any()) and bool(torch.isfinite(got[:64]).all()) and bool(torch.isfinite(got[150:]).all())
+    assert not bool(torch.isfinite(got[64:150, heads // 2:, 7]).any()) and bool(torch.isfinite(got[:64]).all()) and bool(torch.isfinite(got[150:]).all())
 
 
 def test_attention_prompt_strides_stream_and_graph(coral):
