@@ -9,7 +9,9 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+from coral_inputs import CONFIGS, make_head  # noqa: E402
 from oracle import attention as plain  # noqa: E402
+from oracle import compare, operators  # noqa: E402
 
 TORCH = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 DTYPES = ["bf16", "f16", "f32"]
@@ -616,6 +618,225 @@ def test_attention_prompt_strides_stream_and_graph(coral):
         out.fill_(3)
         graph.replay()
         assert torch.equal(out, eager)
+
+
+# ---------------------------------------------------------------- far places, many rows, several streams, graphs
+def test_cache_past_32_bits(coral):
+    """A cache whose codes take more than 4 GiB on either side: its last pages answer as a small cache's do."""
+    page, kv_heads, D, pages = 256, 8, 256, 17000
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GiB of free memory")
+    big, small = coral.alloc_kv4_cache(pages, page, kv_heads, D), coral.alloc_kv4_cache(4, page, kv_heads, D)
+    assert big[0].numel() > 1 << 32
+    n = 700
+    k, v = (torch.randn((n, kv_heads, D), dtype=torch.bfloat16, device="cuda", generator=torch.Generator("cuda").manual_seed(s)) for s in (1, 2))
+    held = [pages - 1, 16400, pages - 2]                          # pages on both sides of the border and the last
+    place = np.arange(n)
+    slots = ints(np.asarray(held)[place // page] * page + place % page)
+    coral.coral_kv4_append(big, k, v, slots)
+    coral.coral_kv4_append(small, k, v, ints(place))
+    for a, b in zip(coral.coral_kv4_read(big, slots, torch.bfloat16), coral.coral_kv4_read(small, ints(place), torch.bfloat16)):
+        assert torch.equal(a, b)
+    q = torch.randn((5, 16, D), dtype=torch.bfloat16, device="cuda")
+    got, want = (coral.coral_attention_kv4(q, cache, ints([table]), ints([n]), ints([0, 5]), 5) for cache, table in ((big, held), (small, [0, 1, 2])))
+    assert torch.equal(got, want) and bool(got.any())
+    weight, at = torch.ones(D, dtype=torch.bfloat16, device="cuda"), ints(np.arange(n) + 10 ** 6)
+    kw = dict(positions=at, inv_freq=torch.full((64,), 0.01, device="cuda"), k_weight=weight, v=v)
+    assert torch.equal(coral.coral_qk_norm_rope(None, k, cache=big, slots=slots, **kw)[1], coral.coral_qk_norm_rope(None, k, cache=small, slots=ints(place), **kw)[1])
+    for a, b in zip(coral.coral_kv4_read(big, slots, torch.bfloat16), coral.coral_kv4_read(small, ints(place), torch.bfloat16)):
+        assert torch.equal(a, b)
+    assert int(big[1].sum(dtype=torch.int64)) == int(small[1].sum(dtype=torch.int64))        # and nothing elsewhere
+
+
+def test_rows_past_32_bits(coral):
+    """Rows of one wide matrix, the last of them more than 4 GiB behind the first."""
+    T, wide = 300, 1 << 23
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GiB of free memory")
+    rows = torch.zeros((T, wide), dtype=torch.bfloat16, device="cuda")
+    near = torch.randn((T, 8, 128), dtype=torch.bfloat16, device="cuda")
+    rows[:, -1024:] = near.view(T, 1024)
+    far = rows[:, -1024:].unflatten(1, (8, 128))
+    offsets = ints([0, 140, 300])
+    for a, b in zip(coral.coral_qk_norm_rope(far[:, :4], far[:, 4:6]), coral.coral_qk_norm_rope(near[:, :4], near[:, 4:6])):
+        assert torch.equal(a, b)
+    assert torch.equal(coral.coral_attention_prompt(far[:, :4], far[:, 4:6], far[:, 6:], offsets), coral.coral_attention_prompt(near[:, :4], near[:, 4:6], near[:, 6:], offsets))
+    one, two = (coral.alloc_kv4_cache(20, 16, 2, 128) for _ in range(2))
+    slots = ints(np.arange(T)[::-1].copy())
+    coral.coral_kv4_append(one, far[:, 4:6], far[:, 6:], slots)
+    coral.coral_kv4_append(two, near[:, 4:6], near[:, 6:], slots)
+    assert all(torch.equal(a, b) for a, b in zip(one, two))
+    table = ints([np.arange(20)] * 60)
+    args = (ints([300] * 60), ints(np.arange(61) * 5), 5)
+    assert torch.equal(coral.coral_attention_kv4(far[:, :4], one, table, *args), coral.coral_attention_kv4(near[:, :4], one, table, *args))
+
+
+def test_attention_kv4_more_rows_than_a_grid_has_in_its_second_part(coral):
+    c = Cached(coral, "bf16", [(150 + s % 7, 64) for s in range(1030)], 2, 1, 64, 32, tree=True)
+    out = c.run()
+    assert out.shape[0] > 65535
+    c.check(out, only=[0, 511, 1022, 1023, 1024, 1029])
+
+
+def test_two_calls_at_once_on_two_streams(coral):
+    cases = [Cached(coral, "bf16", [(4000, 3), (70, 1)], 8, 2, 128, 64, seed=s) for s in range(2)]
+    want = [c.run() for c in cases]
+    calls = [(c.args()[0], torch.zeros(coral.coral_attention_kv4_workspace_bytes(2, 3, 4032, 8, 2, 128, coral.CORAL_BF16), dtype=torch.uint8, device="cuda"),
+              torch.zeros_like(w), torch.cuda.Stream()) for c, w in zip(cases, want)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for args, ws, out, stream in calls:
+            coral.coral_attention_kv4(*args, max_length=4032, out=out, workspace=ws, stream=stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, w) for (_, _, out, _), w in zip(calls, want))
+
+
+def test_attention_kv4_workspace_made_ready_by_its_call(coral):
+    c = Cached(coral, "f16", [(3000, 2), (500, 7)], 8, 2, 64, 16)
+    want = c.run()
+    ws = torch.full((coral.coral_attention_kv4_workspace_bytes(2, 7, 4000, 8, 2, 64, coral.CORAL_F16),), 0xff, dtype=torch.uint8, device="cuda")
+    coral.coral_lmhead_workspace_init(ws)
+    args, _ = c.args()
+    for _ in range(3):
+        assert torch.equal(coral.coral_attention_kv4(*args, max_length=4000, workspace=ws), want)
+
+
+# ---------------------------------------------------------------- a drafter's layer
+class Layer:
+    """Projections of 4 bits, norms and rotation into the cache, attention, and the projection back onto the
+    residual; every step is checked against its definition, on the inputs that the device gave it."""
+
+    def __init__(self, coral, dtype, H, q_heads, kv_heads, D, pages, page):
+        self.coral, self.dtype, self.n, self.D, self.page = coral, dtype, (q_heads, kv_heads), D, page
+        rng = self.rng = np.random.default_rng([H, q_heads, kv_heads, D])
+        self.weights = [self.projection(H, (q_heads + 2 * kv_heads) * D), self.projection(q_heads * D, H)]
+        self.norms = [stored(1 + 0.2 * rng.standard_normal(D), dtype) for _ in range(2)]
+        self.freq = np.power(10000.0, -np.arange(D // 2) * 2 / D).astype(np.float32)
+        self.cache, self.sides = random_cache(coral, rng, pages, page, kv_heads, D, scales=(124, 128))
+
+    def projection(self, K, N):
+        codes = self.rng.integers(0, 256, (N, K // 2), dtype=np.uint8)
+        scales = stored(0.2 * (1 + self.rng.random((N, K // 64))) / math.sqrt(K), self.dtype)
+        return torch.from_numpy(codes).cuda(), scales[0], codes, scales[1]
+
+    def project(self, x, which, residual=None):
+        codes, scales, codes64, scales64 = self.weights[which]
+        out = self.coral.coral_matvec_w4(x, codes, scales, group=64, residual=residual, out_dtype=x.dtype)
+        args = (host(x), codes64, scales64, None, 64, "int", None, None if residual is None else host(residual))
+        assert (np.abs(host(out) - operators.matvec_w4(*args)) <= operators.matvec_w4_bound(*args, out=self.dtype)).all()
+        return out
+
+    def into_cache(self, x, at, slots):
+        """(q, k, v) of tokens x at positions `at`; k and v also in places `slots` of the cache."""
+        qh, kh = self.n
+        qkv = self.project(x, 0).unflatten(1, (qh + 2 * kh, self.D))
+        q, k, v = qkv[:, :qh], qkv[:, qh:qh + kh], qkv[:, qh + kh:]
+        out = self.coral.coral_qk_norm_rope(q, k, ints(at), torch.from_numpy(self.freq).cuda(), self.norms[0][0], self.norms[1][0],
+                                            cache=self.cache, v=v, slots=ints(slots))
+        for got, x64, (_, w) in zip(out, (host(q), host(k)), self.norms):
+            want, bound = (f(x64, np.asarray(at), self.freq, w, 1e-6, False, *more) for f, more in ((plain.norm_rope, ()), (plain.norm_rope_bound, (self.dtype,))))
+            assert (np.abs(host(got) - want) <= bound).all()
+        for (codes, scales), part in zip(self.sides, (host(out[1]), host(v))):
+            codes[slots // self.page, :, slots % self.page], scales[slots // self.page, :, slots % self.page] = plain.kv4_quantise(part, self.dtype)
+        for got, want in zip(self.cache, (*self.sides[0], *self.sides[1])):
+            assert np.array_equal(got.cpu().numpy(), want)
+        return out[0], out[1], v
+
+    def back(self, attended, x):
+        y = self.project(attended.flatten(1), 1, residual=x)
+        return y, (y.float() * torch.rsqrt(y.float().square().mean(1, keepdim=True))).to(y.dtype)
+
+
+@pytest.mark.parametrize("dtype,q_heads,kv_heads,D", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 7, 1, 64), ("bf16", 2, 1, 256)])
+def test_a_drafters_layer_from_prompt_to_tree(coral, dtype, q_heads, kv_heads, D):
+    cfg = CONFIGS["tiny_f32"].scaled(dtype=dtype, H=256, V=4096)
+    head = make_head(cfg)
+    gate, lm = (coral.device_tensor(w, dtype) for w in (head.gate_W, head.lm_W))
+    gi = coral.GroupIndex(head.group_offsets, head.group_rows)
+    layer = Layer(coral, dtype, 256, q_heads, kv_heads, D, pages=12, page=16)
+    embed = lambda ids: (lm[ids.long()].float() * 50).to(lm.dtype)        # noqa: E731  (the rows' 0.02 to about one)
+    prompts, width, k = [40, 23], 6, 5
+    table = layer.rng.permutation(12)[:8].reshape(2, 4)
+    place = lambda s, at: table[s][at // 16] * 16 + at % 16       # noqa: E731
+    # the prompts, one behind the other
+    x = embed(torch.from_numpy(layer.rng.integers(0, cfg.V, sum(prompts))).cuda())
+    at = np.concatenate([np.arange(n) for n in prompts])
+    slots = np.concatenate([place(s, np.arange(n)) for s, n in enumerate(prompts)])
+    q, keys, values = layer.into_cache(x, at, slots)
+    offsets = np.array([0, 40, 63])
+    out = coral.coral_attention_prompt(q, keys, values, ints(offsets))
+    for s, n in enumerate(prompts):
+        r = slice(offsets[s], offsets[s + 1])
+        want = plain.attention(host(q)[r], host(keys)[r], host(values)[r], np.tri(n, dtype=bool), D ** -0.5)
+        check_attention(host(out)[r], want, dtype, n)
+    _, hidden = layer.back(out, x)
+    hidden = hidden[[39, 62]]
+    # three levels of a tree behind each prompt
+    score, paths, held = [None, None], [[], []], [0, 0]           # paths: a node's ancestors and itself, as bits from the prompt's end
+    nodes = [hidden[:1], hidden[1:]]
+    for depth in range(3):
+        tokens, words = [], []
+        for s in range(2):
+            ids, logp, sel, parent, token, total = coral.coral_lmhead_draft_level(nodes[s].contiguous(), gate, None, lm, gi, cfg.g, k, width if depth else k, parent_score=score[s])
+            as_host = nodes[s].contiguous()
+            as_host = host(as_host).astype(np.float32) if dtype == "f32" else as_host.view(torch.int16).cpu().numpy().view(np.uint16)
+            compare.check_grouped_logprob(as_host, head.gate_W, None, head.lm_W, head.group_offsets, head.group_rows, cfg.g, k, dtype, *(t.cpu().numpy() for t in (ids, logp, sel)))
+            first = held[s]
+            old = paths[s][-1] if depth else [0]
+            paths[s].append([old[p] | 1 << (first + i) for i, p in enumerate(parent.cpu().tolist())])
+            held[s] += len(paths[s][-1])
+            score[s] = total
+            tokens.append(token)
+            words.append(paths[s][-1])
+        rows = [len(w) for w in words]
+        x = embed(torch.cat(tokens))
+        at = np.concatenate([np.full(r, prompts[s] + depth) for s, r in enumerate(rows)])
+        slots = np.concatenate([place(s, prompts[s] + np.arange(held[s] - rows[s], held[s])) for s in range(2)])
+        q = layer.into_cache(x, at, slots)[0]
+        tree = np.array(words[0] + words[1], dtype=np.int64)
+        offsets, lengths = np.concatenate([[0], np.cumsum(rows)]), [n + h for n, h in zip(prompts, held)]
+        out = coral.coral_attention_kv4(q, layer.cache, ints(table), ints(lengths), ints(offsets), max(rows), history=ints(prompts), tree=torch.from_numpy(tree).cuda())
+        for s, n in enumerate(lengths):
+            r = slice(offsets[s], offsets[s + 1])
+            (kk, _), (vv, _) = (plain.kv4_tokens(*side, table[s], n, dtype) for side in layer.sides)
+            seen = np.ones((rows[s], n), bool)
+            seen[:, prompts[s]:] = (tree[r, None] >> np.arange(held[s])) & 1 == 1
+            assert (seen[:, prompts[s]:].sum(axis=1) == depth + 1).all()
+            check_attention(host(out)[r], plain.attention(host(q)[r], kk, vv, seen, D ** -0.5), dtype, n)
+        _, hidden = layer.back(out, x)
+        nodes = [hidden[:rows[0]], hidden[rows[0]:]]
+
+
+def test_a_layer_in_one_graph_as_eagerly(coral):
+    """Projection, norms and rotation into the cache, attention and the projection back as one graph: replays
+    with tokens, places and lengths that change between them give what eager calls give."""
+    graph_side, eager_side = (Layer(coral, "bf16", 256, 8, 2, 64, pages=12, page=16) for _ in range(2))
+    x, at, slots = torch.zeros((3, 256), dtype=torch.bfloat16, device="cuda"), ints([0] * 3), ints([-1] * 3)
+    table, offsets, lengths = ints(np.arange(12).reshape(1, 12)), ints([0, 3]), ints([0])
+    freq = torch.from_numpy(graph_side.freq).cuda()
+    ws = torch.zeros(coral.coral_attention_kv4_workspace_bytes(1, 3, 192, 8, 2, 64, coral.CORAL_BF16), dtype=torch.uint8, device="cuda")
+
+    def step(layer, workspace=None):
+        (codes, scales, _, _), (codes2, scales2, _, _) = layer.weights
+        qkv = coral.coral_matvec_w4(x, codes, scales, group=64, out_dtype=x.dtype).unflatten(1, (12, 64))
+        q, _ = coral.coral_qk_norm_rope(qkv[:, :8], qkv[:, 8:10], at, freq, layer.norms[0][0], layer.norms[1][0], k_out=False, cache=layer.cache, v=qkv[:, 10:], slots=slots)
+        out = coral.coral_attention_kv4(q, layer.cache, table, lengths, offsets, 3, workspace=workspace)
+        return coral.coral_matvec_w4(out.flatten(1), codes2, scales2, group=64, residual=x, out_dtype=x.dtype)
+
+    step(graph_side, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(graph_side, ws)
+    for first in (0, 3, 90, 15, 189):
+        x.copy_(torch.from_numpy(graph_side.rng.standard_normal((3, 256))))
+        at.copy_(ints(first + np.arange(3)))
+        slots.copy_(at)
+        lengths.copy_(ints([first + 3]))
+        want = step(eager_side)
+        torch.cuda.synchronize()
+        graph.replay()
+        assert torch.equal(got, want) and all(torch.equal(a, b) for a, b in zip(graph_side.cache, eager_side.cache))
 
 
 # ---------------------------------------------------------------- binding
