@@ -17,8 +17,6 @@
 
 namespace {
 
-constexpr int kPromptThreads = 256;
-constexpr int kPromptWaves = kPromptThreads / kWave;
 constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
 constexpr int kXcds = 8;
 
@@ -159,9 +157,10 @@ __device__ __forceinline__ unsigned only_finite(unsigned w, bool& odd) {
 __device__ __forceinline__ unsigned long long keys_to(int most) { return most < 0 ? 0ull : most > 62 ? ~0ull : (2ull << most) - 1ull; }
 
 // A wave's 64 pieces of 16 bytes from memory into 1 KB of LDS, past the registers; what lies behind the view's end comes as
-// zero.  Nothing waits for it but dma_arrived.
+// zero.  Nothing waits for it but dma_arrived.  (m0 is the compiler's own to write, and these kernels give it no other use:
+// neither dynamic register indexes nor messages.)
 __device__ __forceinline__ void dma_piece(Buffer from, unsigned at, unsigned lds_place) {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from), "s"(lds_place) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(at), "s"(from), "s"(lds_place) : "memory");
 }
 __device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -397,13 +396,22 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
 }
 
 // fp32 on the matrix cores' fp32 products (a sixteenth of the 16-bit rate): 16 rows a wave, 32 keys at a time, no
-// rounding of the weights.  One value a lane and product: lane (key or column, g) has the g-th of four.
-template <int D>
-__global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
-    constexpr int BN = 32, ROWS = 64, PIECES = D / 4, LOADS = BN * PIECES / kPromptThreads, QC = D / 16, DTILES = D / 16, kRow = D + 4;
-    __shared__ __align__(16) float k_lds[BN][kRow], v_lds[BN][kRow];
-    __shared__ unsigned long long odd[2];
-    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+// rounding of the weights.  One value a lane and product: lane (key or column, g) has the g-th of four.  KS groups of RW waves
+// take every KS-th tile of keys, as in k_prompt.
+template <int D, int RW, int KS>
+__global__ __launch_bounds__(RW * KS * kWave) void k_prompt_f32(PromptParams p) {
+    constexpr int kGroup = RW * kWave;
+    constexpr int BN = 32, ROWS = RW * 16, PIECES = D / 4, LOADS = BN * PIECES / kGroup, QC = D / 16, DTILES = D / 16, kRow = D + 4;
+    static_assert(BN * kRow >= ROWS * D || KS == 1, "a group's sums fit where the keys were");
+    __shared__ struct {
+        __align__(16) float k[KS][BN][kRow], v[KS][BN][kRow];
+        unsigned long long odd[KS][2];
+        float2 stats[KS][ROWS];
+    } lds;
+    const int lane = threadIdx.x & (kWave - 1), all_wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int group = KS == 1 ? 0 : all_wave / RW, wave = KS == 1 ? all_wave : all_wave % RW, thread = wave * kWave + lane;
+    float (*const k_lds)[kRow] = lds.k[group], (*const v_lds)[kRow] = lds.v[group];
+    unsigned long long* const odd = lds.odd[group];
     const int col = lane & 15, g = lane >> 4;
     const PromptTile t = prompt_tile<ROWS>(p, blockIdx.x, lane);
     if (!t.any) return;
@@ -430,22 +438,23 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
     for (int d = 0; d < DTILES; ++d) sum[d] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     float ref = -INFINITY, total = 0.f;
     const int first_cut = (reach + t.first + 1 < 0 ? 0 : reach + t.first + 1) / BN;       // as in k_prompt
-    if (threadIdx.x < 2) odd[threadIdx.x] = 0;
-    for (int j = 0; j < n_tiles; ++j) {
-        const int k0 = j * BN;
+    if (thread < 2) odd[thread] = 0;
+    const int rounds = (n_tiles + KS - 1) / KS;
+    for (int j = 0; j < rounds; ++j) {
+        const int k0 = (j * KS + group) * BN;                    // (no row sees a tile behind the last)
         const Buffer kb = buffer_view(k_base, (size_t)k0 * p.k_stride, k_bytes), vb = buffer_view(v_base, (size_t)k0 * p.v_stride, v_bytes);
         uint4 nk[LOADS], nv[LOADS];
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
+            const int at = i * kGroup + thread, r = at / PIECES, c = at % PIECES;
             nk[i] = buffer_read16(kb, (unsigned)(r * (int)p.k_stride + c * 16));
             nv[i] = buffer_read16(vb, (unsigned)(r * (int)p.v_stride + c * 16));
         }
         __syncthreads();                                         // the tile before has been read
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int at = i * kPromptThreads + threadIdx.x, r = at / PIECES, c = at % PIECES;
-            if (j >= first_cut) {
+            const int at = i * kGroup + thread, r = at / PIECES, c = at % PIECES;
+            if (j * KS + group >= first_cut) {
                 bool bad = false;
                 nv[i].x = only_finite(nv[i].x, bad);
                 nv[i].y = only_finite(nv[i].y, bad);
@@ -457,7 +466,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
             store_vec(reinterpret_cast<uint4*>(&v_lds[r][c * 4]), nv[i]);
         }
         __syncthreads();
-        if (threadIdx.x == 0) odd[(j + 1) & 1] = 0;              // read before the barrier above, written behind the next one
+        if (thread == 0) odd[(j + 1) & 1] = 0;              // read before the barrier above, written behind the next one
         if (k0 > reach + my_first + 15 || my_first >= t.rows) continue;      // uniform over the wave
         f32x4_t s[2];
 #pragma unroll
@@ -492,7 +501,7 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
             w[i] = __builtin_amdgcn_exp2f(x[i] - base);
             total += w[i];
         }
-        if (j >= first_cut && (odd[j & 1] & keys_to(most))) total = NAN;
+        if (j * KS + group >= first_cut && (odd[j & 1] & keys_to(most))) total = NAN;
 #pragma unroll
         for (int d = 0; d < DTILES; ++d)
 #pragma unroll
@@ -500,6 +509,32 @@ __global__ __launch_bounds__(kPromptThreads) void k_prompt_f32(PromptParams p) {
                 sum[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(v_lds[(i / 4) * 16 + 4 * g + i % 4][d * 16 + col], w[i], sum[d], 0, 0, 0);
     }
     total = lane_xor_sum<16>(lane_xor_sum<32>(total));
+    if (KS > 1) {                                                // the other groups hand their sums over, lane to lane
+        __syncthreads();
+        f32x4_t* to = reinterpret_cast<f32x4_t*>(&k_lds[0][0]) + wave * (DTILES * kWave) + lane;
+        if (group) {
+#pragma unroll
+            for (int d = 0; d < DTILES; ++d) to[d * kWave] = sum[d];
+            if (g == 0) lds.stats[group][wave * 16 + col] = make_float2(ref, total);
+        }
+        __syncthreads();
+        if (group) return;
+#pragma unroll
+        for (int o = 1; o < KS; ++o) {
+            const f32x4_t* from = reinterpret_cast<const f32x4_t*>(&lds.k[o][0][0]) + wave * (DTILES * kWave) + lane;
+            const float2 other = lds.stats[o][wave * 16 + col];
+            const float top = fmaxf(ref, other.x), mine = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
+            const float its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - top);
+            ref = top;
+            total = total * mine + other.y * its;
+#pragma unroll
+            for (int d = 0; d < DTILES; ++d) {
+                const f32x4_t x = from[d * kWave];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[d][e] = fmaf(x[e], its, sum[d][e] * mine);
+            }
+        }
+    }
     if (row >= t.rows) return;
     const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;
     char* to = p.out + (int64_t)(t.row0 + row) * p.out_stride + (int64_t)head * (D * 4) + g * 16;

@@ -5,10 +5,16 @@
 
 namespace {
 
-// Tiles of 128 rows, over all heads, up to which two groups of waves share a workgroup's keys.  One prompt, us with one group and with
-// two: 100 tiles of D = 128 12.8 and 12.6, 256 27.3 and 23.9, 384 39.8 and 34.5, 544 54.6 and 59.3, 1056 148 and 154;  D = 64: 192 30.9
-// and 24.7, 384 57.4 and 42.7, 756 131 and 135;  D = 256 (64 rows by two groups): 136 88 and 57, 256 156 and 112, 504 329 and 385.
-constexpr int64_t kFewUnits = 400;
+// Groups of waves share a workgroup's keys where the card has few rows, which do not see very few keys.  Measured for one prompt, by tiles
+// of 128 (fp32: 64) rows over all heads, us with one group and with several:
+//   16 bits, D = 64    192 30.9 24.7   384 57.4 42.7   756 131 135        fp32, D = 64    182 45.6 28.7   288 89 53   756 315 242   1512 933 887
+//            D = 128   96 12.8 12.6   256 27.3 23.9   384 39.8 34.5               D = 128   160 33.5 22.2   352 79 66   520 479 369   768 196 225
+//                      544 54.6 59.3   1056 148 154                               D = 256   32 39.8 31.5   128 167 105   272 345 264   504 694 809
+//            D = 256   136 88 57   256 156 112   504 329 385
+// (two groups of as many rows for 16 bits, of 64 for D = 256; for fp32 four of 32, two for D = 256).  A prompt of 100 tokens took 10.2
+// for 9.8 us in two groups, twenty of 200 in fp32 42 for 29, where a group of most has no keys.
+constexpr int64_t kFewUnits = 400, kFewUnitsF32 = 600;
+constexpr int kFewKeys = 128;
 constexpr int64_t kMostStride = 1 << 24;         // bytes: a tile's rows are addressed by 32-bit offsets
 
 using prompt_fn = void (*)(PromptParams);
@@ -23,7 +29,10 @@ PromptForm prompt_form(int d, bool few) {
     return few ? PromptForm{k_prompt<DT, 256, 2, 2>, 64, 256} : PromptForm{k_prompt<DT, 256, 4, 1>, 128, 256};
 }
 PromptForm prompt_form(coral_dtype dt, int d, bool few) {
-    if (dt == CORAL_F32) return {d == 64 ? k_prompt_f32<64> : d == 128 ? k_prompt_f32<128> : k_prompt_f32<256>, 64, 256};
+    if (dt == CORAL_F32) {
+        if (few) return d == 64 ? PromptForm{k_prompt_f32<64, 2, 4>, 32, 512} : d == 128 ? PromptForm{k_prompt_f32<128, 2, 4>, 32, 512} : PromptForm{k_prompt_f32<256, 2, 2>, 32, 256};
+        return {d == 64 ? k_prompt_f32<64, 4, 1> : d == 128 ? k_prompt_f32<128, 4, 1> : k_prompt_f32<256, 4, 1>, 64, 256};
+    }
     return dt == CORAL_BF16 ? prompt_form<kBF16>(d, few) : prompt_form<kF16>(d, few);
 }
 
@@ -52,9 +61,12 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     if (rows_overlap(out_rows, in_q) || rows_overlap(out_rows, in_k) || rows_overlap(out_rows, in_v) ||
         rows_overlap(out_rows, {q_offsets, offsets, offsets, 1}) || rows_overlap(out_rows, {k_offsets, offsets, offsets, 1}))
         return CORAL_ERR_UNSUPPORTED;
-    const PromptForm form = prompt_form(dt, head_dim, (int64_t)(T / 128 + 1) * q_heads <= kFewUnits);
+    const int not_full = S < T ? S : T;                    // each sequence has at most one tile that is not full
+    const bool f32 = dt == CORAL_F32;
+    const bool few = (T / (f32 ? 64ll : 128ll) + not_full) * q_heads <= (f32 && head_dim != 256 ? kFewUnitsF32 : kFewUnits) && keys / S >= kFewKeys;
+    const PromptForm form = prompt_form(dt, head_dim, few);
     const int rows = form.rows;
-    const int64_t tiles = T / rows + (S < T ? S : T);        // each sequence has at most one tile that is not full
+    const int64_t tiles = T / rows + not_full;
     int parts = 1;
     while (q_heads * parts % kXcds) parts *= 2;
     const int64_t units = (tiles + parts - 1) / parts * q_heads * parts;

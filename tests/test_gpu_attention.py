@@ -499,12 +499,13 @@ def rng_rows(n, count):
 
 SHORT = [(1, 1), (2, 2), (31, 31), (32, 32), (33, 33), (63, 63), (64, 64), (65, 65), (127, 127), (128, 128), (129, 129), (200, 200)]
 BEHIND = [(1, 1), (1, 500), (3, 2), (70, 0), (0, 40), (129, 200), (64, 65), (130, 31), (5, 64), (257, 321)]
+SHARED = [(1, 700), (2, 130), (33, 33), (63, 600), (70, 0), (0, 40), (64, 65), (1, 1), (129, 257), (31, 95), (200, 161), (5, 1000)]      # keys shared by groups
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("q_heads,kv_heads", [(1, 1), (8, 2), (7, 1), (12, 12)])
-@pytest.mark.parametrize("lengths", [SHORT, BEHIND])
+@pytest.mark.parametrize("lengths", [SHORT, BEHIND, SHARED])
 def test_attention_prompt(coral, dtype, D, q_heads, kv_heads, lengths):
     c = Prompt(coral, dtype, lengths, q_heads, kv_heads, D)
     out, kept = guarded(c.q.shape, TORCH[dtype])
@@ -573,11 +574,11 @@ def test_attention_prompt_rows_of_no_sequence_and_offsets_outside(coral):
 @pytest.mark.parametrize("heads", [4, 256])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_attention_prompt_values_that_are_not_finite_reach_only_rows_that_see_them(coral, dtype, D, heads):
-    lengths = [(150, 150), (70, 100), (40, 40)]
+    lengths = [(150, 150), (70, 100), (40, 40)] + [(1, 300)] * (heads == 4)        # (long enough for groups of waves to share the keys)
     c = Prompt(coral, dtype, lengths, heads, 2, D)
     want = c.run()
     spoiled = [(0, 64), (0, 100), (0, 149), (1, 99), (2, 0)]       # (sequence, key)
-    clean = torch.ones(260, dtype=torch.bool)
+    clean = torch.ones(len(c.q), dtype=torch.bool)
     for i, (s, key) in enumerate(spoiled):
         c.v[int(c.k_offsets[s]) + key, 0, 3 + i] = (math.nan, math.inf, -math.inf, math.inf, math.nan)[i]
         c.k[int(c.k_offsets[s]) + key, 0, 2] = (math.inf, math.nan, math.nan, -math.inf, math.inf)[i]
