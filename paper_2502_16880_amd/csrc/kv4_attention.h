@@ -666,13 +666,15 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
     }
 }
 
-// Joins the parts of an item that several workgroups have taken: one workgroup a row, its waves take parts in turn.
-template <int DT, int D, int NT>
+// Joins the parts of an item that several workgroups have taken: WAVES waves a row, which take parts in turn.
+template <int DT, int D, int NT, int WAVES>
 __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
     constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2, kRows = NT * 16;
+    static_assert(WAVES == 1 || WAVES == kKv4Waves, "");
     __shared__ float sums[kKv4Waves][D];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int t = blockIdx.x, q_head = blockIdx.y;
+    const int t = blockIdx.x, q_head = blockIdx.y * (kKv4Waves / WAVES) + wave / WAVES, of_row = wave % WAVES;
+    if (WAVES == 1 && q_head >= p.group * p.kv_heads) return;
     Kv4Line<kRows> line;
     unsigned long long total = 0, start = 0;
     unsigned steps = 0;
@@ -710,7 +712,7 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
         auto load = [&](int i) CORAL_INLINE {                    // eight parts of the wave's
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int j = i + u * kKv4Waves + wave;
+                const int j = i + u * WAVES + of_row;
                 const float* from = p.part + row_of(j0 + (j < left ? j : left - 1)) * D + lane * N;
 #pragma unroll
                 for (int n = 0; n < N; ++n) x[u][n] = from[n];
@@ -727,27 +729,34 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
         for (int i = 0;;) {
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
-                const int j = i + u * kKv4Waves + wave;
+                const int j = i + u * WAVES + of_row;
                 const float f = j < left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j & (kWave - 1))) : 0.f;
 #pragma unroll
                 for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, x[u][n], o[n]);
             }
-            i += 8 * kKv4Waves;
+            i += 8 * WAVES;
             if (i >= left) break;
             load(i);
         }
     }
     all = wave_sum(all);
+    char* to = p.out + (int64_t)t * p.out_stride + (int64_t)q_head * (D * kBytes);
+    auto put = [&](int d, float v) CORAL_INLINE {
+        const float y = all > 0.f ? v / all : all == 0.f ? 0.f : all;
+        if (DT == kF32) reinterpret_cast<float*>(to)[d] = y;
+        else reinterpret_cast<unsigned short*>(to)[d] = narrow16<DT>(y);
+    };
+    if (WAVES == 1) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) put(lane * N + n, o[n]);
+        return;
+    }
 #pragma unroll
     for (int n = 0; n < N; ++n) sums[wave][lane * N + n] = o[n];
     __syncthreads();
     if (threadIdx.x >= D) return;
     const int d = threadIdx.x;
-    const float v = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
-    const float y = all > 0.f ? v / all : all == 0.f ? 0.f : all;
-    char* to = p.out + (int64_t)t * p.out_stride + ((int64_t)q_head * D + d) * kBytes;
-    if (DT == kF32) *reinterpret_cast<float*>(to) = y;
-    else *reinterpret_cast<unsigned short*>(to) = narrow16<DT>(y);
+    put(d, (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]));
 }
 
 using kv4_attn_fn = void (*)(Kv4AttnParams);
@@ -762,9 +771,10 @@ kv4_attn_fn kv4_kernel(int tiles) {
     return k_kv4_attention<DT, D, 1, DT == kF32 ? 3 : 2>;
 }
 template <int DT, int D>
-kv4_join_fn kv4_join(int tiles) {
-    constexpr int most = kv4_most_tiles(D, kv4_terms(DT));
-    return tiles == 2 ? k_kv4_join<DT, D, most >= 2 ? 2 : 1> : k_kv4_join<DT, D, 1>;
+kv4_join_fn kv4_join(int tiles, bool wave_a_row) {
+    constexpr int many = kv4_most_tiles(D, kv4_terms(DT)) >= 2 ? 2 : 1;
+    if (tiles == 2) return wave_a_row ? k_kv4_join<DT, D, many, 1> : k_kv4_join<DT, D, many, kKv4Waves>;
+    return wave_a_row ? k_kv4_join<DT, D, 1, 1> : k_kv4_join<DT, D, 1, kKv4Waves>;
 }
 
 }  // namespace

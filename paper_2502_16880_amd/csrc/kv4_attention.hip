@@ -83,9 +83,11 @@ extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, con
     hipLaunchKernelGGL(reinterpret_cast<kv4_attn_fn>(const_cast<void*>(fn)), grid, dim3(kKv4Threads), 0, stream, p);
     if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
     if (need && !plan.join_inside) {
-        const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim, plan.tiles) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim, plan.tiles)
-                                                                                                        : coral_kv4_join_f16(head_dim, plan.tiles);
-        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(T, q_heads), dim3(kKv4Threads), 0, stream, p);
+        const bool one = plan.wave_a_row;
+        const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim, plan.tiles, one) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim, plan.tiles, one)
+                                                                                                             : coral_kv4_join_f16(head_dim, plan.tiles, one);
+        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(T, one ? (q_heads + kKv4Waves - 1) / kKv4Waves : q_heads), dim3(kKv4Threads), 0,
+                           stream, p);
         if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
     }
     return CORAL_OK;

@@ -5,6 +5,6 @@
 __attribute__((visibility("hidden"))) const void* coral_kv4_kernel_bf16(int head_dim, int tiles);
 __attribute__((visibility("hidden"))) const void* coral_kv4_kernel_f16(int head_dim, int tiles);
 __attribute__((visibility("hidden"))) const void* coral_kv4_kernel_f32(int head_dim, int tiles);
-__attribute__((visibility("hidden"))) const void* coral_kv4_join_bf16(int head_dim, int tiles);
-__attribute__((visibility("hidden"))) const void* coral_kv4_join_f16(int head_dim, int tiles);
-__attribute__((visibility("hidden"))) const void* coral_kv4_join_f32(int head_dim, int tiles);
+__attribute__((visibility("hidden"))) const void* coral_kv4_join_bf16(int head_dim, int tiles, bool wave_a_row);
+__attribute__((visibility("hidden"))) const void* coral_kv4_join_f16(int head_dim, int tiles, bool wave_a_row);
+__attribute__((visibility("hidden"))) const void* coral_kv4_join_f32(int head_dim, int tiles, bool wave_a_row);

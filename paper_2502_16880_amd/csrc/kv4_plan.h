@@ -8,7 +8,8 @@ struct Kv4Plan {
     int row_blocks;    // so many times that, at most, for one sequence's rows of one head of keys
     int workgroups;    // among which all sequences' steps are shared equally, or
     bool apart;        // one workgroup for each sequence, head of keys and block of rows
-    bool join_inside;  // an item's last workgroup joins its parts; or a kernel of its own does, many workgroups at once
+    bool join_inside;  // an item's last workgroup joins its parts; or a kernel of its own does, many workgroups at once,
+    bool wave_a_row;   // with a wave a row, or four
 };
 
 constexpr size_t kKv4Control = 16896;   // bytes of the workspace's control words and the words behind them
@@ -17,7 +18,10 @@ constexpr int kKv4MostRows = 64;        // rows (tokens) of a sequence in one ca
 constexpr int kKv4Units = 256;          // compute units of the card
 constexpr int kKv4Apart = 256;          // sequences beyond which they are not shared out (each workgroup sums them all up)
 constexpr int kKv4JoinRows = 8;         // rows and parts of an item, at most, that one workgroup joins as fast as another
-constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave
+constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave (D = 256: half as many; eight tokens' 34 parts 34 us, apart 22)
+// Parts of an item, at most, that a wave joins by itself: 60 nodes over 4111 tokens (11 parts) 27.8 us with four waves a row, 25.9 with
+// one; 32 sequences' 16 rows (2 parts) 58.6 and 45.2; one token of 32768 (98 parts) 20.5 and 24.6, eight of 131072 (66) 48.8 and 51.2.
+constexpr int kKv4JoinWave = 16;
 
 // Query operands and sums of a wave's tiles stay in registers: with `terms` 16-bit values for a query value
 // (3 for fp32, else 1) this many tiles fit.
@@ -38,7 +42,8 @@ inline Kv4Plan kv4_plan(int S, int max_rows, int max_length, int q_heads, int kv
     p.workgroups = (int)(all < places ? all : places);
     p.apart = S > kKv4Apart;
     const int64_t parts = p.workgroups / ((int64_t)S * kv_heads * p.row_blocks) + 2, rows = max_rows * (q_heads / kv_heads);
-    p.join_inside = rows <= kKv4JoinRows && parts <= kKv4JoinParts;
+    p.join_inside = rows <= kKv4JoinRows && parts <= kKv4JoinParts && parts * head_dim <= kKv4JoinParts * 128;
+    p.wave_a_row = parts <= kKv4JoinWave;
     return p;
 }
 
