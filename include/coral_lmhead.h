@@ -439,7 +439,7 @@ coral_status coral_logits_topk(const void *logits, const coral_logit_rules *rule
  *   - Rows of heads [T, heads, head_dim] may be columns of a wider matrix (a projection's output that
  *     holds queries, keys and values): a stride is the distance of two tokens in elements, at least
  *     heads * head_dim, and a multiple of 16 bytes, as the base is.
- *   - T may be 0: such a call checks its other sizes, and does nothing.
+ *   - T may be 0: such a call checks its other sizes, and does nothing.  T is below 2^24, as keys are.
  *   - An output shares memory with no input, but where it says so.
  */
 
@@ -569,7 +569,7 @@ coral_status coral_attention_kv4(const void *q, int64_t q_stride, const coral_kv
  *   q_offsets, k_offsets [device] [S+1] int32, ascending, cut to 0 .. T and 0 .. keys; k_offsets NULL: the
  *        same as q_offsets (keys = T).  Rows of no sequence are left as they were
  *   out  [device] out [T,q_heads,head_dim] of dt, dense, 16-byte aligned
- * Limits: S >= 1.  A key, a value or a query that is not finite makes the results of the rows that see it
+ * Limits: 1 <= S <= 65535.  A key, a value or a query that is not finite makes the results of the rows that see it
  * unspecified, of no other row.  Needs no workspace.
  */
 coral_status coral_attention_prompt(const void *q, int64_t q_stride, const void *k,

@@ -111,6 +111,8 @@ inline size_t storage_bytes(coral_dtype dt) { return dt == CORAL_F32 ? 4 : 2; }
 inline bool storage_known(coral_dtype dt) { return dt == CORAL_F32 || dt == CORAL_BF16 || dt == CORAL_F16; }
 inline bool head_dim_known(int d) { return d == 64 || d == 128 || d == 256; }
 constexpr int kMostHeads = 1024;
+constexpr int kMostSequences = 65535;
+constexpr int kMostTokens = (1 << 24) - 1;                   // a grid's threads are counted in 32 bits
 
 // Scores are multiplied by a number above zero, to powers of two: the sign goes to q (exactly), and a scale of nothing (all
 // weights equal) is little enough.
@@ -142,7 +144,7 @@ inline coral_status check_rows(const void* base, int64_t stride, int heads, int 
     const int64_t w = (int64_t)storage_bytes(dt), width = (int64_t)heads * head_dim;
     if (!base) return CORAL_ERR_NULL;
     if (stride < width) return CORAL_ERR_SHAPE;
-    if (((uintptr_t)base & 15u) || (stride * w) % 16 != 0 || stride > ((int64_t)1 << 40)) return CORAL_ERR_UNSUPPORTED;
+    if (((uintptr_t)base & 15u) || (stride * w) % 16 != 0 || stride > ((int64_t)1 << 40) || n > kMostTokens) return CORAL_ERR_UNSUPPORTED;
     *out = {base, stride * w, width * w, n};
     return CORAL_OK;
 }

@@ -171,7 +171,7 @@ struct Kv4Params {
 template <int DT, int D, bool READ>
 __global__ __launch_bounds__(kHeadThreads) void k_kv4_move(Kv4Params p) {
     constexpr int kRaw = DT == kF32 ? 2 : 1, kLanes = D / 8, kBytes = DT == kF32 ? 4 : 2;
-    const int64_t item = (int64_t)blockIdx.x * kHeadThreads + threadIdx.x;
+    const int64_t item = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kHeadThreads + threadIdx.x;
     if (item >= p.items) return;                                 // whole heads: groups of lanes leave together
     const int l = (int)(item % kLanes);
     const int64_t head = item / kLanes;
@@ -234,8 +234,8 @@ kv4_fn move_kernel(int head_dim, coral_dtype dt) {
 coral_status move_launch(kv4_fn fn, Kv4Params& p, int T, int head_dim, void* hip_stream) {
     p.items = (int64_t)T * 2 * p.cache.kv_heads * (head_dim / 8);
     const int64_t blocks = (p.items + kHeadThreads - 1) / kHeadThreads;
-    if (blocks > INT32_MAX) return CORAL_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL(fn, dim3((unsigned)blocks), dim3(kHeadThreads), 0, static_cast<hipStream_t>(hip_stream), p);
+    const int64_t down = (blocks + kMostTokens - 1) / kMostTokens;
+    hipLaunchKernelGGL(fn, dim3((unsigned)((blocks + down - 1) / down), (unsigned)down), dim3(kHeadThreads), 0, static_cast<hipStream_t>(hip_stream), p);
     return hipGetLastError() == hipSuccess ? CORAL_OK : CORAL_ERR_HIP;
 }
 

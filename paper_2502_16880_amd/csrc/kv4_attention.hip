@@ -9,8 +9,6 @@
 
 namespace {
 
-constexpr int kMostSequences = 65535;
-
 // Sizes that the plan is made of; false where one is out of range.
 coral_status check_kv4_sizes(int T, int S, int max_rows, int max_length, int q_heads, int kv_heads, int head_dim, coral_dtype dt) {
     if (!storage_known(dt) || T < 0 || S < 1 || max_rows < 1 || max_length < 0 || q_heads < 1 || kv_heads < 1 || head_dim < 1) return CORAL_ERR_SHAPE;

@@ -19,6 +19,7 @@ namespace {
 
 constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
 constexpr int kXcds = 8;
+constexpr int kPromptLevelled = 256;                        // sequences beyond which tiles come in the sequences' order
 
 struct PromptParams {
     const char *q, *k, *v;
@@ -76,6 +77,25 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, 
     if (p.S == 1) {
         r.first = (__builtin_amdgcn_readfirstlane(q.tiles) - 1 - rank) * ROWS;
         r.any = r.first >= 0;
+    } else if (p.S > kPromptLevelled) {
+        // sequence s has the places from before(s) on: at least as many as it has tiles
+        auto before = [&](int s) CORAL_INLINE {
+            const int a = p.q_offsets[s];
+            return (a < 0 ? 0 : a > p.T ? p.T : a) / ROWS + s;
+        };
+        for (int n = p.S; n > 1;) {                          // among the n from seq on, 64 at once
+            const int step = (n + kWave - 1) / kWave;
+            const bool reached = lane * step < n && before(seq + (lane * step < n ? lane * step : 0)) <= rank;
+            const uint64_t behind = ~__builtin_amdgcn_ballot_w64(reached);
+            const int last = behind ? __builtin_ctzll(behind) - 1 : kWave - 1;
+            if (last < 0) return r;
+            seq += last * step;
+            n = n - last * step < step ? n - last * step : step;
+        }
+        q = prompt_sequence<ROWS>(p, seq);
+        const int i = rank - __builtin_amdgcn_readfirstlane(before(seq)), tiles = __builtin_amdgcn_readfirstlane(q.tiles);
+        r.first = (tiles - 1 - i) * ROWS;
+        r.any = i >= 0 && i < tiles;
     } else {
         // the largest level l that, with all above it, has more than `rank` tiles
         auto chunk = [&](int s0) CORAL_INLINE {

@@ -43,7 +43,7 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
                                                int kv_heads, int head_dim, float scale, coral_dtype dt, void* out, void* hip_stream) {
     if (!storage_known(dt) || T < 0 || keys < 0 || S < 1 || q_heads < 1 || kv_heads < 1 || head_dim < 1 || !isfinite(scale)) return CORAL_ERR_SHAPE;
     if (q_heads % kv_heads || (!k_offsets && keys != T)) return CORAL_ERR_SHAPE;
-    if (!head_dim_known(head_dim) || q_heads > kMostHeads) return CORAL_ERR_UNSUPPORTED;
+    if (!head_dim_known(head_dim) || q_heads > kMostHeads || S > kMostSequences) return CORAL_ERR_UNSUPPORTED;
     if (T == 0) return CORAL_OK;
     PromptParams p = {};
     Rows in_q, in_k = {}, in_v = {}, out_rows;
@@ -61,7 +61,7 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     if (rows_overlap(out_rows, in_q) || rows_overlap(out_rows, in_k) || rows_overlap(out_rows, in_v) ||
         rows_overlap(out_rows, {q_offsets, offsets, offsets, 1}) || rows_overlap(out_rows, {k_offsets, offsets, offsets, 1}))
         return CORAL_ERR_UNSUPPORTED;
-    const int not_full = S < T ? S : T;                    // each sequence has at most one tile that is not full
+    const int not_full = S < T || S > kPromptLevelled ? S : T;       // each sequence has at most one tile that is not full
     const bool f32 = dt == CORAL_F32;
     const bool few = (T / (f32 ? 64ll : 128ll) + not_full) * q_heads <= (f32 && head_dim != 256 ? kFewUnitsF32 : kFewUnits) && keys / S >= kFewKeys;
     const PromptForm form = prompt_form(dt, head_dim, few);
@@ -70,7 +70,7 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
     int parts = 1;
     while (q_heads * parts % kXcds) parts *= 2;
     const int64_t units = (tiles + parts - 1) / parts * q_heads * parts;
-    if (units > INT32_MAX - 64) return CORAL_ERR_UNSUPPORTED;
+    if (units * form.threads > UINT32_MAX) return CORAL_ERR_UNSUPPORTED;
     p.q = static_cast<const char*>(q); p.k = static_cast<const char*>(k); p.v = static_cast<const char*>(v);
     p.out = static_cast<char*>(out);
     p.q_stride = in_q.stride; p.k_stride = in_k.stride; p.v_stride = in_v.stride; p.out_stride = out_rows.stride;

@@ -89,7 +89,7 @@ def test_nothing_to_do_is_no_error():
 @pytest.mark.parametrize("status,cache,kw", [
     (NULL, None, {}), (NULL, {}, dict(k=None)), (NULL, {}, dict(v=None)), (NULL, {}, dict(slots=None)), (SHAPE, {}, dict(T=-1)), (SHAPE, {}, dict(dt=7)),
     (SHAPE, {}, dict(k_stride=1016)), (UNSUPPORTED, {}, dict(v_stride=1025)), (UNSUPPORTED, {}, dict(v=at(1) + 4)), (UNSUPPORTED, {}, dict(slots=at(2) + 2)),
-    (UNSUPPORTED, {}, dict(k=at(22))), (UNSUPPORTED, {}, dict(slots=at(23))), (UNSUPPORTED, dict(head_dim=32), {}), (SHAPE, dict(kv_heads=0), {}),
+    (UNSUPPORTED, {}, dict(k=at(22))), (UNSUPPORTED, {}, dict(slots=at(23))), (UNSUPPORTED, {}, dict(T=1 << 24)), (UNSUPPORTED, dict(head_dim=32), {}), (SHAPE, dict(kv_heads=0), {}),
     (UNSUPPORTED, dict(kv_heads=1025), dict(k_stride=1 << 20, v_stride=1 << 20)),
 ])
 def test_kv4_append_refusals(status, cache, kw):
@@ -146,7 +146,8 @@ def prompt(**kw):
     (SHAPE, dict(dt=3)), (SHAPE, dict(k_stride=1016)), (UNSUPPORTED, dict(head_dim=96)), (UNSUPPORTED, dict(q_heads=2048, q_stride=2048 * 128)),
     (UNSUPPORTED, dict(v=at(2) + 8)), (UNSUPPORTED, dict(v_stride=1028)), (UNSUPPORTED, dict(k_stride=1 << 24)), (UNSUPPORTED, dict(q_offsets=at(3) + 2)),
     (UNSUPPORTED, dict(out=at(0))), (UNSUPPORTED, dict(out=at(1) + 512)), (UNSUPPORTED, dict(out=at(2))), (UNSUPPORTED, dict(out=at(3))),
-    (UNSUPPORTED, dict(k_offsets=at(4))),
+    (UNSUPPORTED, dict(k_offsets=at(4))), (UNSUPPORTED, dict(S=65536)), (UNSUPPORTED, dict(T=1 << 24, keys=1 << 24)), (UNSUPPORTED, dict(keys=1 << 24, k_offsets=at(5))),
+    (UNSUPPORTED, dict(T=1 << 23, keys=1 << 23, q_heads=1024, q_stride=1024 * 128)),         # more threads than a grid's 32 bits count
 ])
 def test_attention_prompt_refusals(status, kw):
     assert prompt(**kw) == status

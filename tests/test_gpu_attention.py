@@ -543,6 +543,22 @@ def test_attention_prompt_many_sequences(coral):
     c.check(c.run())
 
 
+@pytest.mark.parametrize("count", [256, 257, 2000, 4097])
+def test_attention_prompt_sequences_beyond_those_ordered_by_length(coral, count):
+    rng = np.random.default_rng(count)
+    n = rng.choice([0, 1, 1, 2, 5, 31, 64, 127, 128, 129, 300], count)
+    c = Prompt(coral, "bf16", [(int(a), int(a)) for a in n], 3, 1, 64, behind=5)
+    out = torch.full_like(c.q, 7)
+    c.run(out=out)
+    ends = np.concatenate([[0], np.cumsum(n)])
+    assert bool((out[ends[-1]:] == 7).all())
+    for s in np.unique(np.r_[0:8, count - 8:count, rng.integers(0, count, 40)]):
+        rows = slice(ends[s], ends[s + 1])
+        want = plain.attention(c.q64[rows], c.k64[rows], c.v64[rows], np.tri(int(n[s]), dtype=bool), 64 ** -0.5)
+        check_attention(host(out[rows]), want, "bf16", int(n[s]))
+    assert bool((out[:ends[-1]] != 7).any(dim=-1).all())         # no row is left out
+
+
 def test_attention_prompt_peaked_scores(coral):
     for dtype in DTYPES:
         c = Prompt(coral, dtype, [(300, 300), (40, 90)], 4, 2, 128, q_size=40.0)
