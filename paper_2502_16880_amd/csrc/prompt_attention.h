@@ -19,7 +19,7 @@ namespace {
 
 constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
 constexpr int kXcds = 8;
-constexpr int kPromptLevelled = 256;                        // sequences beyond which tiles come in the sequences' order
+constexpr int kPromptLevelled = kWave;                      // sequences beyond which tiles come in the sequences' order
 
 struct PromptParams {
     const char *q, *k, *v;
@@ -62,6 +62,7 @@ __device__ __forceinline__ int wave_sum_int(int x) { return __builtin_amdgcn_rea
 // L2: of `parts` as few as make the heads' parts a multiple of eight, a part being every parts-th tile.  Tiles of all of a
 // die's heads come by their levels, the longest first: twelve prompts of 8191 tokens whose tiles came in order took 148 us,
 // the last of them alone, against 118; one of 8192 whose tiles came head after head 527 us against 508, of 2115 64 against 55.
+// More than 64 sequences come in their own order, found by a search (levels of 256 prompts of 300 tokens: 994 us, order 664).
 template <int ROWS>
 __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, int lane) {
     PromptTile r = {};
@@ -98,53 +99,25 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, 
         r.any = i >= 0 && i < tiles;
     } else {
         // the largest level l that, with all above it, has more than `rank` tiles
-        auto chunk = [&](int s0) CORAL_INLINE {
-            if (p.S > kWave) q = prompt_sequence<ROWS>(p, s0 + lane);
-        };
         auto from_level = [&](int l) CORAL_INLINE {
-            int n = 0;
-            for (int s0 = 0; s0 < p.S; s0 += kWave) {
-                chunk(s0);
-                const int k = q.tiles + q.base - l + 1;
-                n += wave_sum_int(k < 0 ? 0 : k > q.tiles ? q.tiles : k);
-            }
-            return n;
+            const int k = q.tiles + q.base - l + 1;
+            return wave_sum_int(k < 0 ? 0 : k > q.tiles ? q.tiles : k);
         };
-        int top = 0;
-        for (int s0 = 0; s0 < p.S; s0 += kWave) {
-            chunk(s0);
-            int m = q.tiles ? q.tiles + q.base : 0;
-#pragma unroll
-            for (int i = 32; i; i >>= 1) {
-                const int o = __shfl_xor(m, i, kWave);
-                m = o > m ? o : m;
-            }
-            top = m > top ? m : top;
-        }
-        top = __builtin_amdgcn_readfirstlane(top);
         if (from_level(1) <= rank) return r;
-        int low = 1, high = top + 1;                         // from_level(low) > rank >= from_level(high)
-        while (high - low > 1) {
+        const float top = q.tiles ? (float)(q.tiles + q.base) : 0.f;       // (to 24 bits: a few levels too many at most)
+        int low = 1, high = __builtin_amdgcn_readfirstlane((int)(lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(top, [](float x, float y) { return fmaxf(x, y); }))) * 1.000001f)) + 2;
+        while (high - low > 1) {                             // from_level(low) > rank >= from_level(high)
             const int mid = low + (high - low) / 2;
             if (from_level(mid) > rank) low = mid;
             else high = mid;
         }
-        int left = rank - from_level(high);                  // so many sequences of the level come before
-        for (int s0 = 0; s0 < p.S && !r.any; s0 += kWave) {
-            chunk(s0);
-            const int i = low - 1 - q.base;
-            const bool has = i >= 0 && i < q.tiles;
-            const uint64_t all = __builtin_amdgcn_ballot_w64(has);
-            const int n = __builtin_popcountll(all);
-            if (left >= n) {
-                left -= n;
-                continue;
-            }
-            src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(has && __builtin_popcountll(all & ((1ull << lane) - 1ull)) == left));
-            seq = s0 + src;
-            r.any = true;
-            r.first = __builtin_amdgcn_readlane(i, src) * ROWS;
-        }
+        const int left = rank - from_level(high);            // so many sequences of the level come before
+        const int i = low - 1 - q.base;
+        const bool has = i >= 0 && i < q.tiles;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(has);
+        seq = src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(has && __builtin_popcountll(all & ((1ull << lane) - 1ull)) == left));
+        r.any = true;
+        r.first = __builtin_amdgcn_readlane(i, src) * ROWS;
     }
     if (!r.any) return r;
     r.row0 = __builtin_amdgcn_readlane(q.row0, src);

@@ -543,7 +543,7 @@ def test_attention_prompt_many_sequences(coral):
     c.check(c.run())
 
 
-@pytest.mark.parametrize("count", [256, 257, 2000, 4097])
+@pytest.mark.parametrize("count", [64, 65, 257, 2000, 4097])
 def test_attention_prompt_sequences_beyond_those_ordered_by_length(coral, count):
     rng = np.random.default_rng(count)
     n = rng.choice([0, 1, 1, 2, 5, 31, 64, 127, 128, 129, 300], count)
