@@ -726,11 +726,20 @@ def _kv4_cache(cache, device):
     if max(codes) > _INT_MAX // 2:
         raise ValueError("sizes must fit 32 bits")
     u8, scales = torch.uint8, (pages, kv_heads, page_size, half // 16)
-    struct = _Kv4CacheStruct(_same_device_ptr(k_codes, "k_codes", device, u8, codes),
-                             _same_device_ptr(k_scales, "k_scales", device, u8, scales),
-                             _same_device_ptr(v_codes, "v_codes", device, u8, codes),
-                             _same_device_ptr(v_scales, "v_scales", device, u8, scales), pages, page_size, kv_heads, half * 2)
+    # what _same_device_ptr checks of each, in one expression (1 us less a call); it names what is wrong
+    if not (k_codes.dtype is u8 and v_codes.dtype is u8 and k_scales.dtype is u8 and v_scales.dtype is u8
+            and k_codes.device == device and v_codes.device == device and k_scales.device == device and v_scales.device == device
+            and v_codes.shape == codes and k_scales.shape == scales and v_scales.shape == scales
+            and k_codes.is_contiguous() and v_codes.is_contiguous() and k_scales.is_contiguous() and v_scales.is_contiguous()):
+        for t, name in zip(cache, KV4Cache._fields):
+            _same_device_ptr(t, name, device, u8, codes if name.endswith("codes") else scales)
+    struct = _Kv4CacheStruct(k_codes.data_ptr(), k_scales.data_ptr(), v_codes.data_ptr(), v_scales.data_ptr(), pages, page_size, kv_heads, half * 2)
     return ctypes.byref(struct), page_size, kv_heads, half * 2
+
+
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A dense tensor of this shape, type and device (1.3 us; torch.empty with the three of them 2.2)."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _heads_ptr(t: torch.Tensor, name: str, device, dtype) -> Tuple[int, int]:
@@ -755,7 +764,7 @@ def _heads_out(out, like, name, device, stream) -> Tuple[torch.Tensor, int, int]
     """(tensor, pointer, elements from token to token) of an output like `like`: the one given, or a new dense one."""
     if out is None:
         shape = like.shape
-        out = like.new_empty(shape) if stream is None else _new(shape, like.dtype, device, stream)
+        out = _like(like) if stream is None else _new(shape, like.dtype, device, stream)
         return out, out.data_ptr(), shape[1] * shape[2]
     if out.shape != like.shape:
         raise ValueError(f"{name} must be {list(like.shape)}, got {list(out.shape)}")
@@ -858,7 +867,7 @@ def coral_kv4_read(cache, slots: torch.Tensor, dtype: torch.dtype, k_out: Option
     else:
         k_ptr = _same_device_ptr(k_out, "k_out", dev, dtype, shape)
     if v_out is None:
-        v_out = _new(shape, dtype, dev, stream)
+        v_out = _like(k_out) if stream is None else _new(shape, dtype, dev, stream)
         v_ptr = v_out.data_ptr()
     else:
         v_ptr = _same_device_ptr(v_out, "v_out", dev, dtype, shape)
@@ -910,7 +919,7 @@ def coral_attention_kv4(q: torch.Tensor, cache, page_table: torch.Tensor, length
             _same_device_ptr(lengths, "lengths", dev, i32, (S,)), _same_device_ptr(q_offsets, "q_offsets", dev, i32, (S + 1,)),
             _same_device_ptr(history, "history", dev, i32, (S,)), _same_device_ptr(tree, "tree", dev, torch.int64, (T,)))
     if out is None:
-        out = q.new_empty((T, q_heads, D)) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
+        out = _like(q) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
         out_ptr = out.data_ptr()
     else:
         out_ptr = _same_device_ptr(out, "out", dev, dtype, (T, q_heads, D))
@@ -945,7 +954,7 @@ def coral_attention_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_
     offsets_ptr = _same_device_ptr(q_offsets, "q_offsets", dev, torch.int32, (S + 1,))
     k_offsets_ptr = _same_device_ptr(k_offsets, "k_offsets", dev, torch.int32, (S + 1,))
     if out is None:
-        out = q.new_empty((T, q_heads, D)) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
+        out = _like(q) if stream is None else _new((T, q_heads, D), dtype, dev, stream)
         out_ptr = out.data_ptr()
     else:
         out_ptr = _same_device_ptr(out, "out", dev, dtype, (T, q_heads, D))
