@@ -37,6 +37,7 @@ struct Kv4AttnParams {
     float2* part_stats;
     unsigned* arrived;                  // [workgroup] counters, kKv4ArrivalStride words apart, zero between calls
     int max_pages, T, S, max_rows, group, kv_heads, workgroups;
+    int join_heads;                     // of a wave in k_kv4_join, one after the other
     bool apart, join_inside;
     float scale_log2;                   // scores are kept in powers of two; above zero, the sign is taken by q
     unsigned q_sign;                    // bit to flip in every value of q
@@ -678,12 +679,11 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
     static_assert(WAVES == 1 || WAVES == kKv4Waves, "");
     __shared__ float sums[kKv4Waves][D];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int t = blockIdx.x, q_head = blockIdx.y * (kKv4Waves / WAVES) + wave / WAVES, of_row = wave % WAVES;
-    if (WAVES == 1 && q_head >= p.group * p.kv_heads) return;
+    const int t = blockIdx.x, of_row = wave % WAVES;
     Kv4Line<kRows> line;
-    unsigned long long total = 0, start = 0;
-    unsigned steps = 0;
-    int r = 0;
+    unsigned long long total = 0, base = 0;
+    unsigned steps = 0, blocks = 0;
+    int row = 0;
     for (int s = 0; s < p.S; s += kWave) {
         line.load(p, s, lane);
         const uint64_t found = __builtin_amdgcn_ballot_w64(t >= line.lanes.row0 && t < line.lanes.row0 + line.lanes.rows);
@@ -691,77 +691,84 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_join(Kv4AttnParams p) {
             const int src = __builtin_ctzll(found);
             const Kv4Item first = line.at(p, src, 0);
             steps = first.steps;
-            r = (t - first.row0) * p.group + q_head % p.group;
-            const unsigned blocks = (unsigned)(first.rows * p.group + kRows - 1) / kRows;
-            start = total + readlane64(line.upto, src) - readlane64(line.lanes.cost, src) + (unsigned long long)(q_head / p.group * blocks + r / kRows) * (steps + kKv4ItemSteps);
+            if (steps == 1) return;                              // one workgroup's, which has written it
+            row = (t - first.row0) * p.group;
+            blocks = (unsigned)(first.rows * p.group + kRows - 1) / kRows;
+            base = total + readlane64(line.upto, src) - readlane64(line.lanes.cost, src);
         }
         total += readlane64(line.upto, kWave - 1);
     }
     if (!steps) return;                                          // a row of no sequence
     line.deal(p, total);
-    const unsigned long long end = start + kKv4ItemSteps + steps;
-    const unsigned w0 = line.share_of(start + kKv4ItemSteps), last = line.share_of(end - 1);
-    if (w0 == last) return;                                      // one workgroup's, which has written it
-    // part j: share w0 + j; the first lies behind what else its share holds, unless it begins with the item
-    const int64_t first = ((int64_t)w0 * 2 + (line.begin(w0) >= start ? 0 : 1)) * kRows + r % kRows, others = (int64_t)(w0 + 1) * 2 * kRows + r % kRows;
-    const int parts = (int)(last - w0) + 1;
-    auto row_of = [&](int j) CORAL_INLINE { return j == 0 ? first : others + (int64_t)(j - 1) * 2 * kRows; };
-    float ref = -INFINITY, all = 0.f, o[N];
+    for (int h = 0; h < p.join_heads; ++h) {                     // (four waves a row: one)
+        const int q_head = (blockIdx.y * p.join_heads + h) * (kKv4Waves / WAVES) + wave / WAVES;
+        if (q_head >= p.group * p.kv_heads) return;
+        const int of_kv = q_head / p.group, r = row + q_head - of_kv * p.group;
+        const unsigned long long start = base + (unsigned long long)(of_kv * blocks + r / kRows) * (steps + kKv4ItemSteps);
+        const unsigned long long end = start + kKv4ItemSteps + steps;
+        const unsigned w0 = line.share_of(start + kKv4ItemSteps), last = line.share_of(end - 1);
+        if (w0 == last) continue;
+        // part j: share w0 + j; the first lies behind what else its share holds, unless it begins with the item
+        const int64_t first = ((int64_t)w0 * 2 + (line.begin(w0) >= start ? 0 : 1)) * kRows + r % kRows, others = (int64_t)(w0 + 1) * 2 * kRows + r % kRows;
+        const int parts = (int)(last - w0) + 1;
+        auto row_of = [&](int j) CORAL_INLINE { return j == 0 ? first : others + (int64_t)(j - 1) * 2 * kRows; };
+        float ref = -INFINITY, all = 0.f, o[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) o[n] = 0.f;
-    for (int j0 = 0; j0 < parts; j0 += kWave) {
-        float2 stat = make_float2(-INFINITY, 0.f);
-        if (j0 + lane < parts) stat = p.part_stats[row_of(j0 + lane)];
-        const int left = parts - j0 < kWave ? parts - j0 : kWave;
-        float x[8][N];
-        auto load = [&](int i) CORAL_INLINE {                    // eight parts of the wave's
+        for (int n = 0; n < N; ++n) o[n] = 0.f;
+        for (int j0 = 0; j0 < parts; j0 += kWave) {
+            float2 stat = make_float2(-INFINITY, 0.f);
+            if (j0 + lane < parts) stat = p.part_stats[row_of(j0 + lane)];
+            const int left = parts - j0 < kWave ? parts - j0 : kWave;
+            float x[8][N];
+            auto load = [&](int i) CORAL_INLINE {                    // eight parts of the wave's
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int j = i + u * WAVES + of_row;
-                const float* from = p.part + row_of(j0 + (j < left ? j : left - 1)) * D + lane * N;
+                for (int u = 0; u < 8; ++u) {
+                    const int j = i + u * WAVES + of_row;
+                    const float* from = p.part + row_of(j0 + (j < left ? j : left - 1)) * D + lane * N;
 #pragma unroll
-                for (int n = 0; n < N; ++n) x[u][n] = from[n];
+                    for (int n = 0; n < N; ++n) x[u][n] = from[n];
+                }
+            };
+            load(0);
+            float top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(stat.x, [](float a, float b) { return fmaxf(a, b); })));
+            top = fmaxf(top, ref);
+            const float keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top), by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
+            ref = top;
+            all = fmaf(all, keep, by * stat.y);
+#pragma unroll
+            for (int n = 0; n < N; ++n) o[n] *= keep;
+            for (int i = 0;;) {
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {
+                    const int j = i + u * WAVES + of_row;
+                    const float f = j < left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j & (kWave - 1))) : 0.f;
+#pragma unroll
+                    for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, x[u][n], o[n]);
+                }
+                i += 8 * WAVES;
+                if (i >= left) break;
+                load(i);
             }
-        };
-        load(0);
-        float top = lane_xor_max<16>(lane_xor_max<32>(lanes_reduce<16>(stat.x, [](float a, float b) { return fmaxf(a, b); })));
-        top = fmaxf(top, ref);
-        const float keep = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top), by = stat.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat.x - top);
-        ref = top;
-        all = fmaf(all, keep, by * stat.y);
-#pragma unroll
-        for (int n = 0; n < N; ++n) o[n] *= keep;
-        for (int i = 0;;) {
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int j = i + u * WAVES + of_row;
-                const float f = j < left ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), j & (kWave - 1))) : 0.f;
-#pragma unroll
-                for (int n = 0; n < N; ++n) o[n] = f == 0.f ? o[n] : fmaf(f, x[u][n], o[n]);
-            }
-            i += 8 * WAVES;
-            if (i >= left) break;
-            load(i);
         }
-    }
-    all = wave_sum(all);
-    char* to = p.out + (int64_t)t * p.out_stride + (int64_t)q_head * (D * kBytes);
-    auto put = [&](int d, float v) CORAL_INLINE {
-        const float y = all > 0.f ? v / all : all == 0.f ? 0.f : all;
-        if (DT == kF32) reinterpret_cast<float*>(to)[d] = y;
-        else reinterpret_cast<unsigned short*>(to)[d] = narrow16<DT>(y);
-    };
-    if (WAVES == 1) {
+        all = wave_sum(all);
+        char* to = p.out + (int64_t)t * p.out_stride + (int64_t)q_head * (D * kBytes);
+        auto put = [&](int d, float v) CORAL_INLINE {
+            const float y = all > 0.f ? v / all : all == 0.f ? 0.f : all;
+            if (DT == kF32) reinterpret_cast<float*>(to)[d] = y;
+            else reinterpret_cast<unsigned short*>(to)[d] = narrow16<DT>(y);
+        };
+        if (WAVES == 1) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) put(lane * N + n, o[n]);
-        return;
-    }
+            for (int n = 0; n < N; ++n) put(lane * N + n, o[n]);
+            continue;
+        }
 #pragma unroll
-    for (int n = 0; n < N; ++n) sums[wave][lane * N + n] = o[n];
-    __syncthreads();
-    if (threadIdx.x >= D) return;
-    const int d = threadIdx.x;
-    put(d, (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]));
+        for (int n = 0; n < N; ++n) sums[wave][lane * N + n] = o[n];
+        __syncthreads();
+        if (threadIdx.x >= D) return;
+        const int d = threadIdx.x;
+        put(d, (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]));
+    }
 }
 
 using kv4_attn_fn = void (*)(Kv4AttnParams);

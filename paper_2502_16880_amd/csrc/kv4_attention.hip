@@ -84,8 +84,11 @@ extern "C" coral_status coral_attention_kv4(const void* q, int64_t q_stride, con
         const bool one = plan.wave_a_row;
         const void* join = dt == CORAL_F32 ? coral_kv4_join_f32(head_dim, plan.tiles, one) : dt == CORAL_BF16 ? coral_kv4_join_bf16(head_dim, plan.tiles, one)
                                                                                                              : coral_kv4_join_f16(head_dim, plan.tiles, one);
-        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(T, one ? (q_heads + kKv4Waves - 1) / kKv4Waves : q_heads), dim3(kKv4Threads), 0,
-                           stream, p);
+        // where there are more rows than the chip holds waves, a wave takes several heads of a token, whose place it has looked up once
+        const int at_once = one ? kKv4Waves : 1, groups = (q_heads + at_once - 1) / at_once;
+        const int64_t heads = one ? (int64_t)T * groups / (kKv4Units * 8) : 1;
+        p.join_heads = (int)(heads < 1 ? 1 : heads < groups ? heads : groups);
+        hipLaunchKernelGGL(reinterpret_cast<kv4_join_fn>(const_cast<void*>(join)), dim3(T, (groups + p.join_heads - 1) / p.join_heads), dim3(kKv4Threads), 0, stream, p);
         if (hipGetLastError() != hipSuccess) return CORAL_ERR_HIP;
     }
     return CORAL_OK;

@@ -688,6 +688,17 @@ def test_rows_past_32_bits(coral):
     assert torch.equal(coral.coral_attention_kv4(far[:, :4], one, table, *args), coral.coral_attention_kv4(near[:, :4], one, table, *args))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("q_heads,kv_heads,D", [(14, 2, 64), (9, 9, 128), (6, 3, 256)])
+def test_attention_kv4_many_rows_joined_several_heads_a_wave(coral, dtype, q_heads, kv_heads, D):
+    c = Cached(coral, dtype, [(20 + 11 * (s % 50), 20) for s in range(110)], q_heads, kv_heads, D, 32, behind=2)
+    out = torch.full_like(c.q, 7)
+    c.run(out=out)
+    c.check(out, only=[0, 1, 30, 49, 50, 77, 108, 109])
+    assert bool((out[2200:] == 7).all()) and bool((out[:2200] != 7).any(dim=-1).all())
+    assert torch.equal(c.run()[:2200], out[:2200])
+
+
 def test_attention_kv4_more_rows_than_a_grid_has_in_its_second_part(coral):
     c = Cached(coral, "bf16", [(150 + s % 7, 64) for s in range(1030)], 2, 1, 64, 32, tree=True)
     out = c.run()
