@@ -5,16 +5,25 @@
 
 namespace {
 
-// Groups of waves share a workgroup's keys where the card has few rows, which do not see very few keys.  Measured for one prompt, by tiles
-// of 128 (fp32: 64) rows over all heads, us with one group and with several:
-//   16 bits, D = 64    192 30.9 24.7   384 57.4 42.7   756 131 135        fp32, D = 64    182 45.6 28.7   288 89 53   756 315 242   1512 933 887
-//            D = 128   96 12.8 12.6   256 27.3 23.9   384 39.8 34.5               D = 128   160 33.5 22.2   352 79 66   520 479 369   768 196 225
-//                      544 54.6 59.3   1056 148 154                               D = 256   32 39.8 31.5   128 167 105   272 345 264   504 694 809
-//            D = 256   136 88 57   256 156 112   504 329 385
+// Groups of waves share a workgroup's keys where the card has few rows, which do not see very few keys: where each compute unit has a
+// tile of rows at most, and for one prompt, whose long tiles go with short ones, where it has up to about two.  Measured by tiles of 128
+// (fp32: 64) rows over all heads, us with one group and with several:
+//   16 bits, one prompt, D = 64   192 30.9 24.7   384 57.4 42.7   441 93 78   560 78 75   756 131 135
+//                        D = 128  96 12.8 12.6   256 27.3 23.9   384 39.8 34.5   420 45.8 45.6   544 54.6 59.3   1056 148 154
+//                        D = 256  136 88 57   256 156 112   336 202 197   376 229 241   504 329 385
+//            several, D = 64      477 21.1 24.2, D = 128 348 20.7 23.4, behind older keys 364 32 40
+//   fp32, one prompt, D = 64      182 45.6 28.7   288 89 53   756 315 242   1512 933 887
+//                     D = 128     160 33.5 22.2   352 79 66   520 479 369   768 196 225
+//                     D = 256     32 39.8 31.5   128 167 105   272 345 264   504 694 809
 // (two groups of as many rows for 16 bits, of 64 for D = 256; for fp32 four of 32, two for D = 256).  A prompt of 100 tokens took 10.2
 // for 9.8 us in two groups, twenty of 200 in fp32 42 for 29, where a group of most has no keys.
-constexpr int64_t kFewUnits = 400, kFewUnitsF32 = 600;
+constexpr int64_t kFewUnits = 256, kFewUnitsOnePrompt = 400, kFewUnitsOnePromptNarrow = 600;
 constexpr int kFewKeys = 128;
+bool few_rows(int64_t units, int T, int keys, int S, int head_dim, bool f32) {
+    if (keys / S < kFewKeys) return false;
+    if (S > 1 || keys / 2 >= T) return units <= kFewUnits;
+    return units <= (head_dim == 64 || (f32 && head_dim == 128) ? kFewUnitsOnePromptNarrow : kFewUnitsOnePrompt);
+}
 constexpr int64_t kMostStride = 1 << 24;         // bytes: a tile's rows are addressed by 32-bit offsets
 
 using prompt_fn = void (*)(PromptParams);
@@ -63,7 +72,7 @@ extern "C" coral_status coral_attention_prompt(const void* q, int64_t q_stride, 
         return CORAL_ERR_UNSUPPORTED;
     const int not_full = S < T || S > kPromptLevelled ? S : T;       // each sequence has at most one tile that is not full
     const bool f32 = dt == CORAL_F32;
-    const bool few = (T / (f32 ? 64ll : 128ll) + not_full) * q_heads <= (f32 && head_dim != 256 ? kFewUnitsF32 : kFewUnits) && keys / S >= kFewKeys;
+    const bool few = few_rows((T / (f32 ? 64ll : 128ll) + not_full) * q_heads, T, keys, S, head_dim, f32);
     const PromptForm form = prompt_form(dt, head_dim, few);
     const int rows = form.rows;
     const int64_t tiles = T / rows + not_full;
