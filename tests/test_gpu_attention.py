@@ -699,6 +699,16 @@ def test_attention_kv4_many_rows_joined_several_heads_a_wave(coral, dtype, q_hea
     assert torch.equal(c.run()[:2200], out[:2200])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [1, 2, 9])
+def test_attention_kv4_one_long_sequence_among_short_ones(coral, dtype, rows):
+    """Joined as if parts were few, where one item has hundreds."""
+    c = Cached(coral, dtype, [(5 + s % 3, 1) for s in range(40)] + [(60000, rows)] + [(9, 2)] * 20, 8, 2, 64, 128)
+    out = c.run()
+    c.check(out, only=[0, 39, 40, 41, 60])
+    assert torch.equal(c.run(), out)
+
+
 def test_attention_kv4_more_rows_than_a_grid_has_in_its_second_part(coral):
     c = Cached(coral, "bf16", [(150 + s % 7, 64) for s in range(1030)], 2, 1, 64, 32, tree=True)
     out = c.run()
