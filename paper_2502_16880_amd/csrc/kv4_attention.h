@@ -281,12 +281,12 @@ __device__ __forceinline__ void kv4_write(const Kv4AttnParams& p, const Kv4Kept&
 }
 
 // A wave joins the parts of a row, D / 64 values a lane: the parts' statistics first, one a lane, then eight parts' sums
-// at a time.
-template <int DT, int D, class RowOf>
-__device__ __forceinline__ void kv4_join_row(const Kv4AttnParams& p, const Kv4Kept& item, int r, float inv_group, int lane, RowOf row_of) {
-    constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2;
-    const unsigned parts = item.parts;
-    float ref = -INFINITY, all = 0.f, o[N];
+// at a time.  Sums are relative to `ref` then, `all` is the sum of their weights.
+template <int D, class RowOf>
+__device__ __forceinline__ void kv4_join_row(const Kv4AttnParams& p, unsigned parts, int lane, RowOf row_of, float (&o)[D / kWave], float& ref, float& all) {
+    constexpr int N = D / kWave;
+    ref = -INFINITY;
+    all = 0.f;
 #pragma unroll
     for (int n = 0; n < N; ++n) o[n] = 0.f;
     for (unsigned j0 = 0; j0 < parts; j0 += kWave) {
@@ -322,6 +322,10 @@ __device__ __forceinline__ void kv4_join_row(const Kv4AttnParams& p, const Kv4Ke
         }
     }
     all = wave_sum(all);
+}
+template <int DT, int D>
+__device__ __forceinline__ void kv4_write_row(const Kv4AttnParams& p, const Kv4Kept& item, int r, float inv_group, int lane, const float (&o)[D / kWave], float all) {
+    constexpr int N = D / kWave, kBytes = DT == kF32 ? 4 : 2;
     const float inv = all > 0.f ? 1.f / all : all == 0.f ? 0.f : all;
     const int i = (int)quotient20(r, inv_group);
     char* to = p.out + (int64_t)(item.row0 + i) * p.out_stride + (int64_t)(item.head * p.group + r - i * p.group) * (D * kBytes) + lane * (N * kBytes);
@@ -351,7 +355,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
     __shared__ __align__(256) char staged[kKv4Waves][kKv4Values<D>];
     __shared__ float wave_top[kKv4Waves][NT * 16], wave_sum_[kKv4Waves][NT * 16];
     __shared__ Kv4Kept kept;
-    __shared__ bool is_last;
+    __shared__ bool is_last[2];
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, g = lane >> 4;
     unsigned long long place, share_end;
@@ -640,32 +644,63 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
         }
     }
     if (end_of.parts > 1 && p.join_inside) {
-        // The item's last workgroup joins its parts.  They are counted in the word of the share that has its first step.
-        __builtin_amdgcn_s_waitcnt(0x0F70);                      // vmcnt(0): this wave's stores are out
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            unsigned* word = p.arrived + end_of.w0 * kKv4ArrivalStride;
-            const unsigned old = __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            is_last = old + 1 == end_of.parts;
-            if (is_last) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (is_last) {                                           // uniform
-            for (int r = wave; r < NT * 16 && end_of.first_row + r < end_of.n_rows; r += kKv4Waves) {
-                auto row_of = [&](unsigned j) CORAL_INLINE { return ((int64_t)(end_of.w0 + j) * 2 + (j == 0 && !end_of.opens ? 1 : 0)) * (NT * 16) + r; };
-                kv4_join_row<DT, D>(p, end_of, end_of.first_row + r, inv_group_, lane, row_of);
+        // The last workgroup of kEach neighbouring parts joins them, into the first one's place, and the last of these joins what has
+        // come together so (one long sequence among short ones: 384 parts joined by one workgroup took 45 us).  They are
+        // counted in the words of the shares that the neighbours begin with: the item's first (word 0) may be the last of
+        // an item before, which has that share in its second words.
+        constexpr unsigned kEach = D == 256 ? kKv4JoinParts / 2 : kKv4JoinParts;
+        int at_lane = lane, at_wave = wave;
+        asm volatile("" : "+v"(at_lane), "+s"(at_wave));         // (what follows from them would be held from the beginning on, and spilled)
+        const unsigned mine = blockIdx.x - end_of.w0, first = mine - mine % kEach, groups = (end_of.parts + kEach - 1) / kEach;
+        const unsigned in_group = end_of.parts - first < kEach ? end_of.parts - first : kEach;
+        auto place_of = [&](unsigned j) CORAL_INLINE { return ((int64_t)(end_of.w0 + j) * 2 + (j == 0 && !end_of.opens ? 1 : 0)) * (NT * 16); };
+        auto arrive = [&](unsigned* word, unsigned of, bool& last) CORAL_INLINE {
+            __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0): this wave's stores are out
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const unsigned old = __hip_atomic_fetch_add(word, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                last = old + 1 == of;
+                if (last) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
+            __syncthreads();
+            return last;
+        };
+        unsigned from = first, n = in_group, step = 1;
+        bool whole = groups == 1;
+        unsigned* word = p.arrived + (end_of.w0 + first) * kKv4ArrivalStride + (first ? 1 : 0);
+        while (arrive(word, n, is_last[whole])) {                // (uniform)
+            for (int r = at_wave; r < NT * 16 && end_of.first_row + r < end_of.n_rows; r += kKv4Waves) {
+                float o[D / kWave], top, all;
+                kv4_join_row<D>(p, n, at_lane, [&](unsigned j) CORAL_INLINE { return place_of(from + j * step) + r; }, o, top, all);
+                if (whole) {
+                    kv4_write_row<DT, D>(p, end_of, end_of.first_row + r, inv_group_, at_lane, o, all);
+                    continue;
+                }
+                const int64_t at_row = place_of(from) + r;
+                if (D == kWave) __hip_atomic_store(reinterpret_cast<unsigned*>(p.part + at_row * D + at_lane), __float_as_uint(o[0]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+                for (int i = 0; i + 1 < D / kWave; i += 2) publish2(p.part + at_row * D + at_lane * (D / kWave) + i, o[i], o[i + 1]);
+                if (at_lane == 0) publish2(&p.part_stats[at_row].x, top, all);
+            }
+            if (whole) break;
+            whole = true;
+            from = 0;
+            n = groups;
+            step = kEach;
+            word = p.arrived + end_of.w0 * kKv4ArrivalStride + 2;
         }
     }
-    place = end_of.place;
-    share_end = end_of.share_end;
+    asm volatile("" ::: "memory");                               // (read again: held over the join they would be spilled)
+    const Kv4Kept next = kv4_kept(kept);
+    place = next.place;
+    share_end = next.share_end;
     if (place >= share_end) return;
     __syncthreads();                                             // the sums have been read: the next item's values may come
-    line.load(p, end_of.s0, lane);
-    line.before = end_of.before;
-    line.each = end_of.each;
-    line.more = end_of.more;
-    line.shares = end_of.shares;
+    line.load(p, next.s0, lane);
+    line.before = next.before;
+    line.each = next.each;
+    line.more = next.more;
+    line.shares = next.shares;
     line.inv_shares = reciprocal(line.shares ? line.shares : 1);
     }
     }
