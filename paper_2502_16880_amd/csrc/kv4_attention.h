@@ -343,7 +343,7 @@ typedef const __attribute__((address_space(4))) Kv4AttnParams* Kv4ArgsPtr;
 // workgroup puts together, or, where parts and rows are many, k_kv4_join.
 // Bound by memory where one row reads a long cache (64 sequences of up to 8192 tokens, 32 heads of 128 on 8: 61 us, 4.9 TB/s; 131072 tokens:
 // 32); by a step's instructions for 32 rows (8 nodes over 131072 tokens: 41; 60 nodes of 28 heads on 4 over 4111: 21); for one token
-// over 2000 by the chain of dependent trips (10.5).  Work is dealt by cost (kKv4ItemSteps), not by sequences,
+// over 2000 by the chain of dependent trips (11).  Work is dealt by cost (kKv4ItemSteps), not by sequences,
 // whose lengths differ.
 template <int DT, int D, int NT, int TP>
 __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT)))) void k_kv4_attention(Kv4AttnParams) {
@@ -645,9 +645,9 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
     }
     if (end_of.parts > 1 && p.join_inside) {
         // The last workgroup of kEach neighbouring parts joins them, into the first one's place, and the last of these joins what has
-        // come together so (one long sequence among short ones: 384 parts joined by one workgroup took 45 us).  They are
-        // counted in the words of the shares that the neighbours begin with: the item's first (word 0) may be the last of
-        // an item before, which has that share in its second words.
+        // come together so (131072 tokens among 15 short sequences, 14 heads of 64 on 2: 67 us with one workgroup for all
+        // parts, 26 so).  Arrivals are counted in the words of the share that the neighbours begin with: word 0 of the item's
+        // first share, word 1 of others, which may be another item's first; word 2 of the first for the second step.
         constexpr unsigned kEach = D == 256 ? kKv4JoinParts / 2 : kKv4JoinParts;
         int at_lane = lane, at_wave = wave;
         asm volatile("" : "+v"(at_lane), "+s"(at_wave));         // (what follows from them would be held from the beginning on, and spilled)

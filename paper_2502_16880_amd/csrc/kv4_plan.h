@@ -18,7 +18,8 @@ constexpr int kKv4MostRows = 64;        // rows (tokens) of a sequence in one ca
 constexpr int kKv4Units = 256;          // compute units of the card
 constexpr int kKv4Apart = 256;          // sequences beyond which they are not shared out (each workgroup sums them all up)
 constexpr int kKv4JoinRows = 8;         // rows and parts of an item, at most, that one workgroup joins as fast as another
-constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave (D = 256: half as many; eight tokens' 34 parts 34 us, apart 22)
+constexpr int kKv4JoinParts = 40;       // kernel begins: two rows a wave (D = 256: half as many; eight tokens' 34 parts 34 us, apart 22).  An
+                                        // item that has more than sequences have on average is joined in two steps
 // Parts of an item, at most, that a wave joins by itself: 60 nodes over 4111 tokens (11 parts) 27.8 us with four waves a row, 25.9 with
 // one; 32 sequences' 16 rows (2 parts) 58.6 and 45.2; one token of 32768 (98 parts) 20.5 and 24.6, eight of 131072 (66) 48.8 and 51.2.
 constexpr int kKv4JoinWave = 16;
