@@ -36,7 +36,7 @@ constexpr int kPreparedWords = kWords + kGateScoreWords;
 // call uses them for both): one word a row, each in a 256-byte block of its own.
 constexpr int kRowArrival = kGateScores;
 constexpr int kRowArrivalStride = 64;
-// So do the workgroups of attention over the 4-bit cache that share a block of rows, in a word every fourth.
+// So do the workgroups of attention over the 4-bit cache that share a block of rows, in three words of every four.
 
 constexpr Entry kMap[] = {
     {"fused_arrival", kFusedArrival, 1},
