@@ -47,9 +47,11 @@ struct Kv4AttnParams {
 // one head of keys) times their steps of 128 tokens and what an item takes before and behind its steps (pages,
 // queries, sums: 3.5 us against 2 for a step among others; without it a share of short sequences took 82 us where
 // others took 47).  One sequence a lane.
+// `rows` are those taken, max_rows at most; `old` tokens are seen by all of them: with a tree the history's, without one row i of
+// all n rows that the offsets give sees old + i of them (old = length - n + 1, which may be below zero).
 constexpr unsigned kKv4ItemSteps = 3;
 struct Kv4Seq {
-    int row0, rows, length, history;
+    int row0, rows, length, old;
     unsigned steps;
     unsigned long long cost;
 };
@@ -62,12 +64,12 @@ __device__ __forceinline__ Kv4Seq kv4_sequence(const Kv4AttnParams& p, int s) {
     const int h = p.tree ? p.history[s] : 0;
     q.row0 = a < 0 ? 0 : a > p.T ? p.T : a;
     const int end = b > p.T ? p.T : b;
-    q.rows = end - q.row0 < p.max_rows ? end - q.row0 : p.max_rows;
-    q.rows = q.rows < 0 ? 0 : q.rows;
+    const int n = end - q.row0;
+    q.rows = n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
     const int64_t room = (int64_t)p.max_pages << p.cache.page_shift;
     length = length < 0 ? 0 : length > room ? (int)room : length;
-    q.history = h < 0 ? 0 : h > length ? length : h;
-    q.length = p.tree && length - q.history > 64 ? q.history + 64 : length;
+    q.old = !p.tree ? length - n + 1 : h < 0 ? 0 : h > length ? length : h;
+    q.length = p.tree && length - q.old > 64 ? q.old + 64 : length;
     q.steps = q.length > kKv4Step ? ((unsigned)q.length + kKv4Step - 1) / kKv4Step : 1;       // (rows that see nothing are written too)
     q.cost = (unsigned long long)((q.rows * p.group + ROWS - 1) / ROWS) * p.kv_heads * (q.steps + kKv4ItemSteps);
     return q;
@@ -92,7 +94,7 @@ __device__ __forceinline__ unsigned long long divide64(unsigned long long n, uns
 // An item (a block of a sequence's rows for one head of keys), and a place in it: step j is place
 // kKv4ItemSteps + j.
 struct Kv4Item {
-    int seq, row0, rows, length, history, head, first_row;
+    int seq, row0, rows, length, old, head, first_row;
     unsigned place, steps;
     __device__ __forceinline__ unsigned step_at(unsigned at) const {
         return at < kKv4ItemSteps ? 0 : at - kKv4ItemSteps < steps ? at - kKv4ItemSteps : steps;
@@ -157,7 +159,7 @@ struct Kv4Line {
         t.row0 = __builtin_amdgcn_readlane(lanes.row0, src);
         t.rows = __builtin_amdgcn_readlane(lanes.rows, src);
         t.length = __builtin_amdgcn_readlane(lanes.length, src);
-        t.history = __builtin_amdgcn_readlane(lanes.history, src);
+        t.old = __builtin_amdgcn_readlane(lanes.old, src);
         t.steps = (unsigned)__builtin_amdgcn_readlane((int)lanes.steps, src);
         const unsigned size = t.steps + kKv4ItemSteps, item = (unsigned)divide64(in, size), blocks = (unsigned)(t.rows * p.group + ROWS - 1) / ROWS;
         t.place = (unsigned)(in - (unsigned long long)item * size);
@@ -384,9 +386,8 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
     const unsigned size = work.steps + kKv4ItemSteps, rest = share_end - place < size - work.place ? (unsigned)(share_end - place) : size - work.place;
     const unsigned first_step = work.step_at(work.place), n_steps = work.step_at(work.place + rest) - first_step;
     if (n_steps == 0) break;                                     // the share ends before the item's first step
-    const int head = work.head, first_row = work.first_row, n_rows = work.rows * p.group, length = work.length, history = work.history;
+    const int head = work.head, first_row = work.first_row, n_rows = work.rows * p.group, length = work.length, old = work.old;
     const unsigned begin = first_step * kKv4Step, stop = begin + n_steps * kKv4Step, end = stop < (unsigned)length ? stop : (unsigned)length;
-    const int seen_by_all = p.tree ? history : length - (work.rows - 1);       // row i of n sees tokens up to length - n + i
 
     // Pages of the wave's next 32 steps, two tiles of 16 tokens each: one a lane.
     const int32_t* table = p.page_table + (int64_t)work.seq * p.max_pages;
@@ -477,7 +478,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int r = first_row + n * 16 + col, i = (int)quotient20(r < n_rows ? r : n_rows - 1, inv_group);
-        sees_to[n] = p.tree ? history : length - work.rows + i + 1;
+        sees_to[n] = p.tree ? old : old + i;
         sees[n] = p.tree ? p.tree[work.row0 + i] : 0;
     }
 
@@ -517,7 +518,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
                           kv4_operand<OT>(v[set][i].code[c], kv4_unit<DT>(v[set][i].scale[c / 4])));
         const int at = (int)now[set];
         const bool held0 = held[set][0], held1 = held[set][1];
-        const bool all_seen = at + kKv4WaveStep <= seen_by_all && held0 && held1;
+        const bool all_seen = at + kKv4WaveStep <= old && held0 && held1;
         fetch(set, step + 2);
         uint4 weight[NT][TP];
         float s[NT][8], to[NT];
@@ -529,7 +530,7 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
             if (!all_seen) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int token = at + (j / 4) * 16 + 4 * g + j % 4, bit = token - history;
+                    const int token = at + (j / 4) * 16 + 4 * g + j % 4, bit = token - old;
                     const bool in = token < sees_to[n] || (bit >= 0 && bit < 64 && (sees[n] >> (bit & 63) & 1));
                     s[n][j] = in && token < length && (j < 4 ? held0 : held1) ? s[n][j] : -INFINITY;
                 }

@@ -427,6 +427,27 @@ def test_attention_kv4_arguments_outside_the_arrays(coral):
     assert bool((out[2] == 7).all()) and bool((out[7:] == 7).all()) and torch.equal(out[3:5], want[3:5])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("most", [1, 2, 3, 7, 40])
+@pytest.mark.parametrize("D,q_heads,kv_heads,tree", [(64, 4, 1, False), (128, 8, 8, False), (128, 28, 4, False), (256, 2, 1, False), (128, 8, 2, True)])
+def test_attention_kv4_sequences_of_more_rows_than_are_taken(coral, dtype, D, q_heads, kv_heads, tree, most):
+    """Of n rows the first `most` are written, and row i still sees what row i of n does."""
+    sequences = [(100, 3), (50, 2), (70, 4), (5003, 41), (20, 33), (1, 2)]
+    for more in (0, 260) if dtype == "bf16" and D == 64 else (0,):          # (a sequence a workgroup beyond 256 sequences)
+        c = Cached(coral, dtype, sequences + [(40, 3)] * more, q_heads, kv_heads, D, 32, tree)
+        args, kw = c.args()
+        out = torch.full_like(c.q, 7)
+        coral.coral_attention_kv4(*args[:5], most, out=out, **kw)
+        got = host(out)
+        for s, (n, r) in enumerate(c.sequences[:8]):
+            k, held = plain.kv4_tokens(*c.sides[0], c.table[s], n, dtype)
+            v, _ = plain.kv4_tokens(*c.sides[1], c.table[s], n, dtype)
+            a, taken = c.offsets[s], min(r, most)
+            want = plain.attention(c.q64[a:a + taken], k, v, c.seen(s)[:taken] & held[None], D ** -0.5)
+            check_attention(got[a:a + taken], want, dtype, n, f"sequence {s} of {n} tokens, {taken} of {r} rows")
+            assert (got[a + taken:a + r] == 7).all()
+
+
 def test_attention_kv4_a_query_that_is_not_finite_spoils_only_itself(coral):
     for dtype in DTYPES:
         c = Cached(coral, dtype, [(400, 6), (33, 2)], 4, 2, 128, 32)
