@@ -29,6 +29,9 @@ __device__ __forceinline__ float kv4_unit(unsigned byte) {
     return __uint_as_float((byte < most ? byte : most) << 23);
 }
 
+// An offset cut to an array of `most` rows: differences of two such never pass 32 bits, whatever the offsets are.
+__device__ __forceinline__ int cut_offset(int at, int most) { return at < 0 ? 0 : at > most ? most : at; }
+
 // Eight values of storage type DT as fp32, and back with one rounding to nearest even.
 template <int DT>
 __device__ __forceinline__ void widen8(const uint4 (&raw)[DT == kF32 ? 2 : 1], float (&x)[8]) {

@@ -59,12 +59,10 @@ template <int ROWS>
 __device__ __forceinline__ Kv4Seq kv4_sequence(const Kv4AttnParams& p, int s) {
     Kv4Seq q = {};
     if (s >= p.S) return q;
-    const int a = p.q_offsets[s], b = p.q_offsets[s + 1];
     int length = p.lengths[s];
     const int h = p.tree ? p.history[s] : 0;
-    q.row0 = a < 0 ? 0 : a > p.T ? p.T : a;
-    const int end = b > p.T ? p.T : b;
-    const int n = end - q.row0;
+    q.row0 = cut_offset(p.q_offsets[s], p.T);
+    const int n = cut_offset(p.q_offsets[s + 1], p.T) - q.row0;
     q.rows = n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
     const int64_t room = (int64_t)p.max_pages << p.cache.page_shift;
     length = length < 0 ? 0 : length > room ? (int)room : length;

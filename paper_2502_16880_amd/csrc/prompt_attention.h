@@ -45,9 +45,8 @@ template <int ROWS>
 __device__ __forceinline__ PromptSeq prompt_sequence(const PromptParams& p, int s) {
     PromptSeq q = {0, 0, 0, 0};
     if (s >= p.S) return q;
-    const int a = p.q_offsets[s], b = p.q_offsets[s + 1];
-    q.row0 = a < 0 ? 0 : a > p.T ? p.T : a;
-    q.rows = (b > p.T ? p.T : b) - q.row0;
+    q.row0 = cut_offset(p.q_offsets[s], p.T);
+    q.rows = cut_offset(p.q_offsets[s + 1], p.T) - q.row0;
     q.rows = q.rows < 0 ? 0 : q.rows;
     q.tiles = (q.rows + ROWS - 1) / ROWS;
     if (p.k_offsets) {
@@ -80,10 +79,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, 
         r.any = r.first >= 0;
     } else if (p.S > kPromptLevelled) {
         // sequence s has the places from before(s) on: at least as many as it has tiles
-        auto before = [&](int s) CORAL_INLINE {
-            const int a = p.q_offsets[s];
-            return (a < 0 ? 0 : a > p.T ? p.T : a) / ROWS + s;
-        };
+        auto before = [&](int s) CORAL_INLINE { return cut_offset(p.q_offsets[s], p.T) / ROWS + s; };
         for (int n = p.S; n > 1;) {                          // among the n from seq on, 64 at once
             const int step = (n + kWave - 1) / kWave;
             const bool reached = lane * step < n && before(seq + (lane * step < n ? lane * step : 0)) <= rank;
@@ -125,9 +121,8 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptParams& p, int x, 
     r.k0 = r.row0;
     r.keys = r.rows;
     if (p.k_offsets) {
-        const int ka = p.k_offsets[seq], kb = p.k_offsets[seq + 1];
-        r.k0 = ka < 0 ? 0 : ka > p.keys ? p.keys : ka;
-        r.keys = (kb > p.keys ? p.keys : kb) - r.k0;
+        r.k0 = cut_offset(p.k_offsets[seq], p.keys);
+        r.keys = cut_offset(p.k_offsets[seq + 1], p.keys) - r.k0;
         r.keys = r.keys < 0 ? 0 : r.keys;
     }
     return r;

@@ -608,6 +608,39 @@ def test_attention_prompt_rows_of_no_sequence_and_offsets_outside(coral):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_attention_offsets_of_any_number(coral, dtype):
+    """Offsets whose differences pass 32 bits: such sequences have no rows, or no keys."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    c = Cached(coral, dtype, [(100, 3), (50, 2), (70, 4)], 4, 1, 64, 32)
+    (q, cache, table, lengths, _, rows), _ = c.args()
+    out = torch.full_like(q, 7)
+    coral.coral_attention_kv4(q, cache, table, lengths, ints([8, low, 5, 0]), 4, out=out)                   # none, [0,5), none
+    n, k, v = 50, *(plain.kv4_tokens(*side, c.table[1], 50, dtype)[0] for side in c.sides)
+    seen = np.arange(n)[None] <= (n - 5 + np.arange(4))[:, None]                                            # (four of five are taken)
+    check_attention(host(out)[:4], plain.attention(c.q64[:4], k, v, seen, 64 ** -0.5), dtype, n)
+    assert bool((out[4:] == 7).all())
+    for offsets in ([8, low, low, low], [high, low, low, -7], [9, 5, low, -1]):
+        out.fill_(7)
+        coral.coral_attention_kv4(q, cache, table, lengths, ints(offsets), 4, out=out)
+        assert bool((out == 7).all())
+    p = Prompt(coral, dtype, [(40, 40), (30, 30)], 4, 2, 64, behind=5)
+    want = coral.coral_attention_prompt(p.q[:70], p.k[:70], p.v[:70], ints([0, 40, 70]))
+    out = torch.full_like(p.q, 7)
+    for offsets in ([60, low, low], [high, low, -5], [75, 74, low]):
+        coral.coral_attention_prompt(p.q, p.k, p.v, ints(offsets), out=out)
+        assert bool((out == 7).all())
+    coral.coral_attention_prompt(p.q, p.k, p.v, ints([60, low, 40]), out=out)                               # none, [0,40)
+    assert torch.equal(out[:40], want[:40]) and bool((out[40:] == 7).all())
+    out.fill_(7)
+    coral.coral_attention_prompt(p.q, p.k, p.v, ints([0, 40, 70]), k_offsets=ints([60, low, low]), out=out)
+    assert bool((out[:70] == 0).all()) and bool((out[70:] == 7).all())                                      # rows without keys
+    out, kept = guarded(p.q.shape, TORCH[dtype])
+    more = ints([75, low] * 40)                                                                             # beyond those ordered by length
+    coral.coral_attention_prompt(p.q, p.k, p.v, more, k_offsets=more, out=out)
+    kept()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("heads", [4, 256])
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_attention_prompt_values_that_are_not_finite_reach_only_rows_that_see_them(coral, dtype, D, heads):
