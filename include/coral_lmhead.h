@@ -530,7 +530,8 @@ coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, 
  *                 b < 64: a draft tree's nodes see their ancestors and themselves
  * and never a token from lengths[s] on.  A row that sees nothing is zero.  Products are exact but for the
  * weights p, which keep the bits of the storage type, or twice as many where a sequence has at most 16
- * rows of queries for a head of keys; sums and statistics are fp32.
+ * rows of queries for a head of keys (fp16: of weights down to 2^-21 of the row's largest, smaller ones are
+ * multiples of 2^-31 of it); sums and statistics are fp32.
  *   q          [device] [T,q_heads,head_dim] storage type dt
  *   page_table [device] [S,max_pages] int32; tokens of a page that is none of the cache's are not seen
  *   lengths    [device] [S] int32: tokens in the cache, the new ones among them; cut to 0 .. max_pages *
@@ -563,7 +564,7 @@ coral_status coral_attention_kv4(const void *q, int64_t q_stride, const coral_kv
  * k_offsets[s+1], m of them; its row i sees keys 0 .. m - n + i (with m = n: itself and all before; with
  * m > n: a prompt that goes on behind keys that are there; with m < n: the first n - m rows see nothing).
  * A row that sees nothing is zero.  Scores, statistics and sums are fp32; the weights p are rounded to the
- * storage type.
+ * storage type (fp16: as above).
  *   q    [device] [T,q_heads,head_dim], k and v [device] [keys,kv_heads,head_dim], storage type dt;
  *        keys and values may be 0 tokens (and NULL); their strides at most 2^24 bytes
  *   q_offsets, k_offsets [device] [S+1] int32, ascending, cut to 0 .. T and 0 .. keys; k_offsets NULL: the

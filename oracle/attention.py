@@ -124,15 +124,16 @@ def attention(q, k, v, seen, scale):
 
 WEIGHT_STEP = {"f32": 2.0 ** -23, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}       # of a weight's rounding in the second product
 
-SMALLEST_WEIGHT = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}
+SMALLEST_WEIGHT = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -32}
 
 
 def attention_bound(out, mean, spread, score_off, size_v, keys, dtype):
     """Largest error: a weight is off by e^(twice a score's error) - 1, the exponential (4 half steps) and its
     rounding, the sums over keys by a rounding each, and the result is divided and rounded.  Weights are kept
     relative to a reference at most as large as the row's largest (their sum is then 1 or more); fp32 and bf16
-    end at 2^-126, where the exponential and the products give zero, so each key's weight (fp16: of normal
-    numbers from 2^-14 on, subnormal ones to steps of 2^-24) may be off by that much too."""
+    end at 2^-126, where the exponential and the products give zero, so each key's weight may be off by that much
+    too.  fp16 weights have normal numbers from 2^-14 on and subnormal ones in steps of 2^-24, relative to a
+    reference at least 2^7 below the row's largest: off by half a step, 2^-32 of it."""
     part = 2.2 * score_off[..., None] + WEIGHT_STEP[dtype] + (2 * keys + 16) * 2.0 ** -24
     off = part * (mean + np.abs(out)) + SMALLEST_WEIGHT[dtype] * size_v
     return off + rounding(np.abs(out) + off, dtype)

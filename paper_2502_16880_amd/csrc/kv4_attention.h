@@ -10,7 +10,7 @@
 // how the second product wants the weights; the values' operand needs eight tokens of one column in a
 // lane, so converted values pass through the wave's part of LDS and come back transposed
 // (ds_read_b64_tr_b16).  Softmax is taken in one pass: sums are kept relative to a reference of each
-// row that is moved up only when a score passes it by 2^8, so most steps do not touch the sums.
+// row that is moved up only when a weight would pass 2^8 (kWeightsAt), so most steps do not touch the sums.
 // Operands of fp16 calls are fp16 (an append of fp16 values has no others), those of fp32 calls three bf16 values for
 // one; so are the weights p.
 #pragma once
@@ -24,7 +24,6 @@ constexpr int kKv4Threads = 256;
 constexpr int kKv4ArrivalStride = 4;
 constexpr int kKv4Waves = kKv4Threads / kWave;
 constexpr int kKv4WaveStep = kKv4Step / kKv4Waves;          // 32 tokens
-constexpr float kMoveAt = 8.f;                               // weights stay below 2^8
 
 struct Kv4AttnParams {
     const char* q;
@@ -535,8 +534,8 @@ __global__ __launch_bounds__(kKv4Threads, (kv4_occupancy(D, NT, kv4_terms(DT))))
             }
             float top = fmaxf(fmaxf(fmaxf(s[n][0], s[n][1]), fmaxf(s[n][2], s[n][3])), fmaxf(fmaxf(s[n][4], s[n][5]), fmaxf(s[n][6], s[n][7])));
             top = lane_xor_max<16>(lane_xor_max<32>(top)) * scale_log2;
-            const bool move = top > ref[n] + kMoveAt || (ref[n] == -INFINITY && top > -INFINITY);
-            to[n] = move ? top : ref[n];
+            const bool move = top > ref[n] + (kWeightsAt<OT> + kWeightsUpTo) || (ref[n] == -INFINITY && top > -INFINITY);
+            to[n] = move ? top - kWeightsAt<OT> : ref[n];
             any |= move;
         }
         if (__builtin_amdgcn_ballot_w64(any)) {

@@ -17,7 +17,7 @@
 
 namespace {
 
-constexpr float kPromptMoveAt = 8.f;                         // a row's reference moves when a weight would pass 2^8
+constexpr float kNoReference = -3.402823466e38f;             // of a row before its first score: finite, so that a weight of -inf is zero
 constexpr int kXcds = 8;
 constexpr int kPromptLevelled = kWave;                      // sequences beyond which tiles come in the sequences' order
 
@@ -155,6 +155,8 @@ __device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)
 // Bound by the matrix cores and the clock they leave (8192 tokens, 32 heads of 128: 537 us, 1.02 PFLOP/s), where tiles of rows are few by a
 // row's chain: 1.0 us for a tile of keys, 0.43 of it products, and 5 before and behind (300 tokens: 11.8; twelve prompts of 8191: 118).
 // 128 rows a workgroup, as two of them fill a compute unit's registers and LDS and share their keys' reading.
+// A tile's weights are summed by themselves before they are added to the row's total: of tens of thousands of weights below 2^-25 of it
+// that are added two at a time none would arrive.
 // 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
 // (2^-12) each with random signs, which come to about the result's own rounding.
 // RW waves take 32 rows each; with KS = 2 two such groups take every second tile of keys and add up at the end, so that a
@@ -226,7 +228,7 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
     for (int d = 0; d < DT32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum[d][i] = 0.f;
-    float ref = -INFINITY, total = 0.f;
+    float ref = kNoReference, total = 0.f;
     const float scale_log2 = p.scale_log2;
     // operands' places in a buffer: keys (32 kt + col, piece 2 c + h), values (column 32 d + lane % 32; keys 16 c + 4 h + 0..3 and
     // 16 c + 8 + 4 h + 0..3: rows r = 4 h + lane % 16 / 4 and r + 8, lanes pointing at four pieces of eight bytes)
@@ -294,15 +296,14 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kt][i]);
             top = lane_xor_max<32>(top) * scale_log2;
-            const bool move = top > ref + kPromptMoveAt || (ref == -INFINITY && top > -INFINITY);
+            const bool move = top > ref + (kWeightsAt<DT> + kWeightsUpTo);
             if (__builtin_amdgcn_ballot_w64(move)) {
-                const float to = move ? top : ref, by = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to), keep = move ? by : 1.f;
+                const float to = move ? top - kWeightsAt<DT> : ref, keep = move ? __builtin_amdgcn_exp2f(ref - to) : 1.f;
                 ref = to;
                 total *= keep;
 #pragma unroll
                 for (int d = 0; d < DT32; ++d) sum[d] *= keep;
             }
-            const float base = ref == -INFINITY ? 0.f : ref;
             // values' operand i: columns of tile i % DT32, keys of chunk i / DT32
             constexpr int M = DT32 * KC, VAHEAD = 4;
             uint4 b[VAHEAD];
@@ -316,14 +317,15 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
             // Weights of keys 16 c + 8 (g / 2) + 4 h + 2 (g % 2) and the next, g = 0..3: the products of chunk c wait for these four
             // only, so the others' vector instructions run beside products.
             unsigned w[KC][4];
+            float part = 0.f;                                    // of the total: this tile's weights first (see above)
             auto weigh = [&](int c, int g) CORAL_INLINE {
                 const float x = s[c / 2][8 * (c % 2) + 2 * g], y = s[c / 2][8 * (c % 2) + 2 * g + 1];
-                w[c][g] = narrow2<DT>(__builtin_amdgcn_exp2f(fmaf(x, scale_log2, -base)), __builtin_amdgcn_exp2f(fmaf(y, scale_log2, -base)));
-                total = add_pair<DT>(w[c][g], total);            // of the weights as rounded: half the additions
+                w[c][g] = narrow2<DT>(__builtin_amdgcn_exp2f(fmaf(x, scale_log2, -ref)), __builtin_amdgcn_exp2f(fmaf(y, scale_log2, -ref)));
+                part = add_pair<DT>(w[c][g], part);              // of the weights as rounded: half the additions
             };
 #pragma unroll
             for (int g = 0; g < 4; ++g) weigh(0, g);
-            if (CUT && (lds.odd[group][j & 3] & keys_to(most))) total = NAN;
+            if (CUT && (lds.odd[group][j & 3] & keys_to(most))) part = NAN;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < M; ++i) {
@@ -336,6 +338,7 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
+            total += part;
         }
         dma_arrived();
         __syncthreads();
@@ -361,8 +364,7 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
         __syncthreads();
         if (group == 1) return;
         const float2 other = lds.stats[wave * 32 + col];
-        const float top = fmaxf(ref, other.x), mine = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - top);
-        const float its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x - top);
+        const float top = fmaxf(ref, other.x), mine = __builtin_amdgcn_exp2f(ref - top), its = __builtin_amdgcn_exp2f(other.x - top);
         total = total * mine + other.y * its;
 #pragma unroll
         for (int d = 0; d < DT32; ++d)
@@ -477,7 +479,7 @@ __global__ __launch_bounds__(RW * KS * kWave) void k_prompt_f32(PromptParams p) 
         }
         float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
         top = lane_xor_max<16>(lane_xor_max<32>(top));
-        const bool move = top > ref + kPromptMoveAt || (ref == -INFINITY && top > -INFINITY);
+        const bool move = top > ref + kWeightsUpTo || (ref == -INFINITY && top > -INFINITY);
         if (__builtin_amdgcn_ballot_w64(move)) {
             const float to = move ? top : ref, by = ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - to), keep = move ? by : 1.f;
             ref = to;
@@ -490,8 +492,8 @@ __global__ __launch_bounds__(RW * KS * kWave) void k_prompt_f32(PromptParams p) 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             w[i] = __builtin_amdgcn_exp2f(x[i] - base);
-            total += w[i];
         }
+        total += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
         if (j * KS + group >= first_cut && (odd[j & 1] & keys_to(most))) total = NAN;
 #pragma unroll
         for (int d = 0; d < DTILES; ++d)

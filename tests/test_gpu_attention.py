@@ -588,6 +588,58 @@ def test_attention_prompt_peaked_scores(coral):
         c.check(c.run(scale=0.0), scale=0.0)
 
 
+def beside_a_large_one(rows, heads, D, down, dtype, rng):
+    """Queries, and a key with 2^down times the weight that keys near zero have."""
+    q = stored(np.full((rows, heads, D), down * math.log(2) / math.sqrt(D)) * (1 + 0.01 * rng.random((rows, heads, 1))), dtype)
+    return (*q, np.ones((1, 1, D)))
+
+
+def check_beside(got, want, dtype, keys):
+    """The large key's score is one number for its whole row: the error of its sum in fp32 moves all values of a row
+    together (by less than half of score_off: partial sums are half the whole on average), which is below a half step of
+    the 16-bit types and not of fp32, so there each value's own bound is what holds."""
+    if dtype != "f32":
+        return check_attention(got, want, dtype, keys)
+    assert (np.abs(got - want[0]) <= plain.attention_bound(*want, keys, dtype)).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("down", [14.5, 20.0, 22.3, 25.5])
+@pytest.mark.parametrize("value", [0.0, 0.5])
+@pytest.mark.parametrize("rows,heads,D", [(1, 8, 64), (140, 4, 128), (2, 4, 256)])
+def test_attention_prompt_many_small_weights_beside_a_large_one(coral, dtype, down, value, rows, heads, D):
+    """As many small weights count by what they come to (the large one's value is nothing, or of the others' size)."""
+    rng, n = np.random.default_rng(8), 60000
+    q, q64, first = beside_a_large_one(rows, heads, D, down, dtype, rng)
+    k, k64 = stored(np.r_[first, 0.05 * rng.standard_normal((n - 1, 1, D))], dtype)
+    v, v64 = stored(np.r_[np.full((1, 1, D), value), 4 * rng.random((n - 1, 1, D))], dtype)
+    out = coral.coral_attention_prompt(q, k, v, ints([0, rows]), k_offsets=ints([0, n]))
+    pick = np.unique(np.r_[0, rows // 2, rows - 1])
+    check_beside(host(out)[pick], plain.attention(q64[pick], k64, v64, np.arange(n)[None] <= n - rows + pick[:, None], D ** -0.5), dtype, n)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("down", [22.3, 25.5])
+@pytest.mark.parametrize("value", [0x00, 0x11])
+@pytest.mark.parametrize("rows,heads,D", [(1, 8, 64), (3, 8, 64), (1, 8, 128), (5, 4, 128), (2, 4, 256)])
+def test_attention_kv4_many_small_weights_beside_a_large_one(coral, dtype, down, value, rows, heads, D):
+    """The same over the cache: by many workgroups, and (max_length 128) by one, whose waves each pass over a quarter of the keys."""
+    rng, n, page = np.random.default_rng(7), 131072, 256
+    q, q64, _ = beside_a_large_one(rows, heads, D, down, dtype, rng)
+    cache, sides = random_cache(coral, rng, n // page, page, 1, D, scales=(127, 128))
+    sides[0][1][:], sides[1][0][:] = 121, sides[1][0] & 0x77       # keys of at most 6/64, values without a sign
+    sides[0][0][0, 0, 0], sides[0][1][0, 0, 0], sides[1][0][0, 0, 0] = 0x22, 127, value
+    for tensors, arrays in ((cache[:2], sides[0]), (cache[2:], sides[1])):
+        for t, a in zip(tensors, arrays):
+            t.copy_(torch.from_numpy(a))
+    table = np.arange(n // page)
+    k, v = (plain.kv4_tokens(*side, table, n, dtype)[0] for side in sides)
+    want = plain.attention(q64, k, v, np.arange(n)[None] <= n - rows + np.arange(rows)[:, None], D ** -0.5)
+    for most in (None, 128):
+        out = coral.coral_attention_kv4(q, cache, ints(table[None]), ints([n]), ints([0, rows]), rows, max_length=most)
+        check_beside(host(out), want, dtype, n)
+
+
 def test_attention_prompt_rows_of_no_sequence_and_offsets_outside(coral):
     c = Prompt(coral, "f16", [(100, 100), (60, 60)], 4, 2, 64, behind=5)
     out, kept = guarded(c.q.shape, torch.float16)
