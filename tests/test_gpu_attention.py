@@ -207,6 +207,31 @@ def test_kv4_append_and_read(coral, dtype, T, kv_heads, D, page):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T,kv_heads,D,page", [(1, 1, 64, 16), (37, 3, 64, 32), (64, 4, 256, 128), (700, 12, 128, 16)])
+def test_kv4_append_of_what_was_read_changes_no_value_and_no_other_place(coral, dtype, T, kv_heads, D, page):
+    rng = np.random.default_rng(T)
+    pages = -(-T // page) + 2
+    cache, sides = random_cache(coral, rng, pages, page, kv_heads, D)
+    slots = rng.permutation(pages * page)[:T].astype(np.int64)
+    x = border_values(dtype, T * 2 * kv_heads * D // 32).reshape(T, 2 * kv_heads, D).cuda()
+    coral.coral_kv4_append(cache, x[:, :kv_heads], x[:, kv_heads:], ints(slots))
+    before = [t.cpu().numpy().copy() for t in cache]
+    held = coral.coral_kv4_read(cache, ints(slots), TORCH[dtype])
+    skip = rng.random(T) < 0.3                                     # places that are read but not appended to
+    coral.coral_kv4_append(cache, *held, ints(np.where(skip, -1, slots)))
+    after = [t.cpu().numpy() for t in cache]
+    at, off = slots[~skip] // page, slots[~skip] % page
+    for i in (0, 2):
+        old, new = (plain.kv4_values(side[i][at, :, off], side[i + 1][at, :, off], dtype) for side in (before, after))
+        rounded = torch.from_numpy(old).to(TORCH[dtype]).double().numpy()      # (what is read: units of few bits below the type's smallest)
+        assert np.array_equal(new, rounded)
+    for old, new in zip(before, after):                            # every other place has the bytes that it had
+        new = new.copy()
+        new[at, :, off] = old[at, :, off]
+        assert np.array_equal(old, new)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_kv4_read_any_byte(coral, dtype):
     rng = np.random.default_rng(5)
     cache, sides = random_cache(coral, rng, 16, 16, 2, 64, scales=(0, 256))
