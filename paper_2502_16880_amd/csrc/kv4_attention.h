@@ -44,8 +44,9 @@ struct Kv4AttnParams {
 
 // What the arguments say about a sequence, cut to the arrays, and what it takes: its items (a block of ROWS rows for
 // one head of keys) times their steps of 128 tokens and what an item takes before and behind its steps (pages,
-// queries, sums: 3.5 us against 2 for a step among others; without it a share of short sequences took 82 us where
-// others took 47).  One sequence a lane.
+// queries, sums).  Among others an item of n steps, four or more, takes 4.1 + 2.1 n us (one tile of rows, D = 128, bf16), 3.6 + 1.5 n
+// (D = 64), 7.7 + 1.5 n (D = 256), 4.7 + 1.7 n (fp32), 11 + 1.6 n (two tiles): as much as two to seven steps, of which three stand for
+// all (without them a share of short sequences took 82 us where others took 47).  One sequence a lane.
 // `rows` are those taken, max_rows at most; `old` tokens are seen by all of them: with a tree the history's, without one row i of
 // all n rows that the offsets give sees old + i of them (old = length - n + 1, which may be below zero).
 constexpr unsigned kKv4ItemSteps = 3;
