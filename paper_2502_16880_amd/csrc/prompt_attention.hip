@@ -8,20 +8,21 @@ namespace {
 // Groups of waves share a workgroup's keys where the card has few rows, which do not see very few keys: where each compute unit has a
 // tile of rows at most, and for one prompt, whose long tiles go with short ones, where it has up to about two.  Measured by tiles of 128
 // (fp32: 64) rows over all heads, us with one group and with several:
-//   16 bits, one prompt, D = 64   192 30.9 24.7   384 57.4 42.7   441 93 78   560 78 75   756 131 135
-//                        D = 128  96 12.8 12.6   256 27.3 23.9   384 39.8 34.5   420 45.8 45.6   544 54.6 59.3   1056 148 154
-//                        D = 256  136 88 57   256 156 112   336 202 197   376 229 241   504 329 385
-//            several, D = 64      477 21.1 24.2, D = 128 348 20.7 23.4, behind older keys 364 32 40
+//   16 bits, one prompt, D = 64   192 30.0 23.7   384 54.7 43.2   441 82.8 72.4   480 72.0 60.6   560 78 75   756 138 144
+//                        D = 128  96 11.8 11.7   256 25.8 22.9   384 38.3 34.5   420 47.2 45.6   544 55.4 60.6   1056 170 180
+//                        D = 256  136 76 56   256 135 109   280 148 136   304 161 160   336 179 193   504 304 376
+//            several, D = 64      576 20.9 23.5, D = 128 480 20.6 22.7, behind older keys 352 37.6 39.8, D = 256 232 61.7 43.7   328 63.7 61.9
 //   fp32, one prompt, D = 64      182 45.6 28.7   288 89 53   756 315 242   1512 933 887
 //                     D = 128     160 33.5 22.2   352 79 66   520 479 369   768 196 225
 //                     D = 256     32 39.8 31.5   128 167 105   272 345 264   504 694 809
 // (two groups of as many rows for 16 bits, of 64 for D = 256; for fp32 four of 32, two for D = 256).  A prompt of 100 tokens took 10.2
 // for 9.8 us in two groups, twenty of 200 in fp32 42 for 29, where a group of most has no keys.
-constexpr int64_t kFewUnits = 256, kFewUnitsOnePrompt = 400, kFewUnitsOnePromptNarrow = 600;
+constexpr int64_t kFewUnits = 256, kFewUnitsOnePrompt = 400, kFewUnitsOnePromptNarrow = 600, kFewUnitsOnePromptWide = 300;
 constexpr int kFewKeys = 128;
 bool few_rows(int64_t units, int T, int keys, int S, int head_dim, bool f32) {
     if (keys / S < kFewKeys) return false;
     if (S > 1 || keys / 2 >= T) return units <= kFewUnits;
+    if (head_dim == 256 && !f32) return units <= kFewUnitsOnePromptWide;
     return units <= (head_dim == 64 || (f32 && head_dim == 128) ? kFewUnitsOnePromptNarrow : kFewUnitsOnePrompt);
 }
 constexpr int64_t kMostStride = 1 << 24;         // bytes: a tile's rows are addressed by 32-bit offsets
