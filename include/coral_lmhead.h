@@ -530,8 +530,8 @@ coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, 
  *                 b < 64: a draft tree's nodes see their ancestors and themselves
  * and never a token from lengths[s] on.  A row that sees nothing is zero.  Products are exact but for the
  * weights p, which keep the bits of the storage type, or twice as many where a sequence has at most 16
- * rows of queries for a head of keys (fp16: of weights down to 2^-21 of the row's largest, smaller ones are
- * multiples of 2^-31 of it); sums and statistics are fp32.
+ * rows of queries for a head of keys (in fp16 calls no finer than 2^-31 of the row's largest); sums and
+ * statistics are fp32.
  *   q          [device] [T,q_heads,head_dim] storage type dt
  *   page_table [device] [S,max_pages] int32; tokens of a page that is none of the cache's are not seen
  *   lengths    [device] [S] int32: tokens in the cache, the new ones among them; cut to 0 .. max_pages *
@@ -545,7 +545,8 @@ coral_status coral_qk_norm_rope(const void *q, int64_t q_stride, const void *k, 
  *   workspace  [device] at least coral_attention_kv4_workspace_bytes(...) bytes, 256-byte aligned, prepared once by
  *              coral_lmhead_workspace_init with at least that many bytes (or filled with zeros); one of the
  *              heads' serves too, for calls that do not overlap
- * Limits: 1 <= S <= 65535.  q must be finite: a row with other values has unspecified results, others not.
+ * Limits: 1 <= S <= 65535; beyond 256 sequences each is one workgroup's for a head of keys, so one that is much longer than
+ * the others takes its own time.  q must be finite: a row with other values has unspecified results, others not.
  */
 size_t coral_attention_kv4_workspace_bytes(int S, int max_rows, int max_length, int q_heads,
                                            int kv_heads, int head_dim, coral_dtype dt);

@@ -31,7 +31,8 @@ enum RotationForm { kRotNone = 0, kRotPairs = 1, kRotLanes = 2, kRotAny = 3 };
 // over in LDS.  The partner of a value is in the same lane (kRotPairs: neighbours turn), in the lane
 // rot / 16 further (kRotLanes) or, where rot is no multiple of 16, anywhere (kRotAny: through LDS).
 // With CACHE the keys so made (rounded to DT first, as two calls would) and the values go into the cache.
-// Bound by memory: each value is read and written once (8192 tokens of 40 heads of 128, bf16: 33 us, 5.0 TB/s; one token: 3.1, the launch).
+// Bound by memory: each value is read and written once (8192 tokens of 40 heads of 128, bf16: 33 us, 5.0 TB/s; one token: 3.1, the launch).  With the
+// cache, whose pieces are 64 bytes, 49 us (the same tokens and 8 heads of values, 3.6 TB/s) and 3.4.
 template <int DT, int D, int FORM, bool CACHE>
 __global__ __launch_bounds__(kHeadThreads) void k_heads(HeadsParams p) {
     constexpr int kRaw = DT == kF32 ? 2 : 1, kLanes = D / 8, kPer = kWave / kLanes, kBytes = DT == kF32 ? 4 : 2;
@@ -167,8 +168,8 @@ struct Kv4Params {
 };
 
 // A token's keys and values into the cache, or out of it: eight values a lane, D / 8 lanes a head, first all
-// keys of a token, then its values.  Bound by memory, or by the launch (16384 tokens of 32 heads of 128, bf16: 87 us in, 4.0 TB/s, 97 out;
-// 8192 of 4: 7; 64 of 8: 2.9).
+// keys of a token, then its values.  Bound by the launch (8192 tokens of 4 heads of 128: 7 us; 64 of 8: 2.9), by pieces of
+// 64 bytes and a thread's two 64-bit divisions (16384 of 32, bf16: 88 us in, 98 out, 3.9 and 3.5 TB/s; fp32, 8192 of 8: 16 and 18).
 template <int DT, int D, bool READ>
 __global__ __launch_bounds__(kHeadThreads) void k_kv4_move(Kv4Params p) {
     constexpr int kRaw = DT == kF32 ? 2 : 1, kLanes = D / 8, kBytes = DT == kF32 ? 4 : 2;

@@ -341,8 +341,8 @@ typedef const __attribute__((address_space(4))) Kv4AttnParams* Kv4ArgsPtr;
 // Four waves take the steps of an item in turn, 32 tokens each of a step, and add up at the end.  A workgroup's share of
 // all steps is a run of them that may cross items: the first and the last may be parts of an item, which the item's last
 // workgroup puts together, or, where parts and rows are many, k_kv4_join.
-// Bound by memory where one row reads a long cache (64 sequences of up to 8192 tokens, 32 heads of 128 on 8: 61 us, 4.9 TB/s; 131072 tokens:
-// 32); by a step's instructions for 32 rows (8 nodes over 131072 tokens: 41; 60 nodes of 28 heads on 4 over 4111: 21); for one token
+// Bound by memory where one row reads a long cache (64 sequences of up to 8192 tokens, 32 heads of 128 on 8: 61 to 66 us, 4.9 to 4.6 TB/s;
+// 131072 tokens: 32); by a step's instructions for 32 rows (8 nodes over 131072 tokens: 43; 60 nodes of 28 heads on 4 over 4111: 21); for one token
 // over 2000 by the chain of dependent trips (11).  Work is dealt by cost (kKv4ItemSteps), not by sequences,
 // whose lengths differ.
 template <int DT, int D, int NT, int TP>
@@ -809,7 +809,8 @@ using kv4_attn_fn = void (*)(Kv4AttnParams);
 using kv4_join_fn = void (*)(Kv4AttnParams);
 // The weights p of bf16 and fp16 calls are two values of that type where a wave has one tile (which memory bounds: no cost;
 // the result's only rounding is then its own) and one where it has more (the products bound it: a second would take half
-// as long again; the roundings of single weights, 2^-9 and 2^-12 each, average out to about the result's own).
+// as long again; with the roundings of single weights, 2^-9 and 2^-12 each, the error against 64 bits is 1.2 (16 nodes, 4000 tokens) to
+// 1.4 (131072 tokens) times that of the result's rounding alone).
 template <int DT, int D>
 kv4_attn_fn kv4_kernel(int tiles) {
     constexpr int most = kv4_most_tiles(D, kv4_terms(DT)), many = kv4_terms(DT);

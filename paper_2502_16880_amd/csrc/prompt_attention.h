@@ -59,7 +59,7 @@ __device__ __forceinline__ int wave_sum_int(int x) { return __builtin_amdgcn_rea
 
 // Workgroups are dealt to the eight dies in turn, and a die takes neighbouring heads, whose keys are then read through one
 // L2: of `parts` as few as make the heads' parts a multiple of eight, a part being every parts-th tile.  Tiles of all of a
-// die's heads come by their levels, the longest first: twelve prompts of 8191 tokens whose tiles came in order took 148 us,
+// die's heads come by their levels, the longest first (each pair on one card): twelve prompts of 8191 tokens whose tiles came in order took 148 us,
 // the last of them alone, against 118; one of 8192 whose tiles came head after head 527 us against 508, of 2115 64 against 55.
 // More than 64 sequences come in their own order, found by a search (levels of 256 prompts of 300 tokens: 994 us, order 664).
 template <int ROWS>
@@ -152,13 +152,15 @@ __device__ __forceinline__ void dma_piece(Buffer from, unsigned at, unsigned lds
 }
 __device__ __forceinline__ void dma_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// Bound by the matrix cores and the clock they leave (8192 tokens, 32 heads of 128: 537 us, 1.02 PFLOP/s), where tiles of rows are few by a
-// row's chain: 1.0 us for a tile of keys, 0.43 of it products, and 5 before and behind (300 tokens: 11.8; twelve prompts of 8191: 118).
+// Bound by the matrix cores and the clock they leave (8192 tokens, 32 heads of 128: 515 to 557 us by card, 635 in calls one behind the
+// other; 1.07 to 0.87 PFLOP/s), where tiles of rows are few by a row's chain: 1.0 us for a tile of keys, 0.43 of it products, and 5 before
+// and behind (300 tokens: 11.8; twelve prompts of 8191: 111 to 125, 136).
 // 128 rows a workgroup, as two of them fill a compute unit's registers and LDS and share their keys' reading.
 // A tile's weights are summed by themselves before they are added to the row's total: of tens of thousands of weights below 2^-25 of it
 // that are added two at a time none would arrive.
 // 16-bit types.  Weights p are rounded to the storage type, as the products' operand: errors of 2^-9
-// (2^-12) each with random signs, which come to about the result's own rounding.
+// (2^-12) each with random signs.  With the result's own rounding the error against 64 bits is 1.15 (300 tokens) to 1.3 (8192) times
+// that of the rounding alone.
 // RW waves take 32 rows each; with KS = 2 two such groups take every second tile of keys and add up at the end, so that a
 // row's way along its keys is half as long (the entry point takes that where the card has few rows).
 template <int DT, int D, int RW, int KS>
@@ -390,7 +392,8 @@ __global__ __launch_bounds__(RW * KS * kWave, D == 256 ? 1 : 2) void k_prompt(Pr
 
 // fp32 on the matrix cores' fp32 products (a sixteenth of the 16-bit rate): 16 rows a wave, 32 keys at a time, no
 // rounding of the weights.  One value a lane and product: lane (key or column, g) has the g-th of four.  KS groups of RW waves
-// take every KS-th tile of keys, as in k_prompt.  Bound by the products (4096 tokens, 8 heads of 256: 750 us, 92 TFLOP/s).
+// take every KS-th tile of keys, as in k_prompt.  Bound by the products (4096 tokens, 8 heads of 256: 720 to 771 us, 95 to
+// 89 TFLOP/s).
 template <int D, int RW, int KS>
 __global__ __launch_bounds__(RW * KS * kWave) void k_prompt_f32(PromptParams p) {
     constexpr int kGroup = RW * kWave;
