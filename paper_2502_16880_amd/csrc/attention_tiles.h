@@ -7,8 +7,8 @@ namespace {
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 typedef __attribute__((ext_vector_type(4))) short s16x4_t;
 
-// A row's weights are powers of two relative to a reference: so far below the row's largest score when it is set, and moved when a
-// weight would pass 2^8 of that score's.  fp16 has no normal values below 2^-14 and none below 2^-24: with weights of up to 2^15
+// A row's weights are held relative to a reference: kWeightsAt powers of two below the largest score so far when it is set, and moved
+// when a score passes that one by kWeightsUpTo.  fp16 has no normal values below 2^-14 and none below 2^-24: with weights of up to 2^15
 // those that are 2^21 times smaller than the row's largest keep their bits, and down to 2^-32 of it they count (relative to the
 // largest itself 60000 weights of 2^-25.5 were lost beside it: off by 0.13 %, five half steps).  The factor cancels in the division.
 template <int DT>

@@ -10,7 +10,7 @@
 // how the second product wants the weights; the values' operand needs eight tokens of one column in a
 // lane, so converted values pass through the wave's part of LDS and come back transposed
 // (ds_read_b64_tr_b16).  Softmax is taken in one pass: sums are kept relative to a reference of each
-// row that is moved up only when a weight would pass 2^8 (kWeightsAt), so most steps do not touch the sums.
+// row that is moved up only when a score passes it by some powers of two (kWeightsUpTo), so most steps do not touch the sums.
 // Operands of fp16 calls are fp16 (an append of fp16 values has no others), those of fp32 calls three bf16 values for
 // one; so are the weights p.
 #pragma once
@@ -66,7 +66,7 @@ __device__ __forceinline__ Kv4Seq kv4_sequence(const Kv4AttnParams& p, int s) {
     q.rows = n < 0 ? 0 : n < p.max_rows ? n : p.max_rows;
     const int64_t room = (int64_t)p.max_pages << p.cache.page_shift;
     length = length < 0 ? 0 : length > room ? (int)room : length;
-    q.old = !p.tree ? length - n + 1 : h < 0 ? 0 : h > length ? length : h;
+    q.old = !p.tree ? length - (n > 0 ? n - 1 : 0) : h < 0 ? 0 : h > length ? length : h;
     q.length = p.tree && length - q.old > 64 ? q.old + 64 : length;
     q.steps = q.length > kKv4Step ? ((unsigned)q.length + kKv4Step - 1) / kKv4Step : 1;       // (rows that see nothing are written too)
     q.cost = (unsigned long long)((q.rows * p.group + ROWS - 1) / ROWS) * p.kv_heads * (q.steps + kKv4ItemSteps);
